@@ -168,6 +168,7 @@ def prepare(case, seed):
         else:
             s["q"] = _normal(gen, s["total"], case["heads"], d).to(dt)
             s["scale"] = d ** -0.5
+            s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty(s["total"], case["heads"], device="cuda")
         return s
     if kind == "product":
         M, N, K, G = case["rows"], case["n"], case["k"], case["group"]
@@ -177,6 +178,7 @@ def prepare(case, seed):
         s["unit"] = 2.0 ** -18
         x = _normal(gen, M, K)
         s["x"] = (x * 256).round().clamp(-32768, 32767).to(torch.int16) if case["dtype"] == "i16" else x.to(dt)
+        s["out"] = torch.empty(M, N, dtype=torch.int64 if case["dtype"] == "i16" else dt, device="cuda")
         return s
     M, V = case["rows"], case["vocab"]
     x = _normal(gen, M, V, scale=2.5)
@@ -199,21 +201,32 @@ def run(state):
 
 def _own(kind, s):
     import paper_2404_16109_amd as zk
+    # what a serving program makes once and keeps: the cache's descriptor, and a workspace
     if kind in ("append", "attend"):
-        cache = zk.KvCache(s["k_codes"], s["v_codes"], s["k_exp"], s["v_exp"])
+        if "cache" not in s:
+            s["cache"] = zk.KvCache(s["k_codes"], s["v_codes"], s["k_exp"], s["v_exp"])
         if kind == "append":
-            rc = zk.kvcache_append(cache, s["k_new"], s["v_new"], s["cu"], s["lens"], s["table"], s["max_new"])
+            rc = zk.kvcache_append(s["cache"], s["k_new"], s["v_new"], s["cu"], s["lens"], s["table"], s["max_new"])
             assert rc == zk.ZK_OK, rc
             return [s["k_codes"], s["v_codes"], s["k_exp"], s["v_exp"]]
-        rc, out, lse = zk.kvcache_attention(cache, s["q"], s["cu"], s["lens"], s["table"], s["max_new"], s["max_len"],
-                                            s["scale"], window=s["case"]["window"])
+        if "ws" not in s:
+            need = zk.kvcache_attention_workspace_bytes(s["lens"].numel(), s["total"], s["max_new"], s["q"].shape[1],
+                                                        s["k_exp"].shape[1], s["q"].shape[2], s["max_len"])
+            s["ws"] = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        rc, out, lse = zk.kvcache_attention(s["cache"], s["q"], s["cu"], s["lens"], s["table"], s["max_new"], s["max_len"],
+                                            s["scale"], window=s["case"]["window"], out=s["out"], lse=s["lse"], ws=s["ws"])
         assert rc == zk.ZK_OK, rc
         return [out, lse]
     if kind == "product":
-        rc, y = zk.w4_matvec(s["x"], s["codes"], s["scales"], s["group"], s["unit"])
+        if "ws" not in s:
+            need = zk.w4_matvec_workspace_bytes(s["x"].dtype, *s["x"].shape)
+            s["ws"] = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        rc, y = zk.w4_matvec(s["x"], s["codes"], s["scales"], s["group"], s["unit"], out=s["out"], ws=s["ws"])
         assert rc == zk.ZK_OK, rc
         return y
-    rc, got = zk.logprobs(s["logits"], s["targets"], s["top"])
+    if "ws" not in s:
+        s["ws"] = torch.empty(max(zk.logprobs_workspace_bytes(*s["logits"].shape, s["top"]), 1), dtype=torch.uint8, device="cuda")
+    rc, got = zk.logprobs(s["logits"], s["targets"], s["top"], ws=s["ws"])
     assert rc == zk.ZK_OK, rc
     return got
 
