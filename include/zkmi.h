@@ -511,6 +511,153 @@ int zkattn_link_verify(const uint8_t seed[32], const uint8_t* proof, size_t len,
                        const fr_t* bases, const zkattn_link_witness* witness, zkattn_link_claims* claims, void* ws,
                        size_t ws_bytes, void* stream);
 
+/* ---- quantised inference -------------------------------------------------------
+ *
+ * The proofs above are about the integers of a quantised model: 8-bit codes for a
+ * range check, 16-bit X and W and their product Y for a matmul proof.  The entry
+ * points of this section are the steps of an inference that makes and uses such
+ * integers: a paged cache of 8-bit keys and values and the attention that reads
+ * it, products with 4-bit weights, and the log probabilities an answer is
+ * reported with.  They take and give device memory, only enqueue on `stream`,
+ * allocate nothing and wait for nothing; a call may be captured into a graph.
+ * Floating tensors are of one of these types; the innermost dimension is
+ * contiguous, the other strides are given in elements.  Every pointer is aligned
+ * to its element type, and what a comment says beyond that. */
+enum { ZK_F32 = 0, ZK_F16 = 1, ZK_BF16 = 2, ZK_I16 = 3 };
+
+/* A paged cache of keys and values.  A page holds page_tokens tokens (16, 32, 64,
+ * 128 or 256) of all kv_heads heads; head_dim is a multiple of 16, at most 256.
+ *   k: [pages][kv_heads][page_tokens][head_dim], v: [pages][kv_heads][head_dim][page_tokens]
+ * are signed codes (16-byte aligned); k_exp, v_exp: [pages][kv_heads] exponents, one
+ * for each page and head: a code c stands for the number c * 2^exp.  Scales are
+ * powers of two, -40 <= exp <= 40, so that what a code stands for is a fixed-point
+ * integer and a change of scale is a shift: the numbers the attention computes with
+ * are exactly the integers a lookup proof range-checks (Section 3.3).  The exponent
+ * ZK_EXP_NAN says that the page was given a value that is not finite. */
+#define ZK_EXP_MIN (-40)
+#define ZK_EXP_MAX 40
+#define ZK_EXP_NAN (-128)
+
+typedef struct {
+    int8_t* k;
+    int8_t* v;
+    int8_t* k_exp;
+    int8_t* v_exp;
+    uint32_t pages, kv_heads, page_tokens, head_dim;
+} kvcache_i8;
+
+/* The sequences of a call.  Sequence b has lens[b] tokens with those of this call,
+ * which are the rows cu[b] .. cu[b+1]-1 of the call's tensors (cu[0] = 0, not
+ * decreasing, cu[seqs] <= rows) and the sequence's last: row i of them is the token
+ * at position lens[b] - (cu[b+1]-cu[b]) + i.  A row whose position is negative is no
+ * token: nothing is stored for it, and as a query it sees no key.  Token t lies in
+ * page table[b * table_stride + t / page_tokens]; entries that no token needs are
+ * not read.  cu, lens and table are device arrays.  max_new: the most rows any
+ * sequence has (host; at least 1).  max_len: about the longest lens[b] (host; it
+ * decides how the work is spread, not what is computed).
+ *
+ * What the device finds wrong (it cannot return a code) it ORs into *fault, a
+ * device word that the caller clears and reads when it likes (may be NULL): a
+ * sequence with ZK_FAULT_LENGTH (cu as above does not hold, more than max_new rows,
+ * lens[b] negative or more than table_pages pages hold) is skipped, its outputs are
+ * NaN; a page outside the cache (ZK_FAULT_PAGE) is not touched, and the rows that
+ * would see a key in it are NaN. */
+enum { ZK_FAULT_LENGTH = 1, ZK_FAULT_PAGE = 2 };
+
+typedef struct {
+    const int32_t* cu;
+    const int32_t* lens;
+    const int32_t* table;
+    size_t table_stride;
+    uint32_t table_pages; /* entries of a sequence's row; table_stride is at least that where there are several */
+    uint32_t seqs, rows, max_new, max_len;
+    uint32_t* fault;
+} kv_seqs;
+
+/* Stores the call's keys and values (rows x kv_heads x head_dim each; strides of rows
+ * and heads in elements) as codes.  For each page and head that new tokens fall
+ * into, with a the largest magnitude among the page's new values:
+ *   need = the smallest e in [ZK_EXP_MIN, ZK_EXP_MAX] with a <= 127 * 2^e (ZK_EXP_MAX if none),
+ *   exp' = max(exp, need), or need where the page begins with this call (its slot 0 is
+ *          among the new tokens);
+ *   codes it holds become rint(c * 2^(exp - exp')), or 0 where it begins;
+ *   new codes are rint(x * 2^-exp') clipped to [-127, 127];  rint: ties to even.
+ * With a value that is not finite exp' is ZK_EXP_NAN from then on, and new codes are 0.
+ * Storing the same tokens again changes nothing.  A page that is written belongs to
+ * one sequence (shared pages may be read by many).  Keys and values have the same
+ * type.  rows == 0 is a call that does nothing. */
+int kvcache_append(const kvcache_i8* cache, const void* k, size_t k_row_stride, size_t k_head_stride, const void* v,
+                   size_t v_row_stride, size_t v_head_stride, int dtype, const kv_seqs* seqs, void* stream);
+
+/* out = softmax(scale * q k^T) v over the keys that each query sees: with p its
+ * position, those at positions j <= p and, if window > 0, j > p - window.  q, out:
+ * rows x q_heads x head_dim, of one type (ZK_F16, ZK_BF16); query head h reads the cache's
+ * head h / (q_heads / kv_heads).  lse (may be NULL): rows x q_heads floats, the
+ * natural logarithm of the sum of exp(scale * q k).  A row that sees no key is 0
+ * with lse = -inf; one that sees a key of a page with ZK_EXP_NAN, or whose query is not finite, is
+ * NaN.  Scores, sums and the product with v are accumulated in 32 bits; the
+ * probabilities, times their pages' scales, enter that product rounded to 11 bits, those below
+ * 2^-29 of a row's largest to fewer, and below 2^-39 of it as 0.
+ * ws: device, kvcache_attention_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, max_len). */
+size_t kvcache_attention_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
+                                         uint32_t head_dim, uint32_t max_len);
+int kvcache_attention(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
+                      uint32_t q_heads, const kv_seqs* seqs, float scale, uint32_t window, void* out, size_t out_row_stride,
+                      size_t out_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* The codes of one sequence's first `tokens` tokens in order, as the 32-bit integers that
+ * tlookup_prove_small takes: k_codes, v_codes (device): tokens x kv_heads x head_dim each.
+ * pages: device, the sequence's row of the table.  Exponents lie in the cache by page.
+ * A page outside the cache gives zeros and sets *fault (device, may be NULL). */
+int kvcache_read(const kvcache_i8* cache, const int32_t* pages, size_t tokens, int32_t* k_codes, int32_t* v_codes,
+                 uint32_t* fault, void* stream);
+
+/* Weights of n outputs by k inputs in 4 bits: codes [n][k/2] bytes (16-byte aligned), the weight of
+ * input 2i in the lower half of byte i, as c + 8 with -8 <= c <= 7; scales
+ * [n][ceil(k/group)], integers 0..4095, one for each `group` (32, 64 or 128)
+ * consecutive inputs of an output (the last may be shorter).  A weight is
+ * unit * c * scale: the integer c * scale has 16 bits, and `unit` is the fixed-point
+ * step of the whole matrix.  k is a multiple of 32.
+ *
+ * y[m][i] = unit * sum_j w[i][j] x[m][j] for `rows` vectors x (rows x k, y: rows x n, the
+ * rows' strides given; x's rows 16-byte aligned).  ZK_F32, ZK_F16, ZK_BF16: y has the type of x; sums are
+ * accumulated in 32 bits.  A row of x with a value that is not finite gives NaN.  ZK_I16: x are 16-bit integers, y are
+ * int64_t and the sums themselves, exactly (unit is ignored): the Y that
+ * matmul_sumcheck_prove_i16 proves for X = x and W = w4_expand_i16.   |x| < 2^120, else NaN.  rows may be 0.
+ * ws: device, w4_matvec_workspace_bytes(dtype, rows, k) (0 for few rows: ws may be NULL then). */
+size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k);
+int w4_matvec(void* y, size_t y_row_stride, const void* x, size_t x_row_stride, int dtype, size_t rows, const uint8_t* codes,
+              const uint16_t* scales, size_t n, size_t k, uint32_t group, float unit, void* ws, size_t ws_bytes, void* stream);
+
+/* W[j][i] = c * scale of output i's weight for input j: the k x n matrix of 16-bit
+ * integers, row-major, that matmul_sumcheck_prove_i16 takes as W. */
+int w4_expand_i16(int16_t* W, const uint8_t* codes, const uint16_t* scales, size_t n, size_t k, uint32_t group, void* stream);
+
+/* What an answer is reported with, from rows x vocab logits (vocab <= 2^19): per
+ * row, with p = softmax(logits),
+ *   lse      log sum exp(logits)
+ *   target   log p of the given token: logits[targets[r]] - lse; NaN if targets[r] is no token
+ *   rank     how many tokens come before it, by larger logit, among equals by lower index; -1 if no token
+ *   entropy  -sum p log p
+ *   top_ids, top   the `top` (0 <= top <= LOGPROBS_MAX_TOP, at most vocab) first tokens in
+ *            that order and their log p; rows x top each.
+ * A logit of -inf has probability 0.  A row of nothing else has lse = -inf, all log
+ * probabilities -inf and entropy 0.  A row with a NaN has NaN for all of them (NaN comes
+ * first in the order; its rank is not specified).  targets (then target and rank), lse and entropy may be NULL.
+ * All results are 32 bits.  ws: device, logprobs_workspace_bytes(rows, vocab, top). */
+#define LOGPROBS_MAX_TOP 32
+typedef struct {
+    float* target;
+    int32_t* rank;
+    float* lse;
+    float* entropy;
+    int32_t* top_ids;
+    float* top;
+} logprobs_out; /* device */
+size_t logprobs_workspace_bytes(size_t rows, size_t vocab, uint32_t top);
+int logprobs(const void* logits, size_t row_stride, int dtype, size_t rows, size_t vocab, const int32_t* targets, uint32_t top,
+             const logprobs_out* out, void* ws, size_t ws_bytes, void* stream);
+
 /* The calling host thread's pinned state (see Ownership), for callers that want no
  * allocation inside their first proof: zkmi_thread_init allocates it now, with
  * the staging buffer sized for TLOOKUP_BATCH_MAX tables of max_table_rows rows each (a

@@ -61,6 +61,23 @@ class zkattn_link_claims(ctypes.Structure):
                 ("K", ctypes.c_int)]
 
 
+class kvcache_i8(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("pages", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32), ("page_tokens", ctypes.c_uint32),
+                ("head_dim", ctypes.c_uint32)]
+
+
+class kv_seqs(ctypes.Structure):
+    _fields_ = [("cu", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_size_t), ("table_pages", ctypes.c_uint32), ("seqs", ctypes.c_uint32), ("rows", ctypes.c_uint32),
+                ("max_new", ctypes.c_uint32), ("max_len", ctypes.c_uint32), ("fault", ctypes.c_void_p)]
+
+
+class logprobs_out(ctypes.Structure):
+    _fields_ = [("target", ctypes.c_void_p), ("rank", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("entropy", ctypes.c_void_p), ("top_ids", ctypes.c_void_p), ("top", ctypes.c_void_p)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -145,6 +162,16 @@ def _load():
         "zkattn_link_verify_workspace_bytes": (sz, [sz, sz]),
         "zkattn_link_verify": (i32, [vp, vp, sz, sz, sz, sz, P(fr_t), P(zkattn_link_witness), P(zkattn_link_claims), vp,
                                      sz, vp]),
+        "kvcache_append": (i32, [P(kvcache_i8), vp, sz, sz, vp, sz, sz, i32, P(kv_seqs), vp]),
+        "kvcache_attention_workspace_bytes": (sz, [ctypes.c_uint32] * 7),
+        "kvcache_attention": (i32, [P(kvcache_i8), vp, sz, sz, i32, ctypes.c_uint32, P(kv_seqs), ctypes.c_float,
+                                    ctypes.c_uint32, vp, sz, sz, vp, vp, sz, vp]),
+        "kvcache_read": (i32, [P(kvcache_i8), vp, sz, vp, vp, vp, vp]),
+        "w4_matvec_workspace_bytes": (sz, [i32, sz, sz]),
+        "w4_matvec": (i32, [vp, sz, vp, sz, i32, sz, vp, vp, sz, sz, ctypes.c_uint32, ctypes.c_float, vp, sz, vp]),
+        "w4_expand_i16": (i32, [vp, vp, vp, sz, sz, ctypes.c_uint32, vp]),
+        "logprobs_workspace_bytes": (sz, [sz, sz, ctypes.c_uint32]),
+        "logprobs": (i32, [vp, sz, i32, sz, sz, vp, ctypes.c_uint32, P(logprobs_out), vp, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -168,7 +195,8 @@ EXPORTS = ["zkmi_version", "zkmi_thread_init", "zkmi_thread_release", "zkmi_self
            "matmul_verify_workspace_bytes", "matmul_sumcheck_verify", "zkattn_link_proof_bytes",
            "zkattn_link_workspace_bytes", "zkattn_link_prove", "zkattn_link_prove_small",
            "zkattn_link_verify_workspace_bytes",
-           "zkattn_link_verify"]
+           "zkattn_link_verify", "kvcache_append", "kvcache_attention_workspace_bytes", "kvcache_attention", "kvcache_read",
+           "w4_matvec_workspace_bytes", "w4_matvec", "w4_expand_i16", "logprobs_workspace_bytes", "logprobs"]
 
 
 def raw():
@@ -790,3 +818,149 @@ def zkattn_link_verify(seed, proof, rows, cols, bases, Zp=None, X=None, Y=None, 
                "X_v": [_fr_int(claims.X_v[k]) for k in range(K)], "Yk_v": [_fr_int(claims.Yk_v[k]) for k in range(K)],
                "u": [_fr_int(claims.u[t]) for t in range(n)], "v": [_fr_int(claims.v[t]) for t in range(n)]}
     return rc, out
+
+
+# ---- quantised inference ------------------------------------------------------------------------
+
+ZK_F32, ZK_F16, ZK_BF16, ZK_I16 = 0, 1, 2, 3
+ZK_FAULT_LENGTH, ZK_FAULT_PAGE = 1, 2
+ZK_EXP_MIN, ZK_EXP_MAX, ZK_EXP_NAN = -40, 40, -128
+LOGPROBS_MAX_TOP = 32
+_DTYPES = {torch.float32: ZK_F32, torch.float16: ZK_F16, torch.bfloat16: ZK_BF16, torch.int16: ZK_I16}
+
+
+def _optional(t):
+    return None if t is None else t.data_ptr()
+
+
+class KvCache:
+    """A paged cache of 8-bit keys and values over int8 tensors of the caller's: k (pages, kv_heads, page_tokens, head_dim),
+    v (pages, kv_heads, head_dim, page_tokens), k_exp and v_exp (pages, kv_heads)."""
+
+    def __init__(self, k, v, k_exp, v_exp):
+        pages, heads, tokens, dim = k.shape
+        assert v.shape == (pages, heads, dim, tokens) and k_exp.shape == v_exp.shape == (pages, heads)
+        for t in (k, v, k_exp, v_exp):
+            assert t.dtype == torch.int8 and t.is_cuda and t.is_contiguous()
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.c = kvcache_i8(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, heads, tokens, dim)
+
+    @classmethod
+    def empty(cls, pages, kv_heads, page_tokens, head_dim, device="cuda"):
+        def new(*shape):
+            return torch.zeros(shape, dtype=torch.int8, device=device)
+        return cls(new(pages, kv_heads, page_tokens, head_dim), new(pages, kv_heads, head_dim, page_tokens),
+                   new(pages, kv_heads), new(pages, kv_heads))
+
+
+def _kv_seqs(cu, lens, table, rows, max_new, max_len, fault):
+    assert cu.dtype == lens.dtype == table.dtype == torch.int32 and cu.is_cuda and lens.is_cuda and table.is_cuda
+    seqs = lens.shape[0]
+    assert cu.shape[0] == seqs + 1 and cu.is_contiguous() and lens.is_contiguous()
+    assert table.shape[0] == seqs and (table.stride(1) == 1 or table.shape[1] == 1)
+    return kv_seqs(cu.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1], seqs, rows, max_new, max_len, _optional(fault))
+
+
+def kvcache_append(cache, k, v, cu, lens, table, max_new, fault=None):
+    """k, v: (rows, kv_heads, head_dim), any strides with the innermost 1.  fault: None or an int32 tensor of one element."""
+    assert k.dtype == v.dtype and k.shape == v.shape == (k.shape[0], cache.c.kv_heads, cache.c.head_dim) and k.is_cuda and v.is_cuda
+    assert k.stride(2) == 1 and v.stride(2) == 1
+    s = _kv_seqs(cu, lens, table, k.shape[0], max_new, 0, fault)
+    return _lib.kvcache_append(ctypes.byref(cache.c), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                               v.stride(1), _DTYPES[k.dtype], ctypes.byref(s), _stream())
+
+
+def kvcache_attention_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, max_len):
+    return _lib.kvcache_attention_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, max_len)
+
+
+def kvcache_attention(cache, q, cu, lens, table, max_new, max_len, scale, window=0, out=None, lse=None, ws=None, fault=None):
+    """q: (rows, q_heads, head_dim).  Returns (rc, out, lse); out and lse are made where they are not given."""
+    rows, heads, dim = q.shape
+    assert dim == cache.c.head_dim and q.is_cuda and q.stride(2) == 1
+    if out is None:
+        out = torch.empty(rows, heads, dim, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.stride(2) == 1
+    assert lse.shape == (rows, heads) and lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous()
+    s = _kv_seqs(cu, lens, table, rows, max_new, max_len, fault)
+    if ws is None:
+        ws = _ws(_lib.kvcache_attention_workspace_bytes(s.seqs, rows, max_new, heads, cache.c.kv_heads, dim, max_len))
+    rc = _lib.kvcache_attention(ctypes.byref(cache.c), q.data_ptr(), q.stride(0), q.stride(1), _DTYPES[q.dtype], heads,
+                                ctypes.byref(s), scale, window, out.data_ptr(), out.stride(0), out.stride(1),
+                                lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    return rc, out, lse
+
+
+def kvcache_read(cache, pages, tokens, fault=None):
+    """Returns (rc, k_codes, v_codes): int32 (tokens, kv_heads, head_dim) of the sequence whose pages are given."""
+    assert pages.dtype == torch.int32 and pages.is_cuda and pages.is_contiguous() and pages.numel() * cache.c.page_tokens >= tokens
+    k, v = (torch.empty(tokens, cache.c.kv_heads, cache.c.head_dim, dtype=torch.int32, device=pages.device) for _ in range(2))
+    rc = _lib.kvcache_read(ctypes.byref(cache.c), pages.data_ptr(), tokens, k.data_ptr(), v.data_ptr(), _optional(fault), _stream())
+    return rc, k, v
+
+
+def w4_matvec_workspace_bytes(dtype, rows, k):
+    return _lib.w4_matvec_workspace_bytes(_DTYPES[dtype], rows, k)
+
+
+def w4_matvec(x, codes, scales, group, unit=1.0, out=None, ws=None):
+    """x: (rows, k); codes: uint8 (n, k/2); scales: int16 (n, ceil(k/group)), all 0..4095.  Returns (rc, y): (rows, n) of x's
+    type, int64 for int16."""
+    rows, k = x.shape
+    n = codes.shape[0]
+    assert codes.dtype == torch.uint8 and codes.shape[1] * 2 == k and codes.is_cuda and codes.is_contiguous()
+    assert scales.dtype == torch.int16 and scales.shape == (n, -(-k // group)) and scales.is_cuda and scales.is_contiguous()
+    assert x.is_cuda and x.stride(1) == 1
+    kind = torch.int64 if x.dtype == torch.int16 else x.dtype
+    if out is None:
+        out = torch.empty(rows, n, dtype=kind, device=x.device)
+    assert out.shape == (rows, n) and out.dtype == kind and out.is_cuda and out.stride(1) == 1
+    dtype = _DTYPES[x.dtype]
+    need = _lib.w4_matvec_workspace_bytes(dtype, rows, k)
+    if ws is None and need:
+        ws = _ws(need)
+    rc = _lib.w4_matvec(out.data_ptr(), out.stride(0), x.data_ptr(), x.stride(0), dtype, rows, codes.data_ptr(),
+                        scales.data_ptr(), n, k, group, unit, _optional(ws), ws.numel() if ws is not None else 0, _stream())
+    return rc, out
+
+
+def w4_expand_i16(codes, scales, group):
+    """Returns (rc, W): the int16 (k, n) matrix of c * scale."""
+    n, k = codes.shape[0], codes.shape[1] * 2
+    assert codes.dtype == torch.uint8 and codes.is_cuda and codes.is_contiguous()
+    assert scales.dtype == torch.int16 and scales.shape == (n, -(-k // group)) and scales.is_cuda and scales.is_contiguous()
+    W = torch.empty(k, n, dtype=torch.int16, device=codes.device)
+    rc = _lib.w4_expand_i16(W.data_ptr(), codes.data_ptr(), scales.data_ptr(), n, k, group, _stream())
+    return rc, W
+
+
+def logprobs_workspace_bytes(rows, vocab, top):
+    return _lib.logprobs_workspace_bytes(rows, vocab, top)
+
+
+def logprobs(logits, targets=None, top=0, ws=None):
+    """logits: (rows, vocab); targets: None or int32 (rows).  Returns (rc, dict of target, rank, lse, entropy, top_ids, top);
+    target and rank are None without targets."""
+    rows, vocab = logits.shape
+    assert logits.is_cuda and (logits.stride(1) == 1 or vocab == 1)
+    dev = logits.device
+    given = targets is not None
+    if given:
+        assert targets.dtype == torch.int32 and targets.shape == (rows,) and targets.is_cuda and targets.is_contiguous()
+    # one allocation: six arrays of 32-bit values
+    words = torch.empty(rows * (4 + 2 * top), dtype=torch.float32, device=dev)
+    ints = words.view(torch.int32)
+    r = {"target": words[:rows] if given else None, "rank": ints[rows:2 * rows] if given else None,
+         "lse": words[2 * rows:3 * rows], "entropy": words[3 * rows:4 * rows],
+         "top_ids": ints[4 * rows:(4 + top) * rows].view(rows, top), "top": words[(4 + top) * rows:].view(rows, top)}
+    base, row = words.data_ptr(), 4 * rows
+    o = logprobs_out(base if given else None, base + row if given else None, base + 2 * row, base + 3 * row, base + 4 * row,
+                     base + (4 + top) * row)
+    need = _lib.logprobs_workspace_bytes(rows, vocab, top)
+    if ws is None and need:
+        ws = _ws(need)
+    rc = _lib.logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab, _optional(targets), top,
+                       ctypes.byref(o), _optional(ws), ws.numel() if ws is not None else 0, _stream())
+    return rc, r

@@ -6,7 +6,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libzkmi.so")
-SOURCES = ["field_ops.hip", "poly.hip", "batch_inverse.hip", "tlookup.hip", "product.hip", "zkattn_link.hip"]
+SOURCES = ["field_ops.hip", "poly.hip", "batch_inverse.hip", "tlookup.hip", "product.hip", "zkattn_link.hip", "logprobs.hip",
+           "w4.hip", "kvcache.hip", "attention.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Wall", "-Wshadow", "-Werror=shadow",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

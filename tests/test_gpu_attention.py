@@ -1,0 +1,236 @@
+"""Attention over the 8-bit cache against its definition in 64 bits.
+
+Tolerances, elementwise.  A score is a sum of head_dim exact products in 32 bits and three more roundings: (head_dim + 16)
+* 2^-24 of scale * sum |q k| at most, which moves weights by twice that; the weights enter the product rounded to 11
+bits, half a step of 2^-11 each; len products are added in 32 bits.  Relative to sum p |v| that is
+  2^-11 + 2 * (head_dim + 16) * 2^-24 * score + (len + 64) * 2^-24,
+and half a step of the output's type on top.  A 16-bit float has a smallest step: what a weight loses is at least 2^-25 of
+the 2^14 that the row's largest is scaled to, with the scales of the pages of values, and 127 of that at most for each of
+len keys.  lse: the scores' error, (len + 64) * 2^-24, and two roundings of its size."""
+import math
+
+import pytest
+import torch
+
+from tests import serve_ref
+from tests.test_gpu_kvcache import arrays, device, paged, random_cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def zk():
+    import paper_2404_16109_amd as zk
+    assert torch.cuda.is_available()
+    return zk
+
+
+def check(zk, cache, q, cu, lens, table, scale, window=0, max_new=None, max_len=None, **kw):
+    new = [b - a for a, b in zip(cu, cu[1:])]
+    fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rc, out, lse = zk.kvcache_attention(cache, q, *device(cu, lens, table), max_new or max(max(new), 1), max(lens) if max_len is None else max_len,
+                                        scale, window=window, fault=fault, **kw)
+    assert rc == zk.ZK_OK
+    torch.cuda.synchronize()
+    assert fault.item() == 0
+    want, wlse, size, score, weight = serve_ref.attention(*arrays(cache), q, cu, lens, table, scale, window)
+    d, L = q.shape[2], max(lens)
+    moved = (d + 16) * 2.0 ** -24 * score
+    tol = (2.0 ** -11 + 2 * moved + (L + 64) * 2.0 ** -24)[..., None] * size + torch.finfo(q.dtype).eps / 2 * want.abs() + torch.finfo(q.dtype).tiny
+    tol += (L * 127 * 2.0 ** -39 * weight)[..., None]
+    bad = (out.double() - want).abs() > tol
+    assert torch.equal(out.isnan(), want.isnan())
+    assert not (bad & ~want.isnan()).any(), float((out.double() - want).abs().nan_to_num().max())
+    empty = wlse == -math.inf
+    assert torch.equal(lse == -math.inf, empty) and not out[empty].any()
+    off = (lse.double() - wlse).abs()
+    assert (off <= moved + (L + 64) * 2.0 ** -24 + 4 * 2.0 ** -24 * wlse.abs())[~empty & ~wlse.isnan()].all()
+    assert torch.equal(lse.isnan(), wlse.isnan())
+    return out, lse
+
+
+def make(zk, new, lens, heads, H, d, T, dtype, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    table, pages = paged(lens, T, seed)
+    cache = random_cache(zk, pages, H, T, d, gen)
+    cache.k_exp.copy_(torch.randint(-8, -4, cache.k_exp.shape, generator=gen, device="cuda"))
+    q = torch.randn(sum(new), heads, d, generator=gen, device="cuda").to(dtype)
+    return cache, q, [0] + torch.tensor(new).cumsum(0).tolist(), table, gen
+
+
+CASES = [  # new, lens, heads, kv_heads, head_dim, page, window
+    ([1], [1], 1, 1, 16, 16, 0), ([1], [2], 2, 1, 64, 16, 0), ([1], [15], 5, 1, 128, 16, 0), ([1], [64], 8, 8, 128, 64, 0),
+    ([1], [65], 4, 2, 80, 32, 0), ([1, 1, 1], [63, 128, 129], 6, 3, 96, 64, 0), ([1], [1000], 16, 1, 128, 128, 0),
+    ([1], [3001], 5, 1, 128, 16, 0), ([1, 1], [5000, 7], 4, 4, 64, 256, 0), ([1], [777], 3, 1, 256, 32, 0), ([1], [500], 2, 1, 192, 64, 0),
+    ([1], [400], 17, 1, 64, 16, 0), ([1], [700], 32, 1, 128, 64, 0), ([1], [300], 20, 1, 256, 16, 0), ([1], [333], 18, 1, 160, 32, 0),
+    ([4], [100], 4, 1, 112, 16, 0), ([3, 0, 2], [80, 40, 2], 8, 2, 128, 32, 0), ([1], [900], 4, 1, 128, 16, 100), ([5], [600], 4, 2, 64, 64, 64),
+    ([2, 2], [300, 130], 8, 2, 80, 128, 1), ([1], [200], 2, 2, 48, 16, 1000),
+    ([40], [40], 1, 1, 64, 16, 0), ([129], [129], 2, 1, 128, 64, 0), ([70, 1, 0, 33], [200, 90, 10, 33], 4, 2, 128, 32, 0),
+    ([64], [500], 3, 3, 96, 16, 0), ([33], [257], 2, 1, 256, 128, 0), ([50], [77], 1, 1, 192, 64, 0), ([200], [333], 4, 1, 80, 64, 37),
+    ([65], [65], 1, 1, 16, 16, 3), ([45], [300], 2, 2, 160, 256, 128), ([300], [300], 1, 1, 224, 32, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("new,lens,heads,H,d,T,window", CASES)
+def test_attention(zk, dtype, new, lens, heads, H, d, T, window):
+    cache, q, cu, table, _ = make(zk, new, lens, heads, H, d, T, dtype, sum(lens) + d + heads)
+    check(zk, cache, q, cu, lens, table, d ** -0.5, window)
+
+
+@pytest.mark.parametrize("new,lens,heads,H,d", [([1], [2500], 4, 2, 128), ([20], [300], 4, 2, 64)])
+def test_spread_as_the_caller_says(zk, new, lens, heads, H, d):
+    """max_new and max_len too large, max_len too small: the same rows, whatever the split."""
+    cache, q, cu, table, _ = make(zk, new, lens, heads, H, d, 16, torch.float16, 3)
+    for max_new, max_len in ((new[0], 1), (new[0], 10 ** 6), (new[0] + 7, lens[0]), (1000, 0)):
+        check(zk, cache, q, cu, lens, table, d ** -0.5, 0, max_new, max_len)
+
+
+@pytest.mark.parametrize("new,lens", [([3], [2]), ([40], [7]), ([2, 50, 1], [0, 3, 0]), ([1], [0]), ([33], [0])])
+def test_rows_that_see_nothing(zk, new, lens):
+    """More rows than tokens: the first see no key, their output is zero and lse is -inf."""
+    cache, q, cu, table, _ = make(zk, new, lens, 4, 2, 64, 16, torch.bfloat16, 3)
+    out, lse = check(zk, cache, q, cu, lens, table, 0.125)
+    assert (lse == -math.inf).any()
+
+
+@pytest.mark.parametrize("new,lens", [([1], [300]), ([40], [300])])
+def test_scales_far_apart(zk, new, lens):
+    """Pages whose exponents lie far from each other: the weight of a page with small values is not lost next to one with
+    large values, whichever comes first, and what is cut off is small beside the row's own size."""
+    T, d = 16, 64
+    cache, q, cu, table, gen = make(zk, new, lens, 2, 1, d, T, torch.float16, 5)
+    for low, high in ((-40, 40), (-40, -40), (40, 40), (-3, 12)):
+        cache.v_exp.copy_(torch.where(torch.rand(cache.v_exp.shape, generator=gen, device="cuda") < 0.5, low, high))
+        cache.v.clamp_(-60, 60)
+        rc, out, lse = zk.kvcache_attention(cache, q, *device(cu, lens, table), max(new), lens[0], d ** -0.5)
+        want, wlse, size, score, weight = serve_ref.attention(*arrays(cache), q, cu, lens, table, d ** -0.5)
+        moved = (d + 16) * 2.0 ** -24 * score
+        assert ((lse.double() - wlse).abs() <= moved + (lens[0] + 64) * 2.0 ** -24 + 4 * 2.0 ** -24 * wlse.abs()).all()
+        large = size.amax(-1, keepdim=True)
+        tol = (2.0 ** -11 + 2 * moved + (lens[0] + 64) * 2.0 ** -24)[..., None] * size + 2.0 ** -11 * want.abs() + 2.0 ** -24 * large
+        inside = want.abs() < 60000
+        assert ((out.double() - want).abs() <= tol + 2.0 ** -24)[inside].all()
+
+
+@pytest.mark.parametrize("new", [[1], [40]])
+def test_large_and_small_queries_and_scales(zk, new):
+    lens, d = [200], 128
+    for size, kexp, scale in ((1e30, -40, 1e-25), (1e-30, 20, 1e20), (300.0, -6, 0.3), (1.0, -6, -0.1), (1.0, -6, 0.0)):
+        cache, q, cu, table, gen = make(zk, new, lens, 4, 2, d, 32, torch.bfloat16, 5)
+        cache.k_exp.fill_(kexp)
+        check(zk, cache, (q.float() * size).to(torch.bfloat16), cu, lens, table, scale)
+
+
+@pytest.mark.parametrize("new,lens", [([1], [300]), ([3], [300]), ([60], [300])])
+def test_peaked_rows(zk, new, lens):
+    """Scores of hundreds: the first keys far above the rest, then the last ones."""
+    cache, q, cu, table, gen = make(zk, new, lens, 4, 2, 64, 16, torch.float16, 6)
+    cache.k_exp.fill_(0)
+    check(zk, cache, q, cu, lens, table, 0.5)
+    for first in (True, False):
+        rows = table[0][0] if first else table[0][-1]
+        cache.k_exp.fill_(-6)
+        cache.k_exp[rows] = 2
+        check(zk, cache, q, cu, lens, table, 0.5)
+
+
+@pytest.mark.parametrize("new,lens", [([1, 1], [300, 40]), ([40, 2], [300, 40]), ([2, 2], [2000, 70])])
+def test_not_finite(zk, new, lens):
+    """Poisoned pages reach the rows that see them, a query with an infinity or NaN its own row, and nothing else; codes and
+    exponents behind a sequence's end are never taken in."""
+    T = 16
+    cache, q, cu, table, gen = make(zk, new, lens, 4, 2, 64, T, torch.bfloat16, 7)
+    cache.k_exp[table[0][3], 1] = zk.ZK_EXP_NAN
+    check(zk, cache, q, cu, lens, table, 0.125)
+    check(zk, cache, q, cu, lens, table, 0.125, window=200)
+    check(zk, cache, q, cu, lens, table, 0.125, window=5)
+    cache.k_exp[table[0][3], 1] = -5
+    cache.v_exp[table[1][1], 0] = zk.ZK_EXP_NAN
+    rc, out, lse = zk.kvcache_attention(cache, q, *device(cu, lens, table), max(new), max(lens), 0.125)
+    assert out[cu[1]:, :2].isnan().all() and not out[:cu[1]].isnan().any() and not out[cu[1]:, 2:].isnan().any()
+    cache.v_exp[table[1][1], 0] = -5
+    rc, clean, _ = zk.kvcache_attention(cache, q, *device(cu, lens, table), max(new), max(lens), 0.125)
+    q2 = q.clone()
+    q2[0, 1, 5], q2[-1, 3, 63] = math.inf, math.nan
+    rc, out, lse = zk.kvcache_attention(cache, q2, *device(cu, lens, table), max(new), max(lens), 0.125)
+    hit = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    hit[0, 1] = hit[-1, 3] = True
+    assert out[hit].isnan().all() and lse[hit].isnan().all() and torch.equal(out[~hit], clean[~hit])
+
+
+def test_strides(zk):
+    new, lens, d = [3, 1], [50, 90], 64
+    cache, q, cu, table, gen = make(zk, new, lens, 4, 2, d, 16, torch.bfloat16, 8)
+    rc, want, wlse = zk.kvcache_attention(cache, q, *device(cu, lens, table), 3, 90, 0.125)
+    wide = torch.zeros(4, 9, d + 3, dtype=torch.bfloat16, device="cuda")
+    wide[:, 1:9:2, 2:d + 2] = q
+    out = torch.full((4, 5, d + 7), 3.0, dtype=torch.bfloat16, device="cuda")
+    rc, got, lse = zk.kvcache_attention(cache, wide[:, 1:9:2, 2:d + 2], *device(cu, lens, table), 3, 90, 0.125, out=out[:, 1:, 5:d + 5])
+    assert rc == zk.ZK_OK and torch.equal(got, want) and torch.equal(lse, wlse)
+    assert out[:, 0].eq(3).all() and out[:, :, :5].eq(3).all() and out[:, :, d + 5:].eq(3).all()
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_what_the_device_refuses(zk, many):
+    """A sequence whose lengths do not hold, and rows that would see a page outside the cache, are NaN; others are right."""
+    new = [40, 2] if many else [2, 2]
+    lens = [300, 70]
+    cache, q, cu, table, gen = make(zk, new, lens, 4, 2, 64, 16, torch.bfloat16, 9)
+    rc, want, _ = zk.kvcache_attention(cache, q, *device(cu, lens, table), max(new), 300, 0.125)
+    for bad, what in (({"page": 10 ** 6}, zk.ZK_FAULT_PAGE), ({"page": -1}, zk.ZK_FAULT_PAGE), ({"len": 10 ** 6}, zk.ZK_FAULT_LENGTH),
+                      ({"len": -3}, zk.ZK_FAULT_LENGTH)):
+        t2, l2 = [list(r) for r in table], list(lens)
+        if "page" in bad:
+            t2[0][1] = bad["page"]
+        else:
+            l2[0] = bad["len"]
+        fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+        rc, out, lse = zk.kvcache_attention(cache, q, *device(cu, l2, t2), max(new), 300, 0.125, fault=fault)
+        assert rc == zk.ZK_OK and fault.item() == what
+        assert out[:cu[1]].isnan().all() and lse[:cu[1]].isnan().all() and torch.equal(out[cu[1]:], want[cu[1]:])
+    fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rc, out, lse = zk.kvcache_attention(cache, q, *device([0, 10 ** 6, 5], lens, table), max(new), 300, 0.125, fault=fault)
+    assert rc == zk.ZK_OK and fault.item() == zk.ZK_FAULT_LENGTH and out.isnan().all()
+
+
+@pytest.mark.parametrize("new", [[1, 1], [40, 3]])
+def test_again_on_streams_and_in_a_graph(zk, new):
+    lens = [3000, 100]
+    cache, q, cu, table, gen = make(zk, new, lens, 4, 2, 128, 64, torch.bfloat16, 10)
+    args = device(cu, lens, table)
+    rc, want, wlse = zk.kvcache_attention(cache, q, *args, max(new), 3000, 0.1)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        rc, other, _ = zk.kvcache_attention(cache, q, *args, max(new), 3000, 0.1)
+        stream.synchronize()
+        assert torch.equal(other, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            rc, out, lse = zk.kvcache_attention(cache, q, *args, max(new), 3000, 0.1)
+    for _ in range(3):
+        out.zero_()
+        lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        rc, again, alse = zk.kvcache_attention(cache, q, *args, max(new), 3000, 0.1)
+        assert torch.equal(out, want) and torch.equal(lse, wlse) and torch.equal(again, want) and torch.equal(alse, wlse)
+
+
+def test_a_cache_beyond_32_bits(zk):
+    """Pages whose codes lie more than 2^32 bytes into the cache."""
+    H, d, T = 1, 256, 256
+    pages = (1 << 32) // (T * d) + 40
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    cache = zk.KvCache.empty(pages, H, T, d)
+    L = 600
+    table = [[pages - 1, 5, pages - 3]]
+    for new in (1, 40):
+        k, v = (torch.randn(L, H, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+        assert zk.kvcache_append(cache, k, v, *device([0, L], [L], table), L) == zk.ZK_OK
+        q = torch.randn(new, 2, d, generator=gen, device="cuda").to(torch.bfloat16)
+        check(zk, cache, q, [0, new], [L], table, 0.06)
+    small = zk.KvCache.empty(3, H, T, d)
+    assert zk.kvcache_append(small, k, v, *device([0, L], [L], [[0, 1, 2]]), L) == zk.ZK_OK
+    assert torch.equal(small.k[[0, 1, 2]], cache.k[table[0]]) and torch.equal(small.v[[0, 1, 2]], cache.v[table[0]])
