@@ -16,4 +16,6 @@ def __getattr__(name):
     if name in ("build", "synth", "binding"):
         return importlib.import_module("." + name, __name__)
     binding = importlib.import_module(".binding", __name__)
-    return getattr(binding, name)
+    value = getattr(binding, name)
+    globals()[name] = value  # found without this detour from now on: it costs as much as a launch
+    return value

@@ -27,6 +27,8 @@ namespace {
 static const float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 static const float kHead = 14.0f;      // P reaches up to 2^14
 static const uint32_t kTile = 64;      // tokens
+static const uint32_t kWorkgroups = 1024;
+static const uint32_t kShort = 16;     // tiles
 
 struct Args {
     kvcache_i8 cache;
@@ -37,8 +39,9 @@ struct Args {
     size_t orow, ohead;
     float* lse;
     float scale;
-    uint32_t window, group, page_log, splits;  // group: query heads of a head of the cache
+    uint32_t window, group, page_log, splits, each;  // group: query heads of a head of the cache
     int dtype;
+    bool wide;  // q's rows and heads are 16-byte aligned
     float* parts;  // of (sequence, head, split, row): head_dim sums; after all of them (M, l)
     float2* parts_ml;
     uint32_t rows_most;  // rows of a sequence and head at most
@@ -83,12 +86,58 @@ __device__ __forceinline__ float add_halves(float x) {
     return bits_float(r[0]) + bits_float(r[1]);
 }
 
-__device__ __forceinline__ float value_at(const void* p, size_t i, int dtype) {
-    return dtype == ZK_BF16 ? load_one<ZK_BF16>(p, i) : load_one<ZK_F16>(p, i);
+// N consecutive elements of q (16 bits each, N a multiple of 8), as they lie in memory: one wide load for eight where the
+// caller's addresses allow it.
+template <int N>
+__device__ __forceinline__ void load_raw(const void* p, size_t at, bool wide, v4u (&r)[N / 8]) {
+    const uint16_t* x = (const uint16_t*)p + at;
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) r[i] = ((const v4u*)x)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[i][e] = (uint32_t)x[8 * i + 2 * e] | ((uint32_t)x[8 * i + 2 * e + 1] << 16);
+    }
 }
+
+// A row of q, spread over lanes that hold N elements each: scaled to just below 2^15 by a power of two, as 16-bit floats.
+// Returns the factor that takes the power back and brings the units of log2; NaN for a row that is not finite.
+struct LargestOf2 {
+    __device__ __forceinline__ float operator()(float x) const { return max_halves(x); }
+};
+struct LargestOf4 {
+    __device__ __forceinline__ float operator()(float x) const { return max_halves(max_rows(x)); }
+};
+template <int N, typename Largest>
+__device__ __forceinline__ float scale_row(const v4u (&raw)[N / 8], int dtype, float scale, v8h (&out)[N / 8], Largest largest) {
+    float x[N], amax = 0.0f;
+    if (dtype == ZK_BF16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = half_of<ZK_BF16>(raw[i >> 3][(i & 7) >> 1], i & 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = half_of<ZK_F16>(raw[i >> 3][(i & 7) >> 1], i & 1);
+    }
+    uint32_t most = 0;  // the bits of |x|: infinities and NaN are above every number
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t bits = float_bits(x[i]) & 0x7fffffffu;
+        most = bits > most ? bits : most;
+    }
+    amax = largest(most >= 0x7f800000u ? kInf : bits_float(most));
+    const bool fine = amax < kInf;
+    int ex = 0;
+    if (fine && amax != 0.0f) (void)frexpf(amax, &ex);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i >> 3][i & 7] = fine ? (_Float16)ldexpf(x[i], 15 - ex) : (_Float16)0.0f;
+    return fine ? ldexpf(scale * kLog2e, ex - 15) : __builtin_nanf("");
+}
+
 __device__ __forceinline__ void put_at(void* p, size_t i, float f, int dtype) {
-    if (dtype == ZK_BF16) store_one<ZK_BF16>(p, i, f);
-    else store_one<ZK_F16>(p, i, f);
+    const uint16_t b = half_bits<ZK_BF16>(f), h = half_bits<ZK_F16>(f);
+    ((uint16_t*)p)[i] = dtype == ZK_BF16 ? b : h;
 }
 
 // Where row r of a sequence and head lies in q (or out).
@@ -122,30 +171,40 @@ __device__ __forceinline__ Tiles tiles_of(const Args& a, const SeqView& v, int32
     return t;
 }
 
-// A page of a sequence: its number (0 where the table names none), and what its exponents are worth.
-struct Page {
-    uint32_t at;
-    bool none;
-};
-__device__ __forceinline__ Page page_at(const Args& a, uint32_t b, uint32_t token, uint32_t len) {
-    Page p = {0, false};
-    if (token < len) {
-        p.at = (uint32_t)a.s.table[(size_t)b * a.s.table_stride + (token >> a.page_log)];
-        p.none = p.at >= a.cache.pages;
-        if (p.none) p.at = 0;
-    }
-    return p;
+// Tiles of a workgroup's part.  The same for all sequences of a call, so that workgroups have like work and short sequences
+// fewer of them; more only where a sequence is longer than the caller said.
+__device__ __forceinline__ uint32_t part_of(const Args& a, const Tiles& t) {
+    const uint32_t need = (t.end - t.first + a.splits - 1) / a.splits;
+    return need > a.each ? need : a.each;
 }
+
+// The page of a token, as the table has it: what it is worth is looked at when it is used, not while it is on its way.
+// Tokens behind the sequence have the last one's.  len > 0.
+__device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t b, uint32_t token, uint32_t len) {
+    const uint32_t last = token < len ? token : len - 1;
+    return (uint32_t)a.s.table[(size_t)b * a.s.table_stride + (last >> a.page_log)];
+}
+__device__ __forceinline__ uint32_t page_or_0(const Args& a, uint32_t page) { return page < a.cache.pages ? page : 0; }
+
 __device__ __forceinline__ float exponent_value(int e) { return e == ZK_EXP_NAN ? __builtin_nanf("") : (float)e; }
+
+// 2^-b. Of a poisoned page 0: the weights of the keys that a row sees there are NaN by themselves, those of the others 0.
+__device__ __forceinline__ float back_of(float b) { return b == b ? exp2_of(-b) : 0.0f; }
 
 // What a row ends with.
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -kInf : (m + __log2f(l)) * kLn2; }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
 
-// NJ: head_dim in units of 64, rounded up.  RT: tiles of 16 rows.  Lane 16 g + i: row i of a tile, tokens 16 g .. 16 g + 15.
-template <int NJ, int RT>
-__global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
+// NJ: head_dim in units of 64, rounded up.  RT: tiles of 16 rows.  W: wavefronts.  Lane 16 g + i: row i of a tile, tokens
+// 16 g .. 16 g + 15.
+template <int NJ, int RT, int W>
+struct FewLds {
+    static constexpr int row = 64 * NJ + 4;  // of sums, padded
+    static size_t bytes(uint32_t rows) { return (2 * (size_t)W * 16 * RT + (size_t)W * rows * row) * sizeof(float); }
+};
+template <int NJ, int RT, int W>
+__global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
     constexpr int DT = 4 * NJ;  // tiles of 16 dimensions
     extern __shared__ float sh[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15;
@@ -158,70 +217,52 @@ __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Arg
     if (v.rows == 0) return;
     const uint32_t R = (uint32_t)v.rows * a.group;
     const Tiles tiles = tiles_of(a, v, 0, v.rows - 1);
-    const uint32_t each = (tiles.end - tiles.first + a.splits - 1) / a.splits;
+    const uint32_t each = part_of(a, tiles);
     const uint32_t t_first = tiles.first + split * each, t_end = t_first + each < tiles.end ? t_first + each : tiles.end;
     if (a.splits > 1 && t_first >= t_end) return;  // k_attend_join knows
 
-    // q, scaled by a power of two; qmul takes that back and brings the units of log2
-    v8h qf[RT][NJ][2];
-    float qmul[RT];
-    int32_t pos[RT];  // the last key that the lane's row sees
+    v4u raw[RT][2 * NJ];  // q as it lies in memory; asked for first, since loads come back in order
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const uint32_t r = rt * 16 + i16;
-        float x[NJ][16], amax = 0.0f;
-        const size_t at = r < R ? row_at(a, v, h, r, a.qrow, a.qhead) : 0;
+        const size_t at = row_at(a, v, h, r < R ? r : 0, a.qrow, a.qhead);  // rows behind the last: a copy of the first
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t c = 64 * j + 16 * g + e;
-                x[j][e] = r < R && c < d ? value_at(a.q, at + c, a.dtype) : 0.0f;
-                // NaN has to come through as infinity does
-                amax = fabsf(x[j][e]) <= 3.4028235e38f ? fmaxf(amax, fabsf(x[j][e])) : kInf;
-                if (amax == kInf) x[j][e] = 0.0f;
-            }
-        amax = max_halves(max_rows(amax));
-        int ex = 0;
-        (void)frexpf(amax, &ex);
-        if (amax == 0.0f || amax == kInf) ex = 0;
-        qmul[rt] = amax == kInf ? __builtin_nanf("") : ldexpf(a.scale * kLog2e, ex - 15);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) qf[rt][j][e >> 3][e & 7] = (_Float16)ldexpf(x[j][e], 15 - ex);
-        pos[rt] = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
+        for (int j = 0; j < NJ; ++j) {
+            v4u two[2] = {v4u{0, 0, 0, 0}, v4u{0, 0, 0, 0}};
+            if (64 * j + 16 * g < d) load_raw<16>(a.q, at + 64 * j + 16 * g, a.wide, two);
+            raw[rt][2 * j] = two[0];
+            raw[rt][2 * j + 1] = two[1];
+        }
     }
 
+    // Every load is made: tokens behind the sequence read some page of it, pages that are none page 0, dimensions behind
+    // head_dim the row's first (q is 0 there).  All are numbers, and nothing of them is kept.
     const uint32_t len = (uint32_t)v.len, rk = i16 >> 2;
     const size_t page_stride = (size_t)T * d;
     v4u kr[4][NJ], vr[DT];
-    auto load_k = [&](const Page& p, uint32_t t) {
-        const uint32_t token = t * kTile + 16 * rk;
-        const int8_t* at = a.cache.k + ((size_t)p.at * H + h) * page_stride + (size_t)((token & (T - 1)) + (i16 & 3)) * d + 16 * g;
+    auto load_k = [&](uint32_t page, uint32_t t) {
+        const uint32_t slot = (t * kTile + 16 * rk) & (T - 1);
+        const int8_t* at = a.cache.k + ((size_t)page_or_0(a, page) * H + h) * page_stride + (slot + (i16 & 3)) * d;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int j = 0; j < NJ; ++j) {
+            const uint32_t c = 64 * j + 16 * g < d ? 64 * j + 16 * g : 0;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                kr[u][j] = v4u{0, 0, 0, 0};
-                if (token < len && 64 * j + 16 * g < d) kr[u][j] = __builtin_nontemporal_load((const v4u*)(at + (size_t)(4 * u) * d + 64 * j));
-            }
-    };
-    auto load_v = [&](const Page& p, uint32_t t) {
-        const uint32_t token = t * kTile + 16 * g;
-        const int8_t* at = a.cache.v + ((size_t)p.at * H + h) * page_stride + ((size_t)i16 << a.page_log) + (token & (T - 1));
-#pragma unroll
-        for (int c = 0; c < DT; ++c) {
-            vr[c] = v4u{0, 0, 0, 0};
-            if (token < len && 16u * c < d) vr[c] = __builtin_nontemporal_load((const v4u*)(at + ((size_t)(16 * c) << a.page_log)));
+            for (int u = 0; u < 4; ++u) kr[u][j] = *(const v4u*)(at + 4 * u * d + c);
         }
     };
-    float ke = 0.0f, ve = 0.0f;  // exponents of the lane's 16 tokens
-    auto load_e = [&](const Page& p) {
-        const size_t at = (size_t)p.at * H + h;
-        ke = p.none ? __builtin_nanf("") : exponent_value(a.cache.k_exp[at]);
-        ve = p.none ? 0.0f : exponent_value(a.cache.v_exp[at]);
-        if (p.none) report(a.s, ZK_FAULT_PAGE);
+    auto load_v = [&](uint32_t page, uint32_t t) {
+        const uint32_t slot = (t * kTile + 16 * g) & (T - 1);
+        const int8_t* at = a.cache.v + ((size_t)page_or_0(a, page) * H + h) * page_stride + (i16 << a.page_log) + slot;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) vr[c] = *(const v4u*)(at + ((16u * c < d ? 16u * c : 0) << a.page_log));
+    };
+    int ke = 0, ve = 0;  // exponents of the lane's 16 tokens
+    bool none = false;   // whether their page is none
+    auto load_e = [&](uint32_t page) {
+        const size_t at = (size_t)page_or_0(a, page) * H + h;
+        ke = a.cache.k_exp[at];
+        ve = a.cache.v_exp[at];
+        none = page >= a.cache.pages;
     };
 
     v4f o[RT][DT];
@@ -235,24 +276,29 @@ __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Arg
     }
 
     uint32_t t = t_first + wave;
-    Page pk_next = {0, false}, pv_next = {0, false};
+    uint32_t pk_next = 0, pv_next = 0;
     if (t < t_end) {
-        const Page pk = page_at(a, b, t * kTile + 16 * rk, len), pv = page_at(a, b, t * kTile + 16 * g, len);
+        const uint32_t pk = page_of(a, b, t * kTile + 16 * rk, len), pv = page_of(a, b, t * kTile + 16 * g, len);
+        pk_next = page_of(a, b, (t + W) * kTile + 16 * rk, len);
+        pv_next = page_of(a, b, (t + W) * kTile + 16 * g, len);
         load_k(pk, t);
         load_e(pv);
         load_v(pv, t);
-        if (t + 4 < t_end) {
-            pk_next = page_at(a, b, (t + 4) * kTile + 16 * rk, len);
-            pv_next = page_at(a, b, (t + 4) * kTile + 16 * g, len);
-        }
     }
-    for (; t < t_end; t += 4) {
-        const bool more = t + 4 < t_end;
-        Page pk_after = {0, false}, pv_after = {0, false};
-        if (t + 8 < t_end) {
-            pk_after = page_at(a, b, (t + 8) * kTile + 16 * rk, len);
-            pv_after = page_at(a, b, (t + 8) * kTile + 16 * g, len);
-        }
+    // q, scaled by a power of two; qmul takes that back and brings the units of log2
+    v8h qf[RT][2 * NJ];
+    float qmul[RT];
+    int32_t pos[RT];  // the last key that the lane's row sees
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const uint32_t r = rt * 16 + i16;
+        qmul[rt] = scale_row<16 * NJ>(raw[rt], a.dtype, a.scale, qf[rt], LargestOf4());
+        pos[rt] = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
+    }
+
+    for (; t < t_end; t += W) {
+        const bool more = t + W < t_end;
+        const uint32_t pk_after = page_of(a, b, (t + 2 * W) * kTile + 16 * rk, len), pv_after = page_of(a, b, (t + 2 * W) * kTile + 16 * g, len);
         v4f s[RT][4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -263,36 +309,41 @@ __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Arg
                 const v8h a0 = widen(kr[u][j][0], kr[u][j][1]), a1 = widen(kr[u][j][2], kr[u][j][3]);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
-                    s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, qf[rt][j][0], s[rt][u], 0, 0, 0);
-                    s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, qf[rt][j][1], s[rt][u], 0, 0, 0);
+                    s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0, qf[rt][2 * j], s[rt][u], 0, 0, 0);
+                    s[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, qf[rt][2 * j + 1], s[rt][u], 0, 0, 0);
                 }
             }
         }
-        if (more) load_k(pk_next, t + 4);
-        const float kscale = exp2_of(ke), vback = exp2_of(-ve), vadd = ve;
+        if (more) load_k(pk_next, t + W);
+        // a page that is none has a score that is none
+        const float kscale = none ? __builtin_nanf("") : exp2_of(exponent_value(ke)), vadd = none ? 0.0f : exponent_value(ve), vback = back_of(vadd);
+        if (none && t * kTile + 16 * g < len) report(a.s, ZK_FAULT_PAGE);
         if (more) load_e(pv_next);
 
         const int32_t base = (int32_t)(t * kTile);
         // whether every row sees all 64 tokens
-        const bool whole = base + (int32_t)kTile - 1 <= v.len - v.rows && (!a.window || (int64_t)base > (int64_t)v.len - 1 - a.window);
+        const bool whole = base + (int32_t)kTile - 1 <= v.len - v.rows && base > (a.window ? v.len - 1 - (int32_t)a.window : -1);
         v8h p[RT][2];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const float mul = qmul[rt] * kscale;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[rt][u] = s[rt][u] * mul + vadd;
+            if (!whole) {
+                const int32_t key0 = base + 16 * (int32_t)g, low = a.window ? pos[rt] - (int32_t)a.window : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int32_t key = key0 + 4 * u + e;
+                        if (key > pos[rt] || key <= low) s[rt][u][e] = -kInf;
+                    }
+            }
             float top = -kInf;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = s[rt][u][e] * mul + vadd;
-                    if (!whole) {
-                        const int32_t key = base + 16 * (int32_t)g + 4 * u + e;
-                        const bool seen = key <= pos[rt] && (!a.window || (int64_t)key > (int64_t)pos[rt] - a.window);
-                        x = seen ? x : -kInf;
-                    }
-                    s[rt][u][e] = x;
-                    top = fmaxf(top, x);
-                }
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[rt][u][e]);
             top = max_halves(max_rows(top)) - kHead;
             if (__ballot(top > m[rt])) {
                 const float now = fmaxf(m[rt], top), f = exp2_of(now == -kInf ? 0.0f : m[rt] - now);
@@ -317,7 +368,6 @@ __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Arg
         }
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-            if (16u * c >= d) continue;
             const v8h a0 = widen(vr[c][0], vr[c][1]), a1 = widen(vr[c][2], vr[c][3]);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -325,65 +375,68 @@ __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_few(Arg
                 o[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1, p[rt][1], o[rt][c], 0, 0, 0);
             }
         }
-        if (more) load_v(pv_next, t + 4);
+        if (more) load_v(pv_next, t + W);
         pk_next = pk_after;
         pv_next = pv_after;
     }
 
-    // The wavefronts' sums: relative to one maximum, then two and two in LDS.
-    const uint32_t D = 16 * DT + 4;  // a row of sums, padded
-    float* ml = sh;                  // [wave][16 RT]
-    float* sums = sh + 2 * 4 * 16 * RT;
+    // The wavefronts' sums meet in LDS, each relative to its own maximum.
+    constexpr uint32_t D = FewLds<NJ, RT, W>::row;
+    float* ms = sh;  // [wave][16 RT]
+    float* ls = ms + W * 16 * RT;
+    float* sums = ls + W * 16 * RT;  // [wave][R][D]
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
+        const uint32_t r = rt * 16 + i16;
         l[rt] = add_halves(add_rows(l[rt]));
         if (g == 0) {
-            ml[wave * 16 * RT + rt * 16 + i16] = m[rt];
-            ml[(4 + wave) * 16 * RT + rt * 16 + i16] = l[rt];
+            ms[wave * 16 * RT + r] = m[rt];
+            ls[wave * 16 * RT + r] = l[rt];
         }
+        if (r < R)
+#pragma unroll
+            for (int c = 0; c < DT; ++c) *(v4f*)(sums + (size_t)(wave * R + r) * D + 16 * c + 4 * g) = o[rt][c];
     }
     __syncthreads();
-    for (int turn = 0; turn < 2; ++turn) {
-        if ((int)(wave >> 1) == turn) {
-            float* to = sums + (size_t)(wave & 1) * 16 * RT * D;
+    const uint32_t quads = d >> 2;
+    for (uint32_t i = tid; i < R * quads; i += 64 * W) {
+        const uint32_t r = i / quads, c = (i - r * quads) * 4;
+        float mw[W], all = -kInf, l_all = 0.0f;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float* w = ml + rt * 16 + i16;
-                const float all = fmaxf(fmaxf(w[0], w[16 * RT]), fmaxf(w[2 * 16 * RT], w[3 * 16 * RT]));
-                const float f = exp2_of(all == -kInf ? 0.0f : m[rt] - all);
-#pragma unroll
-                for (int c = 0; c < DT; ++c) {
-                    v4f* cell = (v4f*)(to + (size_t)(rt * 16 + i16) * D + 16 * c + 4 * g);
-                    v4f x = o[rt][c] * f;
-                    if (turn) x += *cell;
-                    *cell = x;
-                }
-            }
+        for (int w = 0; w < W; ++w) {
+            mw[w] = ms[w * 16 * RT + r];
+            all = fmaxf(all, mw[w]);
         }
-        __syncthreads();
-    }
-    for (uint32_t i = tid; i < R * d; i += kBlock) {
-        const uint32_t r = i / d, c = i - r * d;
-        const float* w = ml + r;
-        const float all = fmaxf(fmaxf(w[0], w[16 * RT]), fmaxf(w[2 * 16 * RT], w[3 * 16 * RT])), ref = all == -kInf ? 0.0f : all;
-        float ls = 0.0f;
+        const float ref = all == -kInf ? 0.0f : all;
+        v4f sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int x = 0; x < 4; ++x) ls += w[(4 + x) * 16 * RT] * exp2_of(all == -kInf ? 0.0f : w[x * 16 * RT] - all);
-        const float sum = sums[(size_t)r * D + c] + sums[(size_t)(16 * RT + r) * D + c];
+        for (int w = 0; w < W; ++w) {
+            const float f = exp2_of(mw[w] - ref);
+            l_all += ls[w * 16 * RT + r] * f;
+            sum += *(const v4f*)(sums + (size_t)(w * R + r) * D + c) * f;
+        }
         if (a.splits == 1) {
-            put_at(a.out, row_at(a, v, h, r, a.orow, a.ohead) + c, ls == 0.0f ? 0.0f : sum / ls, a.dtype);
-            if (a.lse && c == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, ls);
+            const size_t at = row_at(a, v, h, r, a.orow, a.ohead) + c;
+            const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put_at(a.out, at + e, l_all == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
+            if (a.lse && c == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l_all);
         } else {
             const size_t part = (((size_t)b * H + h) * a.splits + split) * a.rows_most + r;
-            a.parts[part * d + c] = sum;
-            if (c == 0) a.parts_ml[part] = make_float2(all, ls);
+            *(v4f*)(a.parts + part * d + c) = sum;
+            if (c == 0) a.parts_ml[part] = make_float2(all, l_all);
         }
     }
 }
 
-// A workgroup: one row of one sequence and head; a thread for each dimension.
+// A workgroup: one row of one sequence and head.  Threads hold four dimensions each; what is left of 256 takes splits
+// apart, and LDS adds them up.
+static const uint32_t kMostSplits = 256;
 __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
-    const uint32_t r = blockIdx.x, h = blockIdx.y, b = blockIdx.z, d = a.cache.head_dim, H = a.cache.kv_heads, c = threadIdx.x;
+    __shared__ float weight[kMostSplits];
+    __shared__ float red[4], red_l[4];
+    __shared__ v4f sums[kBlock];
+    const uint32_t r = blockIdx.x, h = blockIdx.y, b = blockIdx.z, d = a.cache.head_dim, H = a.cache.kv_heads, tid = threadIdx.x;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
         if (r == 0) not_a_number(a, b, h);
@@ -391,21 +444,39 @@ __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
     }
     if (r >= (uint32_t)v.rows * a.group) return;
     const Tiles tiles = tiles_of(a, v, 0, v.rows - 1);
-    const uint32_t n = tiles.end - tiles.first, each = (n + a.splits - 1) / a.splits, used = n ? (n + each - 1) / each : 0;
+    const uint32_t each = part_of(a, tiles), used = (tiles.end - tiles.first + each - 1) / each;
     const size_t part0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
-    float top = -kInf;
-    for (uint32_t s = 0; s < used; ++s) top = fmaxf(top, a.parts_ml[part0 + (size_t)s * a.rows_most].x);
-    const float ref = top == -kInf ? 0.0f : top;
-    float l = 0.0f, sum = 0.0f;
-    for (uint32_t s = 0; s < used; ++s) {
-        const size_t part = part0 + (size_t)s * a.rows_most;
-        const float2 ml = a.parts_ml[part];
-        const float f = exp2_of(ml.x - ref);
-        l += ml.y * f;
-        if (c < d) sum += a.parts[part * d + c] * f;
+    const float2 ml = tid < used ? a.parts_ml[part0 + (size_t)tid * a.rows_most] : make_float2(-kInf, 0.0f);
+    float top = ml.x;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if ((tid & 63) == 0) red[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float ref = top == -kInf ? 0.0f : top, f = exp2_of(ml.x - ref);
+    weight[tid] = f;
+    float l = ml.y * f;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+    if ((tid & 63) == 0) red_l[tid >> 6] = l;
+    __syncthreads();
+    l = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+    const uint32_t quads = d >> 2, ways = kBlock / quads, way = tid / quads, c = tid - way * quads;
+    v4f sum = {0, 0, 0, 0};
+    if (way < ways) {
+        const v4f* at = (const v4f*)a.parts + part0 * quads + c;
+#pragma unroll 8
+        for (uint32_t s = way; s < used; s += ways) sum += at[(size_t)s * a.rows_most * quads] * weight[s];
     }
-    if (c < d) put_at(a.out, row_at(a, v, h, r, a.orow, a.ohead) + c, l == 0.0f ? 0.0f : sum / l, a.dtype);
-    if (a.lse && c == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l);
+    sums[tid] = sum;
+    __syncthreads();
+    if (way == 0) {
+        for (uint32_t w = 1; w < ways; ++w) sum += sums[w * quads + c];
+        const size_t at = row_at(a, v, h, r, a.orow, a.ohead) + 4 * c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put_at(a.out, at + e, l == 0.0f ? 0.0f : sum[e] / l, a.dtype);
+    }
+    if (a.lse && tid == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------------
@@ -413,11 +484,16 @@ __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
 static const uint32_t kRows = 128;
 
 // Lane 32 h + i: row i of its wavefront's 32, tokens 16 h .. 16 h + 15 of each half of a tile.
-template <int NJ>
-__global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a) {
-    constexpr int DT = 2 * NJ;            // tiles of 32 dimensions
-    constexpr uint32_t KROW = 128 * NJ;   // bytes of a row of K in LDS
-    constexpr uint32_t BUF = 2 * 64 * KROW;  // K and V
+// DT: head_dim in units of 32, rounded up.  Rows in LDS are padded by 16 bytes: then those of 16 neighbouring rows lie in
+// different banks, whatever DT.
+template <int DT>
+struct ManyLds {
+    static constexpr uint32_t krow = 64 * DT + 16, vrow = 128 + 16, k_bytes = 64 * krow, bytes = k_bytes + 32 * DT * vrow;
+};
+template <int DT>
+__global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a) {
+    using L = ManyLds<DT>;
+    constexpr int PIECES = (DT + 1) / 2;  // of 16 codes, for a thread, of a tile's K and of its V
     extern __shared__ char lds[];
     __shared__ float exps[2][2][4];       // [buffer][K, V][16 tokens]
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, i32 = lane & 31;
@@ -435,49 +511,39 @@ __global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a)
     const Tiles tiles = tiles_of(a, v, tok0, tok1);
     const uint32_t r = r0 + wave * 32 + i32, len = (uint32_t)v.len;
 
-    v8h qf[4 * NJ];
+    v8h qf[2 * DT];
     float qmul;
     {
-        float x[4 * NJ][8], amax = 0.0f;
-        const size_t at = r < R ? row_at(a, v, h, r, a.qrow, a.qhead) : 0;
+        const size_t at = row_at(a, v, h, r < R ? r : 0, a.qrow, a.qhead);
+        v4u raw[2 * DT];
 #pragma unroll
-        for (int k = 0; k < 4 * NJ; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t c = 16 * k + 8 * half + e;
-                x[k][e] = r < R && c < d ? value_at(a.q, at + c, a.dtype) : 0.0f;
-                amax = fabsf(x[k][e]) <= 3.4028235e38f ? fmaxf(amax, fabsf(x[k][e])) : kInf;
-                if (amax == kInf) x[k][e] = 0.0f;
-            }
-        amax = max_halves(amax);
-        int ex = 0;
-        (void)frexpf(amax, &ex);
-        if (amax == 0.0f || amax == kInf) ex = 0;
-        qmul = amax == kInf ? __builtin_nanf("") : ldexpf(a.scale * kLog2e, ex - 15);
-#pragma unroll
-        for (int k = 0; k < 4 * NJ; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) qf[k][e] = (_Float16)ldexpf(x[k][e], 15 - ex);
+        for (int k = 0; k < 2 * DT; ++k) {
+            v4u one[1] = {v4u{0, 0, 0, 0}};
+            if (16u * k < d) load_raw<8>(a.q, at + 16 * k + 8 * half, a.wide, one);
+            raw[k] = one[0];
+        }
+        qmul = scale_row<16 * DT>(raw, a.dtype, a.scale, qf, LargestOf2());
     }
     const int32_t pos = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
+    const int32_t low = a.window ? pos - (int32_t)a.window : -1;  // keys in (low, pos] are seen
     const int32_t pos_first = v.len - v.rows + tok0, pos_last = v.len - v.rows + tok1;
 
     // Row of K for token x of 32: the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
-    v4u kr[NJ], vr[NJ];
+    v4u kr[PIECES], vr[PIECES];
     auto fetch = [&](uint32_t t) {
 #pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-            const uint32_t p = tid + kBlock * i, slot = p / (4 * NJ), c = p % (4 * NJ) * 16, token = t * kTile + slot;
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t p = tid + kBlock * i, slot = p / (2 * DT), c = p % (2 * DT) * 16, token = t * kTile + slot;
             kr[i] = v4u{0, 0, 0, 0};
-            if (c < d && token < len) {
-                const Page page = page_at(a, b, token, len);
-                kr[i] = *(const v4u*)(a.cache.k + (((size_t)page.at * H + h) * T + (token & (T - 1))) * d + c);
+            if (p < 128 * DT && c < d && token < len) {
+                const uint32_t page = page_or_0(a, page_of(a, b, token, len));
+                kr[i] = *(const v4u*)(a.cache.k + (((size_t)page * H + h) * T + (token & (T - 1))) * d + c);
             }
             const uint32_t run = p & 3, dim = p >> 2, vt = t * kTile + 16 * run;
             vr[i] = v4u{0, 0, 0, 0};
-            if (dim < d && vt < len) {
-                const Page page = page_at(a, b, vt, len);
-                vr[i] = *(const v4u*)(a.cache.v + ((((size_t)page.at * H + h) * d + dim) << a.page_log) + (vt & (T - 1)));
+            if (p < 128 * DT && dim < d && vt < len) {
+                const uint32_t page = page_or_0(a, page_of(a, b, vt, len));
+                vr[i] = *(const v4u*)(a.cache.v + ((((size_t)page * H + h) * d + dim) << a.page_log) + (vt & (T - 1)));
             }
         }
     };
@@ -485,25 +551,27 @@ __global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a)
     auto fetch_exp = [&](uint32_t t) {
         if (tid < 8) {
             const uint32_t token = t * kTile + 16 * (tid & 3);
-            const Page page = page_at(a, b, token, len);
-            if (page.none) report(a.s, ZK_FAULT_PAGE);
-            const size_t at = (size_t)page.at * H + h;
-            my_exp = page.none ? (tid < 4 ? __builtin_nanf("") : 0.0f)
-                               : token < len ? exponent_value(tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at]) : 0.0f;
+            const uint32_t page = page_of(a, b, token, len);
+            const bool none = page >= a.cache.pages;
+            if (none && token < len) report(a.s, ZK_FAULT_PAGE);
+            const size_t at = (size_t)page_or_0(a, page) * H + h;
+            my_exp = none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at]);
         }
     };
     auto stage = [&](uint32_t buf) {
-        char* kb = lds + buf * BUF;
-        char* vb = kb + 64 * KROW;
+        char* kb = lds + buf * L::bytes;
+        char* vb = kb + L::k_bytes;
 #pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-            const uint32_t p = tid + kBlock * i, slot = p / (4 * NJ), c = p % (4 * NJ) * 2, x = slot & 31;
-            const uint32_t row = (slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3), turn = row & (8 * NJ - 1) & 15;
-            *(v8h*)(kb + row * KROW + ((c ^ turn) << 4)) = widen(kr[i][0], kr[i][1]);
-            *(v8h*)(kb + row * KROW + (((c + 1) ^ turn) << 4)) = widen(kr[i][2], kr[i][3]);
-            const uint32_t run = (p & 3) * 2, dim = p >> 2;
-            *(v8h*)(vb + dim * 128 + ((run ^ (dim & 7)) << 4)) = widen(vr[i][0], vr[i][1]);
-            *(v8h*)(vb + dim * 128 + (((run + 1) ^ (dim & 7)) << 4)) = widen(vr[i][2], vr[i][3]);
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t p = tid + kBlock * i, slot = p / (2 * DT), c = p % (2 * DT), x = slot & 31;
+            if (p >= 128 * DT) continue;
+            const uint32_t row = (slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3);
+            v8h* k16 = (v8h*)(kb + row * L::krow + c * 32);
+            k16[0] = widen(kr[i][0], kr[i][1]);
+            k16[1] = widen(kr[i][2], kr[i][3]);
+            v8h* v16 = (v8h*)(vb + (p >> 2) * L::vrow + (p & 3) * 32);
+            v16[0] = widen(vr[i][0], vr[i][1]);
+            v16[1] = widen(vr[i][2], vr[i][3]);
         }
         if (tid < 8) exps[buf][tid >> 2][tid & 3] = my_exp;
     };
@@ -524,37 +592,32 @@ __global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a)
             fetch(t + 1);
             fetch_exp(t + 1);
         }
-        const char* kb = lds + buf * BUF;
-        const char* vb = kb + 64 * KROW;
+        const char* kb = lds + buf * L::bytes;
+        const char* vb = kb + L::k_bytes;
         const int32_t base = (int32_t)(t * kTile);
         v16f s[2];
         float vback[2];
         float top = -kInf;
-        const bool whole = base + (int32_t)kTile - 1 <= pos_first && (!a.window || (int64_t)base > (int64_t)pos_last - a.window);
+        const bool whole = base + (int32_t)kTile - 1 <= pos_first && base > (a.window ? pos_last - (int32_t)a.window : -1);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             s[st] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-            const uint32_t row = st * 32 + i32, turn = row & (8 * NJ - 1) & 15;
+            const char* krow = kb + (st * 32 + i32) * L::krow + half * 16;
 #pragma unroll
-            for (int k = 0; k < 4 * NJ; ++k) {
-                if (16u * k >= d) continue;
-                const v8h f = *(const v8h*)(kb + row * KROW + (((2 * k + half) ^ turn) << 4));
-                s[st] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, qf[k], s[st], 0, 0, 0);
-            }
+            for (int k = 0; k < 2 * DT; ++k)
+                s[st] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h*)(krow + 32 * k), qf[k], s[st], 0, 0, 0);
             const float ke = exps[buf][0][2 * st + half], ve = exps[buf][1][2 * st + half];
             const float mul = qmul * exp2_of(ke);
-            vback[st] = exp2_of(-ve);
+            vback[st] = back_of(ve);
+            s[st] = s[st] * mul + ve;
+            if (!whole) {
+                const int32_t key0 = base + 32 * st + 16 * (int32_t)half;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float x = s[st][e] * mul + ve;
-                if (!whole) {
-                    const int32_t key = base + 32 * st + 16 * (int32_t)half + e;
-                    const bool seen = key <= pos && (!a.window || (int64_t)key > (int64_t)pos - a.window);
-                    x = seen ? x : -kInf;
-                }
-                s[st][e] = x;
-                top = fmaxf(top, x);
+                for (int e = 0; e < 16; ++e)
+                    if (key0 + e > pos || key0 + e <= low) s[st][e] = -kInf;
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[st][e]);
         }
         top = max_halves(top) - kHead;
         if (__ballot(top > m)) {
@@ -581,16 +644,12 @@ __global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a)
         }
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-            if (32u * c >= d) continue;
-            const uint32_t dim = 32 * c + i32;
+            const char* vrow = vb + (32 * c + i32) * L::vrow + half * 32;
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t chunk = (2 * st + half) * 2 + k;
-                    const v8h f = *(const v8h*)(vb + dim * 128 + ((chunk ^ (dim & 7)) << 4));
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p[st][k], o[c], 0, 0, 0);
-                }
+                for (int k = 0; k < 2; ++k)
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h*)(vrow + 64 * st + 16 * k), p[st][k], o[c], 0, 0, 0);
         }
     }
     l = add_halves(l);
@@ -610,54 +669,53 @@ __global__ __launch_bounds__(kBlock, NJ <= 2 ? 2 : 1) void k_attend_many(Args a)
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 
-// How many workgroups share a sequence: enough of them for some four on each of 256 CUs, but not less than a tile for each
-// of a workgroup's wavefronts.
-uint32_t splits_of(uint32_t seqs, uint32_t kv_heads, uint32_t max_len) {
-    const uint64_t tiles = div_up(max_len, kTile), most = div_up(tiles, 4), groups = (uint64_t)seqs * kv_heads;
-    uint64_t n = groups >= 1024 ? 1 : div_up(1024, groups ? groups : 1);
-    if (n > most) n = most;
-    return n < 1 ? 1 : (uint32_t)n;
+// How many workgroups share a sequence at most, and the tiles of each.
+struct Split {
+    uint32_t splits, each;
+};
+uint32_t most_splits(uint32_t seqs, uint32_t kv_heads, uint32_t tiles) {
+    const uint64_t groups = (uint64_t)seqs * kv_heads;
+    uint64_t n = groups >= kWorkgroups ? 1 : div_up(kWorkgroups, groups);
+    if (n > div_up(tiles, 4)) n = div_up(tiles, 4);  // a tile for each wavefront
+    return n > kMostSplits ? kMostSplits : (uint32_t)n;
 }
+Split split_of(uint32_t seqs, uint32_t kv_heads, uint32_t tiles) {
+    if (tiles <= kShort) return {1, tiles};
+    const uint32_t each = (uint32_t)align_up(div_up(tiles, most_splits(seqs, kv_heads, tiles)), 4);
+    return {(uint32_t)div_up(tiles, each), each};
+}
+uint32_t tiles_for(uint32_t len) { return len ? (uint32_t)div_up(len, kTile) : 1; }
 
 bool few_rows(uint64_t rows) { return rows <= 32; }
 
-template <int NJ, int RT>
+template <int NJ, int RT, int W>
 int launch_few(const Args& a, hipStream_t stream) {
-    const size_t lds = (2 * 4 * 16 * RT + 2 * (size_t)16 * RT * (64 * NJ + 4)) * sizeof(float);
-    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_few<NJ, RT>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, stream, a);
+    const size_t lds = FewLds<NJ, RT, W>::bytes(a.rows_most);
+    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, W>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_attend_few<NJ, RT, W>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(64 * W), lds, stream, a);
+    if (a.splits > 1) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
     ZK_HIP_TRY(hipGetLastError());
-    if (a.splits > 1) {
-        const unsigned threads = (unsigned)align_up(a.cache.head_dim, 64);
-        hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(threads), 0, stream, a);
-        ZK_HIP_TRY(hipGetLastError());
-    }
+    return ZK_OK;
+}
+
+template <int DT>
+int launch_many(const Args& a, hipStream_t stream) {
+    const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
+    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_attend_many<DT>), dim3((unsigned)div_up(a.rows_most, kRows), a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, stream, a);
+    ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
 
 template <int NJ>
 int launch(const Args& a, hipStream_t stream) {
-    if (a.rows_most <= 16) return launch_few<NJ, 1>(a, stream);
-    if (few_rows(a.rows_most)) return launch_few<NJ, 2>(a, stream);
-    const size_t lds = 2 * 2 * 64 * 128 * (size_t)NJ;
-    ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<NJ>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_many<NJ>), dim3((unsigned)div_up(a.rows_most, kRows), a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, stream, a);
-    ZK_HIP_TRY(hipGetLastError());
-    return ZK_OK;
+    if (a.rows_most <= 16) return a.splits == 1 ? launch_few<NJ, 1, 8>(a, stream) : launch_few<NJ, 1, 4>(a, stream);
+    if (few_rows(a.rows_most)) return launch_few<NJ, 2, 4>(a, stream);
+    return a.cache.head_dim > 64 * NJ - 32 ? launch_many<2 * NJ>(a, stream) : launch_many<2 * NJ - 1>(a, stream);
 }
 
-struct Shape {
-    uint32_t rows_most, splits;
-    size_t parts;  // rows of partial sums
-};
-Shape shape_of(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads, uint32_t max_len) {
-    const uint32_t n = max_new < rows ? max_new : rows;
-    Shape s;
-    s.rows_most = n * (q_heads / kv_heads);
-    s.splits = few_rows((uint64_t)n * (q_heads / kv_heads)) ? splits_of(seqs, kv_heads, max_len) : 1;
-    s.parts = s.splits > 1 ? (size_t)seqs * kv_heads * s.splits * s.rows_most : 0;
-    return s;
-}
+// Rows of a sequence and head at most.
+uint64_t rows_most(uint32_t rows, uint32_t max_new, uint32_t group) { return (uint64_t)(max_new < rows ? max_new : rows) * group; }
 
 }  // namespace
 }  // namespace zkmi
@@ -667,11 +725,14 @@ using namespace zkmi;
 extern "C" size_t kvcache_attention_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
                                                     uint32_t head_dim, uint32_t max_len) {
     if (!kv_heads || q_heads % kv_heads || !seqs || !rows || !max_new) return 0;
-    const Shape s = shape_of(seqs, rows, max_new, q_heads, kv_heads, max_len);
-    if (!s.parts) return 0;
+    const uint64_t most = rows_most(rows, max_new, q_heads / kv_heads);
+    const uint32_t tiles = tiles_for(max_len);
+    if (!few_rows(most) || tiles <= kShort) return 0;
+    // a window makes tiles and workgroups fewer, never more
+    const size_t parts = (size_t)seqs * kv_heads * most_splits(seqs, kv_heads, tiles) * most;
     Carver cv(nullptr, 0);
-    cv.take(s.parts * head_dim * sizeof(float));
-    cv.take(s.parts * sizeof(float2));
+    cv.take(parts * head_dim * sizeof(float));
+    cv.take(parts * sizeof(float2));
     return cv.used();
 }
 
@@ -683,8 +744,12 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     if (seqs->rows == 0 || seqs->seqs == 0) return ZK_OK;
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
-    if ((uint64_t)(seqs->max_new < seqs->rows ? seqs->max_new : seqs->rows) * group >= 0x80000000u) return ZK_E_BADARG;
-    const Shape sh = shape_of(seqs->seqs, seqs->rows, seqs->max_new, q_heads, cache->kv_heads, seqs->max_len);
+    const uint64_t most = rows_most(seqs->rows, seqs->max_new, group);
+    if (most >= 0x80000000u) return ZK_E_BADARG;
+    // what a window lets a sequence's rows see, with a tile that it ends in
+    const uint64_t seen = window ? (uint64_t)window + seqs->max_new + kTile : seqs->max_len;
+    const Split sp = few_rows(most) ? split_of(seqs->seqs, cache->kv_heads, tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len))
+                                    : Split{1, 1};
     Args a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -700,13 +765,16 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     a.group = group;
     a.page_log = (uint32_t)log2_floor(cache->page_tokens);
     a.dtype = dtype;
-    a.rows_most = sh.rows_most;
-    a.splits = sh.splits;
-    if (sh.parts) {
+    a.wide = aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0;
+    a.rows_most = (uint32_t)most;
+    a.splits = sp.splits;
+    a.each = sp.each;
+    if (sp.splits > 1) {
+        const size_t parts = (size_t)seqs->seqs * cache->kv_heads * sp.splits * most;
         if (!ws) return ZK_E_BUFSZ;
         Carver cv(ws, ws_bytes);
-        a.parts = (float*)cv.take(sh.parts * cache->head_dim * sizeof(float));
-        a.parts_ml = (float2*)cv.take(sh.parts * sizeof(float2));
+        a.parts = (float*)cv.take(parts * cache->head_dim * sizeof(float));
+        a.parts_ml = (float2*)cv.take(parts * sizeof(float2));
         if (cv.overflow() || !a.parts || !a.parts_ml) return ZK_E_BUFSZ;
     }
     hipStream_t s = as_stream(stream);

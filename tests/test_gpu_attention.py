@@ -159,6 +159,30 @@ def test_not_finite(zk, new, lens):
     assert out[hit].isnan().all() and lse[hit].isnan().all() and torch.equal(out[~hit], clean[~hit])
 
 
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_poisoned_values_that_no_row_sees(zk, new):
+    """Pages of another sequence, behind this one's end, or before its window share tiles with the keys that are seen."""
+    T, L = 16, 200 + new
+    cache, q, cu, table, gen = make(zk, [new], [L], 4, 2, 64, T, torch.bfloat16, 17)
+    args = device(cu, [L], table)
+    for window in (0, 70, 5):
+        rc, want, wlse = zk.kvcache_attention(cache, q, *args, new, L, 0.125, window=window)
+        keep = [t.clone() for t in arrays(cache)]
+        seen = set(table[0]) if not window else {table[0][p // T] for p in range(max(0, L - new - window + 1), L)}
+        for page in range(cache.k.shape[0]):
+            if page not in seen:
+                cache.v_exp[page] = cache.k_exp[page] = zk.ZK_EXP_NAN
+        rc, out, lse = zk.kvcache_attention(cache, q, *args, new, L, 0.125, window=window)
+        assert torch.equal(out, want) and torch.equal(lse, wlse)
+        for t, w in zip(arrays(cache), keep):
+            t.copy_(w)
+    # page 0 stands in for what lies behind the end: it may be poisoned too
+    cache.v_exp[0] = cache.k_exp[0] = zk.ZK_EXP_NAN
+    table2 = [[p if p != 0 else 1 for p in table[0]]]
+    rc, out, lse = zk.kvcache_attention(cache, q, *device(cu, [L], table2), new, L, 0.125)
+    assert not out.isnan().any() and not lse.isnan().any()
+
+
 def test_strides(zk):
     new, lens, d = [3, 1], [50, 90], 64
     cache, q, cu, table, gen = make(zk, new, lens, 4, 2, d, 16, torch.bfloat16, 8)
