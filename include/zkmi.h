@@ -617,14 +617,14 @@ int kvcache_read(const kvcache_i8* cache, const int32_t* pages, size_t tokens, i
  * [n][ceil(k/group)], integers 0..4095, one for each `group` (32, 64 or 128)
  * consecutive inputs of an output (the last may be shorter).  A weight is
  * unit * c * scale: the integer c * scale has 16 bits, and `unit` is the fixed-point
- * step of the whole matrix.  k is a multiple of 32.
+ * step of the whole matrix.  n <= 2^24; k is a multiple of 32, at most 2^20.
  *
  * y[m][i] = unit * sum_j w[i][j] x[m][j] for `rows` vectors x (rows x k, y: rows x n, the
  * rows' strides given; x's rows 16-byte aligned).  ZK_F32, ZK_F16, ZK_BF16: y has the type of x; sums are
  * accumulated in 32 bits.  A row of x with a value that is not finite gives NaN.  ZK_I16: x are 16-bit integers, y are
  * int64_t and the sums themselves, exactly (unit is ignored): the Y that
- * matmul_sumcheck_prove_i16 proves for X = x and W = w4_expand_i16.   |x| < 2^120, else NaN.  rows may be 0.
- * ws: device, w4_matvec_workspace_bytes(dtype, rows, k) (0 for few rows: ws may be NULL then). */
+ * matmul_sumcheck_prove_i16 proves for X = x and W = w4_expand_i16.   |x| < 2^120, else NaN.  0 <= rows <= 2^20.
+ * ws: device, w4_matvec_workspace_bytes(dtype, rows, k) (0 for few rows and inputs: ws may be NULL then). */
 size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k);
 int w4_matvec(void* y, size_t y_row_stride, const void* x, size_t x_row_stride, int dtype, size_t rows, const uint8_t* codes,
               const uint16_t* scales, size_t n, size_t k, uint32_t group, float unit, void* ws, size_t ws_bytes, void* stream);

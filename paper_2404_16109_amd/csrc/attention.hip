@@ -27,7 +27,7 @@ namespace {
 static const float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 static const float kHead = 14.0f;      // P reaches up to 2^14
 static const uint32_t kTile = 64;      // tokens
-static const uint32_t kWorkgroups = 1024;
+static const uint32_t kWorkgroups = 512;
 static const uint32_t kShort = 16;     // tiles
 
 struct Args {

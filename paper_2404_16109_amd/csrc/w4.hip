@@ -23,7 +23,9 @@ namespace {
 
 static const int kStep = 128;                      // inputs a wavefront takes at a time
 static const int kWaves = 8;
-static const uint32_t kStageHalves = 16384;        // 32 KiB of x in LDS
+static const uint32_t kStageHalves = 32768;        // 64 KiB of x in LDS
+static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of columns
+static const uint32_t kWide = 16384;               // outputs from which a workgroup of the many-column kernel has 128
 
 template <int DT>
 struct Kind {
@@ -58,20 +60,31 @@ __device__ __forceinline__ void transpose_rows(v4u& r) {
     r = v4u{(uint32_t)c[0], (uint32_t)c[1], (uint32_t)d[0], (uint32_t)d[1]};
 }
 
-// Inputs k .. k+7 of a vector as its columns' operands, in the order 0 4 1 5 2 6 3 7.
+// Inputs k .. k+7 of a vector as they lie in memory, and as its columns' operands, in the order 0 4 1 5 2 6 3 7.
 template <int DT>
-__device__ __forceinline__ void columns_of(const void* x, size_t at, v4u (&out)[Kind<DT>::parts]) {
+struct Eight {
+    static constexpr int words = DT == ZK_F32 ? 2 : 1;
+    v4u r[words];
+};
+template <int DT>
+__device__ __forceinline__ Eight<DT> load_eight(const void* x, size_t at) {
+    Eight<DT> e;
+    const v4u* p = (const v4u*)((const char*)x + at * (DT == ZK_F32 ? 4 : 2));
+#pragma unroll
+    for (int i = 0; i < Eight<DT>::words; ++i) e.r[i] = p[i];
+    return e;
+}
+template <int DT>
+__device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<DT>::parts]) {
     if constexpr (DT == ZK_F16 || DT == ZK_BF16) {
-        const v4u r = *(const v4u*)((const uint16_t*)x + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = r[i >> 1], hi = r[2 + (i >> 1)];  // elements i and i + 4
-            out[0][i] = i & 1 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+            const uint32_t lo = x.r[0][i >> 1], hi = x.r[0][2 + (i >> 1)];  // elements i and i + 4
+            out[0][i] = __builtin_amdgcn_perm(hi, lo, i & 1 ? 0x07060302u : 0x05040100u);
         }
     } else if constexpr (DT == ZK_I16) {
-        const v4u r = *(const v4u*)((const uint16_t*)x + at);
         auto part = [&](int e, int p) -> uint32_t {
-            const int v = (int16_t)(r[e >> 1] >> (16 * (e & 1)));
+            const int v = (int16_t)(x.r[0][e >> 1] >> (16 * (e & 1)));
             return half_bits<ZK_BF16>((float)(p == 0 ? v >> 8 : v & 255));
         };
 #pragma unroll
@@ -79,25 +92,54 @@ __device__ __forceinline__ void columns_of(const void* x, size_t at, v4u (&out)[
 #pragma unroll
             for (int i = 0; i < 4; ++i) out[p][i] = part(i, p) | (part(i + 4, p) << 16);
     } else {
-        const v4f* f = (const v4f*)((const float*)x + at);
-        v4f r[2] = {f[0], f[1]};
+        float r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = bits_float(x.r[e >> 2][e & 3]);
 #pragma unroll
         for (int p = 0; p < 3; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t a = half_bits<ZK_BF16>(r[0][i]), b = half_bits<ZK_BF16>(r[1][i]);
-                out[p][i] = a | (b << 16);
-                r[0][i] -= bits_float(a << 16);
-                r[1][i] -= bits_float(b << 16);
+                const uint32_t lo = half_bits<ZK_BF16>(r[i]), hi = half_bits<ZK_BF16>(r[i + 4]);
+                out[p][i] = lo | (hi << 16);
+                r[i] -= bits_float(lo << 16);
+                r[i + 4] -= bits_float(hi << 16);
             }
     }
 }
 
-// Workgroup: 16 outputs, up to 16 columns; its eight wavefronts share out the steps and add up at the end.
+// Where a lane finds its output's weights: 16 bytes (32 inputs) of every step.
+struct Row {
+    const uint8_t* at;
+    uint32_t whole;  // steps whose 128 inputs are all there
+    bool tail;              // whether the lane has inputs in the last step, if that is not whole
+};
+__device__ __forceinline__ Row row_of(const uint8_t* codes, uint32_t n, uint32_t k, uint32_t out, uint32_t g) {
+    Row w = {codes + (size_t)(out < n ? out : n - 1) * (k >> 1), k / kStep, g * 32 < k % kStep};
+    if (w.whole || w.tail) w.at += g * 16;
+    return w;
+}
+// Behind the last input any weights will do, x is 0 there: the first ones.
+__device__ __forceinline__ v4u fetch(const Row& w, uint32_t j) {
+    const bool there = j < w.whole || (w.tail && j == w.whole);
+    return *(const v4u*)(w.at + (there ? (size_t)j * (kStep / 2) : 0));
+}
+
+// ---- few columns -----------------------------------------------------------------------------------------------------
+
+// How a workgroup of 512 brings x into LDS: `across` threads to a vector, each eight inputs at a time.
+__host__ __device__ __forceinline__ uint32_t threads_across(uint32_t vectors) { return vectors == 1 ? 512 : vectors == 2 ? 256 : 128; }
 template <int DT>
-__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, size_t rows,
+struct Pieces {
+    static constexpr int most = DT == ZK_F32 ? 4 : 8;  // of eight inputs, held by a thread
+};
+
+// Workgroup: 16 outputs, up to 16 columns; its eight wavefronts share out the steps and add up at the end.  x comes from
+// LDS where all of it fits there (STAGED), else from `xf`, where k_w4_columns has laid out the operands [k / 8][16]: a
+// wavefront then reads a kilobyte of them for each instruction, out of the L2, and nothing waits for anything in the loop.
+template <int DT, bool STAGED>
+__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, size_t rows,
                                                         const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
-                                                        uint32_t group_log, uint32_t chunk, float unit2) {
+                                                        uint32_t group_log, float unit2) {
     constexpr int parts = Kind<DT>::parts;
     extern __shared__ v4u shared[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15;
@@ -105,68 +147,132 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     const size_t m0 = (size_t)blockIdx.y * Kind<DT>::vectors;
     const uint32_t vectors = rows - m0 < (size_t)Kind<DT>::vectors ? (uint32_t)(rows - m0) : Kind<DT>::vectors;
     const uint32_t cols = vectors * parts;
-    v4u* xs = shared;                                                // [chunk / 8][cols]
-    uint16_t* ss = (uint16_t*)(shared + (size_t)(chunk >> 3) * cols);  // [chunk / group][16]
-    const uint32_t groups = (k + (1u << group_log) - 1) >> group_log, chunk_groups = chunk >> group_log;
-    const uint32_t col = i16 < cols ? i16 : cols - 1;                // rows of the operand behind the last column: not stored
+    const uint32_t steps = (k + kStep - 1) / kStep, groups = (k + (1u << group_log) - 1) >> group_log, all_groups = steps * kStep >> group_log;
+    v4u* xs = shared;                                                            // [k / 8][cols]
+    uint16_t* ss = (uint16_t*)(shared + (STAGED ? (size_t)steps * (kStep / 8) * cols : 0));  // [group][16]
+    const uint32_t col = i16 < cols ? i16 : cols - 1;                            // rows of the operand behind the last column: not stored
 
-    const uint32_t out = n0 + i16 < n ? n0 + i16 : n - 1;
-    const uint8_t* wrow = codes + (size_t)out * (k >> 1) + g * 16;
-    const uint32_t steps = (k + kStep - 1) / kStep;
-    auto fetch = [&](uint32_t j) -> v4u {
-        if (j < steps && j * kStep + g * 32 < k) return __builtin_nontemporal_load((const v4u*)(wrow + (size_t)j * (kStep / 2)));
-        return v4u{0, 0, 0, 0};
-    };
-    constexpr int ahead = 4;
-    v4u w[ahead];
+    // Loads come back in the order they were asked for: what is waited for first comes first.
+    constexpr int early = 4;
+    uint16_t sc[early];
+    const uint32_t out = n0 + (tid & 15) < n ? n0 + (tid & 15) : n - 1;
 #pragma unroll
-    for (int p = 0; p < ahead; ++p) w[p] = fetch(wave + p * kWaves);
+    for (int i = 0; i < early; ++i) {
+        const uint32_t at = (tid >> 4) + 32 * i;
+        sc[i] = scales[(size_t)out * groups + (at < groups ? at : groups - 1)];
+    }
+    constexpr int pieces = STAGED ? Pieces<DT>::most : 1;
+    Eight<DT> raw[pieces];
+    const uint32_t across = threads_across(vectors), first = tid & (across - 1), rounds = (steps * (kStep / 8) + across - 1) / across;
+    if constexpr (STAGED) {
+        uint32_t a = 0, m = tid / across;
+#pragma unroll
+        for (int p = 0; p < pieces; ++p) {
+            const uint32_t at = 8 * (first + across * a);
+            raw[p] = Eight<DT>{};
+            if (m < vectors && at < k) raw[p] = load_eight<DT>(x, (m0 + m) * xstride + at);
+            if (++a == rounds) {
+                a = 0;
+                m += 512 / across;
+            }
+        }
+    }
+    const Row row = row_of(codes, n, k, n0 + i16, g);
+    constexpr int ahead = STAGED ? 4 : 2;
+    v4u w[ahead], xa[ahead][4];
+    const v4u* xat = xf + (size_t)blockIdx.y * steps * (kStep / 8) * 16 + lane;
+    auto fetch_x = [&](uint32_t j, v4u(&to)[4]) {
+        const uint32_t there = j < steps ? j : 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) to[q] = xat[(size_t)there * 256 + q * 64];
+    };
+#pragma unroll
+    for (int p = 0; p < ahead; ++p) {
+        w[p] = fetch(row, wave + p * kWaves);
+        if constexpr (!STAGED) fetch_x(wave + p * kWaves, xa[p]);
+    }
+#pragma unroll
+    for (int i = 0; i < early; ++i) {
+        const uint32_t at = (tid >> 4) + 32 * i;
+        if (at < all_groups) ss[at * 16 + (tid & 15)] = at < groups ? sc[i] : (uint16_t)0;
+    }
+    for (uint32_t at = (tid >> 4) + 32 * early; at < all_groups; at += 32)
+        ss[at * 16 + (tid & 15)] = at < groups ? scales[(size_t)out * groups + at] : (uint16_t)0;
+    if constexpr (STAGED) {
+        uint32_t a = 0, m = tid / across;
+#pragma unroll
+        for (int p = 0; p < pieces; ++p) {
+            const uint32_t k8 = first + across * a;
+            if (m < vectors && k8 < steps * (kStep / 8)) {
+                v4u c[parts];
+                columns_of<DT>(raw[p], c);
+#pragma unroll
+                for (int q = 0; q < parts; ++q) xs[k8 * cols + m * parts + q] = c[q];
+            }
+            if (++a == rounds) {
+                a = 0;
+                m += 512 / across;
+            }
+        }
+    }
+    __syncthreads();
 
     v4f total = {0, 0, 0, 0};
     int64_t itotal[2] = {0, 0};
     const uint32_t minus12 = Kind<DT>::f16 ? 0xca00ca00u : 0xc140c140u;
-    for (uint32_t k0 = 0; k0 < k; k0 += chunk) {
-        if (k0) __syncthreads();
-        for (uint32_t t = tid; t < (chunk >> 3) * vectors; t += kWaves * 64) {
-            const uint32_t k8 = t % (chunk >> 3), m = t / (chunk >> 3);
-            v4u c[parts];
+    const v4u back = {minus12, minus12, minus12, minus12};
+    auto add_group = [&](const v4f& acc, uint32_t group) {
+        const uint32_t s = ss[group * 16 + i16];
+        if constexpr (DT == ZK_I16) {
 #pragma unroll
-            for (int p = 0; p < parts; ++p) c[p] = v4u{0, 0, 0, 0};
-            if (k0 + k8 * 8 < k) columns_of<DT>(x, (m0 + m) * xstride + k0 + k8 * 8, c);
-#pragma unroll
-            for (int p = 0; p < parts; ++p) xs[k8 * cols + m * parts + p] = c[p];
+            for (int v = 0; v < 2; ++v) itotal[v] += (int64_t)((int)(acc[2 * v] * 2.0f) * 256 + (int)(acc[2 * v + 1] * 2.0f)) * (int64_t)s;
+        } else {
+            total += acc * (float)s;
         }
-        for (uint32_t t = tid; t < chunk_groups * 16; t += kWaves * 64) {
-            const uint32_t gr = t % chunk_groups, o = t / chunk_groups, at = (k0 >> group_log) + gr;
-            ss[gr * 16 + o] = at < groups && n0 + o < n ? scales[(size_t)(n0 + o) * groups + at] : (uint16_t)0;
-        }
-        __syncthreads();
-        const uint32_t last = (k0 + chunk < k ? k0 + chunk : k);
+    };
 #pragma unroll 4
-        for (uint32_t j = k0 / kStep + wave; j * kStep < last; j += kWaves) {
-            v4u r = w[0];
+    for (uint32_t j = wave; j < steps; j += kWaves) {
+        v4u r = w[0], a[4];
+        if constexpr (STAGED) {
+            const v4u* at = xs + (j * (kStep / 8) + g) * cols + col;
 #pragma unroll
-            for (int p = 0; p + 1 < ahead; ++p) w[p] = w[p + 1];
-            w[ahead - 1] = fetch(j + ahead * kWaves);
-            transpose_rows(r);
-            const uint32_t kk = j * kStep - k0;
-            v4f acc = {0, 0, 0, 0};
+            for (int q = 0; q < 4; ++q) a[q] = at[q * 4 * cols];
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) a[q] = xa[0][q];
+        }
+#pragma unroll
+        for (int p = 0; p + 1 < ahead; ++p) {
+            w[p] = w[p + 1];
+            if constexpr (!STAGED)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) xa[p][q] = xa[p + 1][q];
+        }
+        w[ahead - 1] = fetch(row, j + ahead * kWaves);
+        if constexpr (!STAGED) fetch_x(j + ahead * kWaves, xa[ahead - 1]);
+        transpose_rows(r);
+        // two halves of a step side by side: their instructions do not wait for each other
+        v4f acc[2];
+        const uint32_t gr = j * kStep >> group_log;
+        if (group_log == 5) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4u a = xs[((kk >> 3) + q * 4 + g) * cols + col];
-                acc = product<DT>(a, v4u{minus12, minus12, minus12, minus12}, acc);
-                acc = product<DT>(a, widen<DT>(r[q]), acc);
-                if (q == 3 || (q & 1 && group_log <= 6) || group_log == 5) {
-                    const uint32_t s = ss[((kk + q * 32) >> group_log) * 16 + i16];
-                    if constexpr (DT == ZK_I16) {
+                const v4f p = product<DT>(a[q], widen<DT>(r[q]), product<DT>(a[q], back, v4f{0, 0, 0, 0}));
+                add_group(p, gr + q);
+            }
+        } else {
 #pragma unroll
-                        for (int v = 0; v < 2; ++v)
-                            itotal[v] += (int64_t)((int)(acc[2 * v] * 2.0f) * 256 + (int)(acc[2 * v + 1] * 2.0f)) * (int64_t)s;
-                    } else {
-                        total += acc * (float)s;
-                    }
-                    acc = v4f{0, 0, 0, 0};
-                }
+            for (int f = 0; f < 2; ++f) {
+                acc[f] = product<DT>(a[2 * f], back, v4f{0, 0, 0, 0});
+                acc[f] = product<DT>(a[2 * f], widen<DT>(r[2 * f]), acc[f]);
+                acc[f] = product<DT>(a[2 * f + 1], back, acc[f]);
+                acc[f] = product<DT>(a[2 * f + 1], widen<DT>(r[2 * f + 1]), acc[f]);
+            }
+            if (group_log == 6) {
+                add_group(acc[0], gr);
+                add_group(acc[1], gr + 1);
+            } else {
+                add_group(acc[0] + acc[1], gr);
             }
         }
     }
@@ -203,6 +309,223 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     }
 }
 
+// x as operands: xf[block][k / 8][columns of a block], zero behind the last column and the last input (up to a step's end);
+// with sums, -12 times the sum over each group of inputs, [block][group][columns of a block].  A block has `vectors`
+// vectors.  Workgroup: one group, or eight of 16 bytes where nobody asks for sums.
+template <int DT>
+__global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, const void* x, size_t xstride, size_t rows, uint32_t k,
+                                                       uint32_t k8_all, uint32_t columns, uint32_t vectors, uint32_t group_log) {
+    constexpr int parts = Kind<DT>::parts;
+    const uint32_t block = blockIdx.y, per = sums ? 1u << (group_log - 3) : 8;  // pieces of eight inputs of a workgroup, 4, 8 or 16
+    const uint32_t sub = threadIdx.x & (per - 1), k8 = blockIdx.x * per + sub;
+    const size_t m0 = (size_t)block * vectors;
+    for (uint32_t m = threadIdx.x / per; m * parts < columns; m += kBlock / per) {
+        v4u c[parts];
+#pragma unroll
+        for (int p = 0; p < parts; ++p) c[p] = v4u{0, 0, 0, 0};
+        if (m < vectors && m0 + m < rows && k8 * 8 < k) columns_of<DT>(load_eight<DT>(x, (m0 + m) * xstride + k8 * 8), c);
+#pragma unroll
+        for (int p = 0; p < parts; ++p) {
+            const uint32_t col = m * parts + p;
+            if (col >= columns) continue;
+            if (k8 < k8_all) xf[((size_t)block * k8_all + k8) * columns + col] = c[p];
+            if (!sums) continue;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += half_of<Kind<DT>::f16 ? ZK_F16 : ZK_BF16>(c[p][i], 0) + half_of<Kind<DT>::f16 ? ZK_F16 : ZK_BF16>(c[p][i], 1);
+            for (uint32_t o = 1; o < per; o <<= 1) sum += __shfl_xor(sum, (int)o);
+            if (sub == 0) sums[((size_t)block * (k8_all / per) + blockIdx.x) * columns + col] = -12.0f * sum;
+        }
+    }
+}
+
+// ---- many columns ----------------------------------------------------------------------------------------------------
+
+// Workgroup: 64 NT outputs by 16 CT columns, chunks of two steps.  Wavefront w: outputs 16 NT (w mod 4) .., step w / 4 of a
+// chunk.  Operands and sums come from k_w4_columns into LDS, one chunk ahead.
+template <int CT, int NT>
+struct ManyLds {
+    static constexpr uint32_t C = 16 * CT, N = 64 * NT, x = 32 * C * 16, sums = 8 * C * 4, scales = 8 * N * 2, bytes = x + sums + scales;
+    static constexpr uint32_t meet = 4 * NT * CT * 64 * 16;  // also the outputs, C * N floats
+    static constexpr uint32_t all = 2 * bytes > meet ? 2 * bytes : meet;
+};
+template <int DT, int CT, int NT>
+__global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, size_t rows, const uint8_t* codes,
+                                                 const uint16_t* scales, uint32_t n, uint32_t k, uint32_t group_log, uint32_t vectors,
+                                                 float unit2) {
+    using L = ManyLds<CT, NT>;
+    constexpr uint32_t C = L::C, N = L::N;
+    extern __shared__ v4u shared[];
+    char* lds = (char*)shared;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15, nw = wave & 3, kw = wave >> 2;
+    const uint32_t n0 = blockIdx.x * N, block = blockIdx.y;
+    const uint32_t steps = (k + kStep - 1) / kStep, k8_all = steps * (kStep / 8), chunks = (steps + 1) / 2;
+    const uint32_t groups = (k + (1u << group_log) - 1) >> group_log, all_groups = k8_all >> (group_log - 3), each = 256u >> group_log;
+
+    v4u xr[CT];
+    float br[2];
+    uint16_t sr[2 * NT];
+    auto ask = [&](uint32_t chunk) {
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            const uint32_t p = tid + 512 * i, k8 = chunk * 32 + p / C;
+            xr[i] = v4u{0, 0, 0, 0};
+            if (k8 < k8_all) xr[i] = xf[((size_t)block * k8_all + k8) * C + p % C];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t p = tid + 512 * i, gr = chunk * each + p / C;
+            br[i] = 0.0f;
+            if (p < each * C && gr < all_groups) br[i] = sums[((size_t)block * all_groups + gr) * C + p % C];
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const uint32_t p = tid + 512 * i, gr = chunk * each + p / N, o = n0 + p % N;
+            sr[i] = 0;
+            if (p < each * N && gr < groups && o < n) sr[i] = scales[(size_t)o * groups + gr];
+        }
+    };
+    auto put = [&](uint32_t buf) {
+        char* at = lds + buf * L::bytes;
+#pragma unroll
+        for (int i = 0; i < CT; ++i) ((v4u*)at)[tid + 512 * i] = xr[i];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (tid + 512 * i < each * C) ((float*)(at + L::x))[tid + 512 * i] = br[i];
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            if (tid + 512 * i < each * N) ((uint16_t*)(at + L::x + L::sums))[tid + 512 * i] = sr[i];
+    };
+    Row row[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) row[t] = row_of(codes, n, k, n0 + (nw * NT + t) * 16 + i16, g);
+    v4u w[2][NT];
+    ask(0);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w[p][t] = fetch(row[t], kw + 2 * p);
+
+    v4f total[NT][CT];
+    int64_t itotal[NT][CT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            total[t][c] = v4f{0, 0, 0, 0};
+            itotal[t][c][0] = itotal[t][c][1] = 0;
+        }
+    for (uint32_t chunk = 0; chunk < chunks; ++chunk) {
+        const uint32_t buf = chunk & 1;
+        put(buf);
+        __syncthreads();
+        if (chunk + 1 < chunks) ask(chunk + 1);
+        v4u r[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            r[t] = w[0][t];
+            w[0][t] = w[1][t];
+            w[1][t] = fetch(row[t], (chunk + 2) * 2 + kw);
+            transpose_rows(r[t]);
+        }
+        const char* at = lds + buf * L::bytes;
+        const v4u* xs = (const v4u*)at + (kw * 16 + g) * C + i16;
+        const float* bs = (const float*)(at + L::x) + 4 * g;
+        const uint16_t* ss = (const uint16_t*)(at + L::x + L::sums) + nw * 16 * NT + i16;
+        v4f acc[NT][CT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[t][c] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v4u f[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) f[t] = widen<DT>(r[t][q]);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const v4u a = xs[q * 4 * C + 16 * c];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t][c] = product<DT>(a, f[t], acc[t][c]);
+            }
+            if (q == 3 || (q & 1 && group_log <= 6) || group_log == 5) {
+                const uint32_t gr = (kw * kStep + q * 32) >> group_log;
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const v4f b = *(const v4f*)(bs + gr * C + 16 * c);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint32_t s = ss[gr * N + 16 * t];
+                        const v4f whole = acc[t][c] + b;
+                        if constexpr (DT == ZK_I16) {
+#pragma unroll
+                            for (int v = 0; v < 2; ++v)
+                                itotal[t][c][v] += (int64_t)((int)(whole[2 * v] * 2.0f) * 256 + (int)(whole[2 * v + 1] * 2.0f)) * (int64_t)s;
+                        } else {
+                            total[t][c] += whole * (float)s;
+                        }
+                        acc[t][c] = v4f{0, 0, 0, 0};
+                    }
+                }
+            }
+        }
+    }
+
+    // the two halves of the inputs, then the columns of a vector
+    __syncthreads();
+    v4u* meet = shared + (size_t)nw * NT * CT * 64 + lane;
+    if (kw == 1)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+                meet[(t * CT + c) * 64] = DT == ZK_I16 ? __builtin_bit_cast(v4u, itotal[t][c]) : __builtin_bit_cast(v4u, total[t][c]);
+    __syncthreads();
+    const size_t m0 = (size_t)block * vectors;
+    if constexpr (DT == ZK_I16) {
+        if (kw == 0)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    struct Two {
+                        int64_t v[2];
+                    };
+                    const Two other = __builtin_bit_cast(Two, meet[(t * CT + c) * 64]);
+                    const uint32_t o = n0 + (nw * NT + t) * 16 + i16;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t m = 8 * c + 2 * g + v;
+                        if (m < vectors && m0 + m < rows && o < n) ((int64_t*)y)[(m0 + m) * ystride + o] = itotal[t][c][v] + other.v[v];
+                    }
+                }
+    } else {
+        if (kw == 0)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) total[t][c] += __builtin_bit_cast(v4f, meet[(t * CT + c) * 64]);
+        __syncthreads();
+        float* tile = (float*)shared;  // [column][output]
+        if (kw == 0)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) tile[(16 * c + 4 * g + e) * N + (nw * NT + t) * 16 + i16] = total[t][c][e];
+        __syncthreads();
+        for (uint32_t i = tid; i < vectors * N; i += 512) {
+            const uint32_t m = i / N, o = i % N;
+            if (m0 + m >= rows || n0 + o >= n) continue;
+            float sum = 0.0f;
+#pragma unroll
+            for (int p = 0; p < Kind<DT>::parts; ++p) sum += tile[(m * Kind<DT>::parts + p) * N + o];
+            store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
+        }
+    }
+}
+
 __global__ __launch_bounds__(kBlock) void k_w4_expand(int16_t* W, const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
                                                       uint32_t group_log) {
     // a thread: one output, eight inputs; consecutive threads are consecutive outputs, whose entries lie side by side in W
@@ -217,29 +540,106 @@ __global__ __launch_bounds__(kBlock) void k_w4_expand(int16_t* W, const uint8_t*
     }
 }
 
+// How a call goes: its columns in blocks, and how x gets to them.
+struct Way {
+    bool staged;                // few columns, x in LDS
+    uint32_t blocks, vectors;   // of columns, and the vectors of each
+    uint32_t tiles;             // of 16 columns of a block; 1: few columns
+    uint32_t k8;                // pieces of eight inputs, whole steps
+    size_t operands, sums;      // in the workspace, bytes
+};
 template <int DT>
-int run(void* y, size_t ystride, const void* x, size_t xstride, size_t rows, const uint8_t* codes, const uint16_t* scales, uint32_t n,
-        uint32_t k, uint32_t group_log, float unit, hipStream_t stream) {
-    constexpr int vectors = Kind<DT>::vectors, parts = Kind<DT>::parts;
-    const uint32_t cols = (uint32_t)(rows < (size_t)vectors ? rows : vectors) * parts;
-    uint32_t chunk = kStageHalves / cols / (kStep * kWaves) * (kStep * kWaves);  // at most 16 columns: at least one step each
-    const uint32_t whole = (uint32_t)align_up(k, kStep * kWaves);
-    if (chunk > whole) chunk = whole;
-    size_t lds = (size_t)(chunk >> 3) * cols * 16 + (size_t)(chunk >> group_log) * 32;
-    if (lds < 8192) lds = 8192;  // the sums at the end
-    for (size_t r0 = 0; r0 < rows; r0 += (size_t)65535 * vectors) {  // the grid's second dimension ends there
-        const size_t r = rows - r0 < (size_t)65535 * vectors ? rows - r0 : (size_t)65535 * vectors;
-        hipLaunchKernelGGL((k_w4_few<DT>), dim3((unsigned)div_up(n, 16), (unsigned)div_up(r, vectors)), dim3(kWaves * 64), lds, stream,
-                           (char*)y + r0 * ystride * (DT == ZK_I16 ? 8 : dtype_bytes(DT)), ystride,
-                           (const char*)x + r0 * xstride * dtype_bytes(DT), xstride, r, codes, scales, n, k, group_log, chunk, unit * 2.0f);
+Way way_of(size_t rows, uint32_t k) {
+    constexpr uint32_t parts = Kind<DT>::parts;
+    Way w = {};
+    w.k8 = (uint32_t)align_up(k, kStep) / 8;
+    if (rows <= (size_t)Kind<DT>::vectors) {
+        const uint32_t v = (uint32_t)rows, across = threads_across(v);
+        w.blocks = w.tiles = 1;
+        w.vectors = Kind<DT>::vectors;
+        w.staged = (size_t)w.k8 * 8 * v * parts <= kStageHalves && div_up(w.k8, across) * div_up(v, 512 / across) <= (size_t)Pieces<DT>::most;
+    } else {
+        // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
+        const size_t most = 96 / parts;
+        const size_t blocks = div_up(rows, most), v = div_up(rows, blocks);
+        w.tiles = v * parts <= 32 ? 2 : v * parts <= 64 ? 4 : 6;
+        w.vectors = (uint32_t)v;
+        w.blocks = (uint32_t)div_up(rows, v);
     }
+    if (!w.staged) w.operands = (size_t)w.blocks * w.k8 * w.tiles * 256;
+    if (w.tiles > 1) w.sums = (size_t)w.blocks * (w.k8 / 4) * w.tiles * 64;  // of the shortest groups
+    return w;
+}
+size_t way_bytes(const Way& w) {
+    Carver cv(nullptr, 0);
+    cv.take(w.operands);
+    cv.take(w.sums);
+    return w.operands ? cv.used() : 0;
+}
+
+struct Call {
+    void* y;
+    size_t ystride;
+    const void* x;
+    size_t xstride, rows;
+    const uint8_t* codes;
+    const uint16_t* scales;
+    uint32_t n, k, group_log;
+    float unit;
+    void* ws;
+    size_t ws_bytes;
+    hipStream_t stream;
+};
+
+template <int DT, int CT, int NT>
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    const size_t lds = ManyLds<CT, NT>::all;
+    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_w4_many<DT, CT, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_w4_many<DT, CT, NT>), dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf,
+                       sums, c.rows, c.codes, c.scales, c.n, c.k, c.group_log, w.vectors, c.unit * 2.0f);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
+template <int DT, int CT>
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums) : run_many<DT, CT, 1>(c, w, xf, sums);
+}
 
+template <int DT>
+int run(const Call& c) {
+    const Way w = way_of<DT>(c.rows, c.k);
+    v4u* xf = nullptr;
+    float* sums = nullptr;
+    if (w.operands) {
+        if (!c.ws) return ZK_E_BUFSZ;
+        Carver cv(c.ws, c.ws_bytes);
+        xf = (v4u*)cv.take(w.operands);
+        if (w.sums) sums = (float*)cv.take(w.sums);
+        if (cv.overflow() || !xf || (w.sums && !sums)) return ZK_E_BUFSZ;
+        const uint32_t per = sums ? 1u << (c.group_log - 3) : 8;
+        hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, c.x, c.xstride,
+                           c.rows, c.k, w.k8, w.tiles * 16, w.vectors, c.group_log);
+        ZK_HIP_TRY(hipGetLastError());
+    }
+    if (w.tiles == 1) {
+        const uint32_t cols = (uint32_t)c.rows * Kind<DT>::parts;
+        size_t lds = (w.staged ? (size_t)w.k8 * cols * 16 : 0) + (size_t)(w.k8 >> (c.group_log - 3)) * 32;
+        if (lds < 8192) lds = 8192;  // the sums at the end
+        const dim3 grid((unsigned)div_up(c.n, 16), 1);
+        auto* kernel = w.staged ? k_w4_few<DT, true> : k_w4_few<DT, false>;
+        if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, c.rows, c.codes, c.scales, c.n,
+                           c.k, c.group_log, c.unit * 2.0f);
+        ZK_HIP_TRY(hipGetLastError());
+        return ZK_OK;
+    }
+    return w.tiles == 2 ? run_many<DT, 2>(c, w, xf, sums) : w.tiles == 4 ? run_many<DT, 4>(c, w, xf, sums) : run_many<DT, 6>(c, w, xf, sums);
+}
+
+bool inputs_ok(size_t k) { return k >= 32 && k <= ((size_t)1 << 20) && k % 32 == 0; }
 bool weights_ok(const uint8_t* codes, const uint16_t* scales, size_t n, size_t k, uint32_t group) {
-    return codes && scales && aligned(codes, 16) && aligned(scales, 2) && n >= 1 && n <= ((size_t)1 << 24) && k >= 32 &&
-           k <= ((size_t)1 << 24) && k % 32 == 0 && (group == 32 || group == 64 || group == 128);
+    return codes && scales && aligned(codes, 16) && aligned(scales, 2) && n >= 1 && n <= ((size_t)1 << 24) && inputs_ok(k) &&
+           (group == 32 || group == 64 || group == 128);
 }
 
 }  // namespace
@@ -248,28 +648,29 @@ bool weights_ok(const uint8_t* codes, const uint16_t* scales, size_t n, size_t k
 using namespace zkmi;
 
 extern "C" size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k) {
-    (void)dtype;
-    (void)rows;
-    (void)k;
-    return 0;
+    if (!dtype_bytes(dtype) || rows == 0 || rows > kMostRows || !inputs_ok(k)) return 0;
+    switch (dtype) {
+        case ZK_F32: return way_bytes(way_of<ZK_F32>(rows, (uint32_t)k));
+        case ZK_F16: return way_bytes(way_of<ZK_F16>(rows, (uint32_t)k));
+        case ZK_BF16: return way_bytes(way_of<ZK_BF16>(rows, (uint32_t)k));
+        default: return way_bytes(way_of<ZK_I16>(rows, (uint32_t)k));
+    }
 }
 
 extern "C" int w4_matvec(void* y, size_t y_row_stride, const void* x, size_t x_row_stride, int dtype, size_t rows, const uint8_t* codes,
                          const uint16_t* scales, size_t n, size_t k, uint32_t group, float unit, void* ws, size_t ws_bytes, void* stream) {
-    (void)ws;
-    (void)ws_bytes;
     const size_t size = dtype_bytes(dtype);
-    if (!size || !weights_ok(codes, scales, n, k, group)) return ZK_E_BADARG;
+    if (!size || !weights_ok(codes, scales, n, k, group) || rows > kMostRows) return ZK_E_BADARG;
     if (rows == 0) return ZK_OK;
     if (!x || !y || !aligned(x, 16) || !aligned(y, dtype == ZK_I16 ? 8 : size)) return ZK_E_BADARG;
     if (rows > 1 && (x_row_stride < k || y_row_stride < n || x_row_stride * size % 16)) return ZK_E_BADARG;
-    const uint32_t gl = group == 32 ? 5 : group == 64 ? 6 : 7;
-    hipStream_t s = as_stream(stream);
+    const Call c = {y, y_row_stride, x, x_row_stride, rows, codes, scales, (uint32_t)n, (uint32_t)k, group == 32 ? 5u : group == 64 ? 6u : 7u,
+                    unit, ws, ws_bytes, as_stream(stream)};
     switch (dtype) {
-        case ZK_F32: return run<ZK_F32>(y, y_row_stride, x, x_row_stride, rows, codes, scales, (uint32_t)n, (uint32_t)k, gl, unit, s);
-        case ZK_F16: return run<ZK_F16>(y, y_row_stride, x, x_row_stride, rows, codes, scales, (uint32_t)n, (uint32_t)k, gl, unit, s);
-        case ZK_BF16: return run<ZK_BF16>(y, y_row_stride, x, x_row_stride, rows, codes, scales, (uint32_t)n, (uint32_t)k, gl, unit, s);
-        default: return run<ZK_I16>(y, y_row_stride, x, x_row_stride, rows, codes, scales, (uint32_t)n, (uint32_t)k, gl, unit, s);
+        case ZK_F32: return run<ZK_F32>(c);
+        case ZK_F16: return run<ZK_F16>(c);
+        case ZK_BF16: return run<ZK_BF16>(c);
+        default: return run<ZK_I16>(c);
     }
 }
 
