@@ -107,22 +107,17 @@ __device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<D
     }
 }
 
-// Where a lane finds its output's weights: 16 bytes (32 inputs) of every step.
+// Where a lane finds its output's weights: 16 bytes (32 inputs) of every step, of `last` + 1 steps.  Behind the last input
+// any weights will do, x is 0 there: the lane's last ones, or the output's first if it has none.
 struct Row {
     const uint8_t* at;
-    uint32_t whole;  // steps whose 128 inputs are all there
-    bool tail;              // whether the lane has inputs in the last step, if that is not whole
+    uint32_t last;
 };
 __device__ __forceinline__ Row row_of(const uint8_t* codes, uint32_t n, uint32_t k, uint32_t out, uint32_t g) {
-    Row w = {codes + (size_t)(out < n ? out : n - 1) * (k >> 1), k / kStep, g * 32 < k % kStep};
-    if (w.whole || w.tail) w.at += g * 16;
-    return w;
+    const uint32_t mine = k / kStep + (g * 32 < k % kStep ? 1 : 0);
+    return Row{codes + (size_t)(out < n ? out : n - 1) * (k >> 1) + (mine ? g * 16 : 0), mine ? mine - 1 : 0};
 }
-// Behind the last input any weights will do, x is 0 there: the first ones.
-__device__ __forceinline__ v4u fetch(const Row& w, uint32_t j) {
-    const bool there = j < w.whole || (w.tail && j == w.whole);
-    return *(const v4u*)(w.at + (there ? (size_t)j * (kStep / 2) : 0));
-}
+__device__ __forceinline__ v4u fetch(const Row& w, uint32_t j) { return *(const v4u*)(w.at + (size_t)((j < w.last ? j : w.last) * (kStep / 2))); }
 
 // ---- few columns -----------------------------------------------------------------------------------------------------
 
@@ -136,11 +131,12 @@ struct Pieces {
 // Workgroup: 16 outputs, up to 16 columns; its eight wavefronts share out the steps and add up at the end.  x comes from
 // LDS where all of it fits there (STAGED), else from `xf`, where k_w4_columns has laid out the operands [k / 8][16]: a
 // wavefront then reads a kilobyte of them for each instruction, out of the L2, and nothing waits for anything in the loop.
-template <int DT, bool STAGED>
+template <int DT, bool STAGED, int GL>
 __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, size_t rows,
                                                         const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
-                                                        uint32_t group_log, float unit2) {
+                                                        float unit2) {
     constexpr int parts = Kind<DT>::parts;
+    constexpr uint32_t group_log = GL;
     extern __shared__ v4u shared[];
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15;
     const uint32_t n0 = blockIdx.x * 16;
@@ -164,10 +160,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     constexpr int pieces = STAGED ? Pieces<DT>::most : 1;
     Eight<DT> raw[pieces];
     const uint32_t across = threads_across(vectors), first = tid & (across - 1), rounds = (steps * (kStep / 8) + across - 1) / across;
+    const int need = (int)(rounds * ((vectors + 512 / across - 1) / (512 / across)));
     if constexpr (STAGED) {
         uint32_t a = 0, m = tid / across;
 #pragma unroll
         for (int p = 0; p < pieces; ++p) {
+            if (p >= need) break;
             const uint32_t at = 8 * (first + across * a);
             raw[p] = Eight<DT>{};
             if (m < vectors && at < k) raw[p] = load_eight<DT>(x, (m0 + m) * xstride + at);
@@ -202,6 +200,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
         uint32_t a = 0, m = tid / across;
 #pragma unroll
         for (int p = 0; p < pieces; ++p) {
+            if (p >= need) break;
             const uint32_t k8 = first + across * a;
             if (m < vectors && k8 < steps * (kStep / 8)) {
                 v4u c[parts];
@@ -230,26 +229,18 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
             total += acc * (float)s;
         }
     };
-#pragma unroll 4
-    for (uint32_t j = wave; j < steps; j += kWaves) {
-        v4u r = w[0], a[4];
+    auto step = [&](uint32_t j, v4u& wr, v4u(&xr)[4]) {
+        v4u r = wr, a[4];
         if constexpr (STAGED) {
             const v4u* at = xs + (j * (kStep / 8) + g) * cols + col;
 #pragma unroll
             for (int q = 0; q < 4; ++q) a[q] = at[q * 4 * cols];
         } else {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) a[q] = xa[0][q];
+            for (int q = 0; q < 4; ++q) a[q] = xr[q];
         }
-#pragma unroll
-        for (int p = 0; p + 1 < ahead; ++p) {
-            w[p] = w[p + 1];
-            if constexpr (!STAGED)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) xa[p][q] = xa[p + 1][q];
-        }
-        w[ahead - 1] = fetch(row, j + ahead * kWaves);
-        if constexpr (!STAGED) fetch_x(j + ahead * kWaves, xa[ahead - 1]);
+        wr = fetch(row, j + ahead * kWaves);
+        if constexpr (!STAGED) fetch_x(j + ahead * kWaves, xr);
         transpose_rows(r);
         // two halves of a step side by side: their instructions do not wait for each other
         v4f acc[2];
@@ -275,7 +266,14 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
                 add_group(acc[0] + acc[1], gr);
             }
         }
-    }
+    };
+    uint32_t j = wave;
+    for (; j + (ahead - 1) * kWaves < steps; j += ahead * kWaves)
+#pragma unroll
+        for (int p = 0; p < ahead; ++p) step(j + p * kWaves, w[p], xa[p]);
+#pragma unroll
+    for (int p = 0; p < ahead - 1; ++p)
+        if (j + p * kWaves < steps) step(j + p * kWaves, w[p], xa[p]);
 
     __syncthreads();
     if constexpr (DT == ZK_I16) {
@@ -626,10 +624,11 @@ int run(const Call& c) {
         size_t lds = (w.staged ? (size_t)w.k8 * cols * 16 : 0) + (size_t)(w.k8 >> (c.group_log - 3)) * 32;
         if (lds < 8192) lds = 8192;  // the sums at the end
         const dim3 grid((unsigned)div_up(c.n, 16), 1);
-        auto* kernel = w.staged ? k_w4_few<DT, true> : k_w4_few<DT, false>;
+        auto* kernel = w.staged ? (c.group_log == 5 ? k_w4_few<DT, true, 5> : c.group_log == 6 ? k_w4_few<DT, true, 6> : k_w4_few<DT, true, 7>)
+                                : (c.group_log == 5 ? k_w4_few<DT, false, 5> : c.group_log == 6 ? k_w4_few<DT, false, 6> : k_w4_few<DT, false, 7>);
         if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, c.rows, c.codes, c.scales, c.n,
-                           c.k, c.group_log, c.unit * 2.0f);
+                           c.k, c.unit * 2.0f);
         ZK_HIP_TRY(hipGetLastError());
         return ZK_OK;
     }
