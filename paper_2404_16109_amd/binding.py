@@ -952,15 +952,13 @@ def logprobs(logits, targets=None, top=0, ws=None):
     given = targets is not None
     if given:
         assert targets.dtype == torch.int32 and targets.shape == (rows,) and targets.is_cuda and targets.is_contiguous()
-    # one allocation: six arrays of 32-bit values
-    words = torch.empty(rows * (4 + 2 * top), dtype=torch.float32, device=dev)
-    ints = words.view(torch.int32)
-    r = {"target": words[:rows] if given else None, "rank": ints[rows:2 * rows] if given else None,
-         "lse": words[2 * rows:3 * rows], "entropy": words[3 * rows:4 * rows],
-         "top_ids": ints[4 * rows:(4 + top) * rows].view(rows, top), "top": words[(4 + top) * rows:].view(rows, top)}
-    base, row = words.data_ptr(), 4 * rows
-    o = logprobs_out(base if given else None, base + row if given else None, base + 2 * row, base + 3 * row, base + 4 * row,
-                     base + (4 + top) * row)
+    target, lse, entropy = torch.empty(3, rows, dtype=torch.float32, device=dev).unbind(0)
+    rank = torch.empty(rows, dtype=torch.int32, device=dev)
+    ids, values = torch.empty(rows, top, dtype=torch.int32, device=dev), torch.empty(rows, top, dtype=torch.float32, device=dev)
+    r = {"target": target if given else None, "rank": rank if given else None, "lse": lse, "entropy": entropy, "top_ids": ids,
+         "top": values}
+    o = logprobs_out(target.data_ptr() if given else None, rank.data_ptr() if given else None, lse.data_ptr(), entropy.data_ptr(),
+                     ids.data_ptr(), values.data_ptr())
     need = _lib.logprobs_workspace_bytes(rows, vocab, top)
     if ws is None and need:
         ws = _ws(need)

@@ -11,10 +11,13 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-static const float kInf = __builtin_inff();
+#define kInf __builtin_inff()
 
 inline size_t dtype_bytes(int dtype) { return dtype == ZK_F32 ? 4 : (dtype == ZK_F16 || dtype == ZK_BF16 || dtype == ZK_I16) ? 2 : 0; }
 inline bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
+// A value that is the same in all lanes, for the compiler to know.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 
 __device__ __forceinline__ float bits_float(uint32_t b) { return __builtin_bit_cast(float, b); }
 __device__ __forceinline__ uint32_t float_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
@@ -45,6 +48,35 @@ template <int DT>
 __device__ __forceinline__ uint16_t half_bits(float f) {
     if constexpr (DT == ZK_F16) return __builtin_bit_cast(uint16_t, (_Float16)f);
     return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+
+// Over the 64 lanes of a wavefront, in every lane: moves within rows of 16 lanes, then two broadcasts from row to row, all at
+// the rate of the vector ALU (lanes_sum in reduce_dev.h has the same steps).  Lanes without a partner keep their own.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t old, uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, uint32_t none, Op op) {
+    x = op(x, from_lane<0x111, 0xf>(none, x));  // row_shr 1, 2, 4, 8: a row's last lane has the row
+    x = op(x, from_lane<0x112, 0xf>(none, x));
+    x = op(x, from_lane<0x114, 0xf>(none, x));
+    x = op(x, from_lane<0x118, 0xf>(none, x));
+    x = op(x, from_lane<0x142, 0xa>(none, x));  // row_bcast 15 into rows 1 and 3
+    x = op(x, from_lane<0x143, 0xc>(none, x));  // row_bcast 31 into rows 2 and 3
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ float wave_add(float x) {
+    return bits_float(over_wave(float_bits(x), 0u, [](uint32_t a, uint32_t b) { return float_bits(bits_float(a) + bits_float(b)); }));
+}
+__device__ __forceinline__ float wave_max(float x) {
+    return bits_float(over_wave(float_bits(x), float_bits(-kInf), [](uint32_t a, uint32_t b) { return float_bits(fmaxf(bits_float(a), bits_float(b))); }));
+}
+__device__ __forceinline__ uint32_t wave_add(uint32_t x) {
+    return over_wave(x, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    return over_wave(x, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 }  // namespace zkmi

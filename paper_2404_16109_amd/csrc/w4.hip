@@ -107,27 +107,34 @@ __device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<D
     }
 }
 
-// Where a lane finds its output's weights: 16 bytes (32 inputs) of every step, of `last` + 1 steps.  Behind the last input
-// any weights will do, x is 0 there: the lane's last ones, or the output's first if it has none.
-struct Row {
-    const uint8_t* at;
-    uint32_t last;
-};
-__device__ __forceinline__ Row row_of(const uint8_t* codes, uint32_t n, uint32_t k, uint32_t out, uint32_t g) {
-    const uint32_t mine = k / kStep + (g * 32 < k % kStep ? 1 : 0);
-    return Row{codes + (size_t)(out < n ? out : n - 1) * (k >> 1) + (mine ? g * 16 : 0), mine ? mine - 1 : 0};
+// Weights are read through a buffer descriptor of a workgroup's outputs: a load behind its end comes back as 0 and costs
+// nothing, so that loads can be asked for ahead without a branch (a branch makes the compiler wait for all of them).
+// Steps behind the last input, and outputs behind the last, read nothing that way.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void* p, size_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes < 0xffffff00u ? (int)bytes : (int)0xffffff00u, 0x00020000);
 }
-__device__ __forceinline__ v4u fetch(const Row& w, uint32_t j) { return *(const v4u*)(w.at + (size_t)((j < w.last ? j : w.last) * (kStep / 2))); }
+static const uint32_t kNowhere = 0xfffffff0u;
+__device__ __forceinline__ v4u load16(Buffer b, uint32_t at) { return __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, 0)); }
+
+// Where a lane finds the weights of an output: 16 bytes (32 inputs) of each of its steps.
+struct Row {
+    uint32_t at, steps;
+};
+__device__ __forceinline__ Row row_of(uint32_t out, uint32_t k, uint32_t g) {
+    return Row{out * (k >> 1) + g * 16, k / kStep + (g * 32 < k % kStep ? 1 : 0)};
+}
+__device__ __forceinline__ v4u fetch(Buffer b, const Row& w, uint32_t j) { return load16(b, j < w.steps ? w.at + j * (kStep / 2) : kNowhere); }
+// A workgroup's weights, from output n0 on.
+__device__ __forceinline__ Buffer weights_of(const uint8_t* codes, uint32_t n, uint32_t k, uint32_t n0, uint32_t outputs) {
+    const uint32_t there = n - n0 < outputs ? n - n0 : outputs;
+    return buffer_of(codes + (size_t)n0 * (k >> 1), (size_t)there * (k >> 1));
+}
 
 // ---- few columns -----------------------------------------------------------------------------------------------------
 
 // How a workgroup of 512 brings x into LDS: `across` threads to a vector, each eight inputs at a time.
 __host__ __device__ __forceinline__ uint32_t threads_across(uint32_t vectors) { return vectors == 1 ? 512 : vectors == 2 ? 256 : 128; }
-template <int DT>
-struct Pieces {
-    static constexpr int most = DT == ZK_F32 ? 4 : 8;  // of eight inputs, held by a thread
-};
-
 // Workgroup: 16 outputs, up to 16 columns; its eight wavefronts share out the steps and add up at the end.  x comes from
 // LDS where all of it fits there (STAGED), else from `xf`, where k_w4_columns has laid out the operands [k / 8][16]: a
 // wavefront then reads a kilobyte of them for each instruction, out of the L2, and nothing waits for anything in the loop.
@@ -138,7 +145,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     constexpr int parts = Kind<DT>::parts;
     constexpr uint32_t group_log = GL;
     extern __shared__ v4u shared[];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, i16 = lane & 15;
     const uint32_t n0 = blockIdx.x * 16;
     const size_t m0 = (size_t)blockIdx.y * Kind<DT>::vectors;
     const uint32_t vectors = rows - m0 < (size_t)Kind<DT>::vectors ? (uint32_t)(rows - m0) : Kind<DT>::vectors;
@@ -157,36 +164,44 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
         const uint32_t at = (tid >> 4) + 32 * i;
         sc[i] = scales[(size_t)out * groups + (at < groups ? at : groups - 1)];
     }
-    constexpr int pieces = STAGED ? Pieces<DT>::most : 1;
-    Eight<DT> raw[pieces];
-    const uint32_t across = threads_across(vectors), first = tid & (across - 1), rounds = (steps * (kStep / 8) + across - 1) / across;
-    const int need = (int)(rounds * ((vectors + 512 / across - 1) / (512 / across)));
+    // Pieces of x, of eight inputs: the thread's first two are asked for before the weights, others (of several vectors, or
+    // long ones) when those are stored.
+    const uint32_t across = threads_across(vectors), first = tid & (across - 1), apart = 512 / across;
+    const uint32_t rounds = (steps * (kStep / 8) + across - 1) / across, need = rounds * ((vectors + apart - 1) / apart);
+    struct Place {
+        uint32_t k8, m;
+    };
+    auto place = [&](uint32_t p) -> Place { return {first + across * (p % rounds), tid / across + apart * (p / rounds)}; };
+    auto ask = [&](uint32_t p) -> Eight<DT> {
+        const Place at = place(p);
+        if (p < need && at.m < vectors && at.k8 * 8 < k) return load_eight<DT>(x, (m0 + at.m) * xstride + at.k8 * 8);
+        return Eight<DT>{};
+    };
+    auto keep = [&](uint32_t p, const Eight<DT>& raw) {
+        const Place at = place(p);
+        if (p >= need || at.m >= vectors || at.k8 >= steps * (kStep / 8)) return;
+        v4u c[parts];
+        columns_of<DT>(raw, c);
+#pragma unroll
+        for (int q = 0; q < parts; ++q) xs[at.k8 * cols + at.m * parts + q] = c[q];
+    };
+    Eight<DT> raw[2];
     if constexpr (STAGED) {
-        uint32_t a = 0, m = tid / across;
-#pragma unroll
-        for (int p = 0; p < pieces; ++p) {
-            if (p >= need) break;
-            const uint32_t at = 8 * (first + across * a);
-            raw[p] = Eight<DT>{};
-            if (m < vectors && at < k) raw[p] = load_eight<DT>(x, (m0 + m) * xstride + at);
-            if (++a == rounds) {
-                a = 0;
-                m += 512 / across;
-            }
-        }
+        raw[0] = ask(0);
+        raw[1] = ask(1);
     }
-    const Row row = row_of(codes, n, k, n0 + i16, g);
-    constexpr int ahead = STAGED ? 4 : 2;
+    const Row row = row_of(i16, k, g);
+    const Buffer weights = weights_of(codes, n, k, n0, 16);
+    constexpr int ahead = STAGED ? 3 : 2;
     v4u w[ahead], xa[ahead][4];
-    const v4u* xat = xf + (size_t)blockIdx.y * steps * (kStep / 8) * 16 + lane;
+    const Buffer operands = buffer_of(xf, STAGED ? 0 : (size_t)steps * 4096);
     auto fetch_x = [&](uint32_t j, v4u(&to)[4]) {
-        const uint32_t there = j < steps ? j : 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) to[q] = xat[(size_t)there * 256 + q * 64];
+        for (int q = 0; q < 4; ++q) to[q] = load16(operands, j * 4096 + q * 1024 + lane * 16);
     };
 #pragma unroll
     for (int p = 0; p < ahead; ++p) {
-        w[p] = fetch(row, wave + p * kWaves);
+        w[p] = fetch(weights, row, wave + p * kWaves);
         if constexpr (!STAGED) fetch_x(wave + p * kWaves, xa[p]);
     }
 #pragma unroll
@@ -197,21 +212,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     for (uint32_t at = (tid >> 4) + 32 * early; at < all_groups; at += 32)
         ss[at * 16 + (tid & 15)] = at < groups ? scales[(size_t)out * groups + at] : (uint16_t)0;
     if constexpr (STAGED) {
-        uint32_t a = 0, m = tid / across;
-#pragma unroll
-        for (int p = 0; p < pieces; ++p) {
-            if (p >= need) break;
-            const uint32_t k8 = first + across * a;
-            if (m < vectors && k8 < steps * (kStep / 8)) {
-                v4u c[parts];
-                columns_of<DT>(raw[p], c);
-#pragma unroll
-                for (int q = 0; q < parts; ++q) xs[k8 * cols + m * parts + q] = c[q];
-            }
-            if (++a == rounds) {
-                a = 0;
-                m += 512 / across;
-            }
+        keep(0, raw[0]);
+        keep(1, raw[1]);
+        for (uint32_t p = 2; p < need; p += 2) {
+            const Eight<DT> r0 = ask(p), r1 = ask(p + 1);
+            keep(p, r0);
+            keep(p + 1, r1);
         }
     }
     __syncthreads();
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
 #pragma unroll
             for (int q = 0; q < 4; ++q) a[q] = xr[q];
         }
-        wr = fetch(row, j + ahead * kWaves);
+        wr = fetch(weights, row, j + ahead * kWaves);
         if constexpr (!STAGED) fetch_x(j + ahead * kWaves, xr);
         transpose_rows(r);
         // two halves of a step side by side: their instructions do not wait for each other
@@ -355,7 +361,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
     constexpr uint32_t C = L::C, N = L::N;
     extern __shared__ v4u shared[];
     char* lds = (char*)shared;
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15, nw = wave & 3, kw = wave >> 2;
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, i16 = lane & 15, nw = wave & 3, kw = wave >> 2;
     const uint32_t n0 = blockIdx.x * N, block = blockIdx.y;
     const uint32_t steps = (k + kStep - 1) / kStep, k8_all = steps * (kStep / 8), chunks = (steps + 1) / 2;
     const uint32_t groups = (k + (1u << group_log) - 1) >> group_log, all_groups = k8_all >> (group_log - 3), each = 256u >> group_log;
@@ -396,13 +402,14 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
     };
     Row row[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) row[t] = row_of(codes, n, k, n0 + (nw * NT + t) * 16 + i16, g);
+    for (int t = 0; t < NT; ++t) row[t] = row_of((nw * NT + t) * 16 + i16, k, g);
+    const Buffer weights = weights_of(codes, n, k, n0, N);
     v4u w[2][NT];
     ask(0);
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) w[p][t] = fetch(row[t], kw + 2 * p);
+        for (int t = 0; t < NT; ++t) w[p][t] = fetch(weights, row[t], kw + 2 * p);
 
     v4f total[NT][CT];
     int64_t itotal[NT][CT][2];
@@ -423,7 +430,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
         for (int t = 0; t < NT; ++t) {
             r[t] = w[0][t];
             w[0][t] = w[1][t];
-            w[1][t] = fetch(row[t], (chunk + 2) * 2 + kw);
+            w[1][t] = fetch(weights, row[t], (chunk + 2) * 2 + kw);
             transpose_rows(r[t]);
         }
         const char* at = lds + buf * L::bytes;
@@ -552,10 +559,9 @@ Way way_of(size_t rows, uint32_t k) {
     Way w = {};
     w.k8 = (uint32_t)align_up(k, kStep) / 8;
     if (rows <= (size_t)Kind<DT>::vectors) {
-        const uint32_t v = (uint32_t)rows, across = threads_across(v);
         w.blocks = w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
-        w.staged = (size_t)w.k8 * 8 * v * parts <= kStageHalves && div_up(w.k8, across) * div_up(v, 512 / across) <= (size_t)Pieces<DT>::most;
+        w.staged = (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
     } else {
         // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
         const size_t most = 96 / parts;
