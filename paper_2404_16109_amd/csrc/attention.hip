@@ -496,16 +496,17 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     constexpr int PIECES = (DT + 1) / 2;  // of 16 codes, for a thread, of a tile's K and of its V
     extern __shared__ char lds[];
     __shared__ float exps[2][2][4];       // [buffer][K, V][16 tokens]
+    __shared__ uint32_t pages[2][4];      // of the next tile
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, i32 = lane & 31;
-    const uint32_t h = blockIdx.y, b = blockIdx.z, d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads;
+    const uint32_t h = blockIdx.x, b = blockIdx.z, d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (blockIdx.x == 0) not_a_number(a, b, h);
+        if (blockIdx.y == 0) not_a_number(a, b, h);
         return;
     }
     const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + kRows - 1) / kRows;
-    if (blockIdx.x >= row_tiles) return;
-    const uint32_t r0 = (row_tiles - 1 - blockIdx.x) * kRows;  // the rows that see most first
+    if (blockIdx.y >= row_tiles) return;
+    const uint32_t r0 = (row_tiles - 1 - blockIdx.y) * kRows;  // the rows that see most first, of all heads
     const uint32_t r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
     const Tiles tiles = tiles_of(a, v, tok0, tok1);
@@ -528,33 +529,33 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     const int32_t low = a.window ? pos - (int32_t)a.window : -1;  // keys in (low, pos] are seen
     const int32_t pos_first = v.len - v.rows + tok0, pos_last = v.len - v.rows + tok1;
 
-    // Row of K for token x of 32: the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
+    // What a thread brings of a tile: of K, pieces of 16 dimensions of a token; of V, of 16 tokens of a dimension.  As in
+    // k_attend_few every load is made; what lies outside is not kept.
+    uint32_t k_run[PIECES], k_at[PIECES], v_run[PIECES], v_at[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const uint32_t p = tid + kBlock * i < 128 * DT ? tid + kBlock * i : tid, slot = p / (2 * DT), c = p % (2 * DT) * 16, dim = p >> 2;
+        k_run[i] = slot >> 4;
+        k_at[i] = (slot & 15) * d + (c < d ? c : 0);
+        v_run[i] = p & 3;
+        v_at[i] = (dim < d ? dim : 0) << a.page_log;
+    }
     v4u kr[PIECES], vr[PIECES];
-    auto fetch = [&](uint32_t t) {
+    float my_exp = 0.0f;  // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens
+    auto fetch = [&](uint32_t t, const uint32_t(&page)[4]) {
+        const uint32_t head = T * d;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t p = tid + kBlock * i, slot = p / (2 * DT), c = p % (2 * DT) * 16, token = t * kTile + slot;
-            kr[i] = v4u{0, 0, 0, 0};
-            if (p < 128 * DT && c < d && token < len) {
-                const uint32_t page = page_or_0(a, page_of(a, b, token, len));
-                kr[i] = *(const v4u*)(a.cache.k + (((size_t)page * H + h) * T + (token & (T - 1))) * d + c);
-            }
-            const uint32_t run = p & 3, dim = p >> 2, vt = t * kTile + 16 * run;
-            vr[i] = v4u{0, 0, 0, 0};
-            if (p < 128 * DT && dim < d && vt < len) {
-                const uint32_t page = page_or_0(a, page_of(a, b, vt, len));
-                vr[i] = *(const v4u*)(a.cache.v + ((((size_t)page * H + h) * d + dim) << a.page_log) + (vt & (T - 1)));
-            }
+            const uint32_t kp = page_or_0(a, page[k_run[i]]), vp = page_or_0(a, page[v_run[i]]);
+            const uint32_t k_slot = (t * kTile + 16 * k_run[i]) & (T - 1), v_slot = (t * kTile + 16 * v_run[i]) & (T - 1);
+            kr[i] = *(const v4u*)(a.cache.k + ((size_t)kp * H + h) * head + k_slot * d + k_at[i]);
+            vr[i] = *(const v4u*)(a.cache.v + ((size_t)vp * H + h) * head + v_at[i] + v_slot);
         }
-    };
-    float my_exp = 0.0f;  // threads 0..7: K's and V's exponents of the tile's runs
-    auto fetch_exp = [&](uint32_t t) {
         if (tid < 8) {
-            const uint32_t token = t * kTile + 16 * (tid & 3);
-            const uint32_t page = page_of(a, b, token, len);
-            const bool none = page >= a.cache.pages;
-            if (none && token < len) report(a.s, ZK_FAULT_PAGE);
-            const size_t at = (size_t)page_or_0(a, page) * H + h;
+            const uint32_t it = page[tid & 3];
+            const bool none = it >= a.cache.pages;
+            if (none && t * kTile + 16 * (tid & 3) < len) report(a.s, ZK_FAULT_PAGE);
+            const size_t at = (size_t)page_or_0(a, it) * H + h;
             my_exp = none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at]);
         }
     };
@@ -565,6 +566,7 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t p = tid + kBlock * i, slot = p / (2 * DT), c = p % (2 * DT), x = slot & 31;
             if (p >= 128 * DT) continue;
+            // the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
             const uint32_t row = (slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3);
             v8h* k16 = (v8h*)(kb + row * L::krow + c * 32);
             k16[0] = widen(kr[i][0], kr[i][1]);
@@ -580,17 +582,23 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[c] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     float m = -kInf, l = 0.0f;
+    // pages are looked up two tiles ahead, by threads 0..3
+    uint32_t my_page = 0;
     if (tiles.first < tiles.end) {
-        fetch(tiles.first);
-        fetch_exp(tiles.first);
+        uint32_t page[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = page_of(a, b, tiles.first * kTile + 16 * i, len);
+        if (tid < 4) my_page = page_of(a, b, (tiles.first + 1) * kTile + 16 * tid, len);
+        fetch(tiles.first, page);
     }
     for (uint32_t t = tiles.first; t < tiles.end; ++t) {
         const uint32_t buf = (t - tiles.first) & 1;
         stage(buf);
+        if (tid < 4) pages[buf][tid] = my_page;
         __syncthreads();
         if (t + 1 < tiles.end) {
-            fetch(t + 1);
-            fetch_exp(t + 1);
+            if (tid < 4) my_page = page_of(a, b, (t + 2) * kTile + 16 * tid, len);
+            fetch(t + 1, pages[buf]);
         }
         const char* kb = lds + buf * L::bytes;
         const char* vb = kb + L::k_bytes;
@@ -702,7 +710,7 @@ template <int DT>
 int launch_many(const Args& a, hipStream_t stream) {
     const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
     if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_many<DT>), dim3((unsigned)div_up(a.rows_most, kRows), a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, stream, a);
+    hipLaunchKernelGGL((k_attend_many<DT>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs), dim3(kBlock), lds, stream, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -745,7 +753,7 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
     const uint64_t most = rows_most(seqs->rows, seqs->max_new, group);
-    if (most >= 0x80000000u) return ZK_E_BADARG;
+    if (div_up(most, kRows) > 65535) return ZK_E_BADARG;
     // what a window lets a sequence's rows see, with a tile that it ends in
     const uint64_t seen = window ? (uint64_t)window + seqs->max_new + kTile : seqs->max_len;
     const Split sp = few_rows(most) ? split_of(seqs->seqs, cache->kv_heads, tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len))
