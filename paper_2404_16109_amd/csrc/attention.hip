@@ -28,7 +28,6 @@ static const float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 static const float kHead = 14.0f;      // P reaches up to 2^14
 static const uint32_t kTile = 64;      // tokens
 static const uint32_t kWorkgroups = 512;
-static const uint32_t kShort = 16;     // tiles
 
 struct Args {
     kvcache_i8 cache;
@@ -41,6 +40,7 @@ struct Args {
     float scale;
     uint32_t window, group, page_log, splits, each;  // group: query heads of a head of the cache
     int dtype;
+    bool few;   // which kernel leaves the parts
     bool wide;  // q's rows and heads are 16-byte aligned
     float* parts;  // of (sequence, head, split, row): head_dim sums; after all of them (M, l)
     float2* parts_ml;
@@ -169,6 +169,13 @@ __device__ __forceinline__ Tiles tiles_of(const Args& a, const SeqView& v, int32
     t.first = low > 0 ? (uint32_t)(low / kTile) : 0;
     t.end = last < 0 ? t.first : (uint32_t)(last / kTile) + 1;
     return t;
+}
+
+// The same for the 128 rows from r0 on that a workgroup of k_attend_many has.
+static const uint32_t kRows = 128;
+__device__ __forceinline__ Tiles tiles_of_rows(const Args& a, const SeqView& v, uint32_t r0) {
+    const uint32_t R = (uint32_t)v.rows * a.group, last = r0 + kRows < R ? r0 + kRows - 1 : R - 1;
+    return tiles_of(a, v, (int32_t)(r0 / a.group), (int32_t)(last / a.group));
 }
 
 // Tiles of a workgroup's part.  The same for all sequences of a call, so that workgroups have like work and short sequences
@@ -443,7 +450,7 @@ __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
         return;
     }
     if (r >= (uint32_t)v.rows * a.group) return;
-    const Tiles tiles = tiles_of(a, v, 0, v.rows - 1);
+    const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / kRows * kRows);
     const uint32_t each = part_of(a, tiles), used = (tiles.end - tiles.first + each - 1) / each;
     const size_t part0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
     const float2 ml = tid < used ? a.parts_ml[part0 + (size_t)tid * a.rows_most] : make_float2(-kInf, 0.0f);
@@ -481,8 +488,6 @@ __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
 
 // ---- many rows -------------------------------------------------------------------------------------------------------
 
-static const uint32_t kRows = 128;
-
 // Lane 32 h + i: row i of its wavefront's 32, tokens 16 h .. 16 h + 15 of each half of a tile.
 // DT: head_dim in units of 32, rounded up.  Rows in LDS are padded by 16 bytes: then those of 16 neighbouring rows lie in
 // different banks, whatever DT.
@@ -498,10 +503,11 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     __shared__ float exps[2][2][4];       // [buffer][K, V][16 tokens]
     __shared__ uint32_t pages[2][4];      // of the next tile
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, i32 = lane & 31;
-    const uint32_t h = blockIdx.x, b = blockIdx.z, d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads;
+    const uint32_t h = blockIdx.x, b = blockIdx.z / a.splits, split = blockIdx.z - b * a.splits;
+    const uint32_t d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (blockIdx.y == 0) not_a_number(a, b, h);
+        if (blockIdx.y == 0 && a.splits == 1) not_a_number(a, b, h);
         return;
     }
     const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + kRows - 1) / kRows;
@@ -509,7 +515,13 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     const uint32_t r0 = (row_tiles - 1 - blockIdx.y) * kRows;  // the rows that see most first, of all heads
     const uint32_t r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
-    const Tiles tiles = tiles_of(a, v, tok0, tok1);
+    Tiles tiles = tiles_of_rows(a, v, r0);
+    if (a.splits > 1) {
+        const uint32_t each = part_of(a, tiles);
+        tiles.first += split * each;
+        if (tiles.first >= tiles.end) return;  // k_attend_join knows
+        tiles.end = tiles.first + each < tiles.end ? tiles.first + each : tiles.end;
+    }
     const uint32_t r = r0 + wave * 32 + i32, len = (uint32_t)v.len;
 
     v8h qf[2 * DT];
@@ -661,18 +673,29 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         }
     }
     l = add_halves(l);
-    if (r < R) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const size_t at = row_at(a, v, h, r, a.orow, a.ohead);
+    if (r >= R) return;
+    if (a.splits > 1) {
+        const size_t part = (((size_t)b * H + h) * a.splits + split) * a.rows_most + r;
 #pragma unroll
         for (int c = 0; c < DT; ++c)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t dim = 32 * c + 8 * (e >> 2) + 4 * half + (e & 3);
-                if (dim < d) put_at(a.out, at + dim, l == 0.0f ? 0.0f : o[c][e] * inv, a.dtype);
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t dim = 32 * c + 2 * e + 4 * half;
+                if (dim < d) *(v4f*)(a.parts + part * d + dim) = v4f{o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
             }
-        if (a.lse && half == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(m == -kInf ? 0.0f : m, l);
+        if (half == 0) a.parts_ml[part] = make_float2(m, l);
+        return;
     }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const size_t at = row_at(a, v, h, r, a.orow, a.ohead);
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t dim = 32 * c + 8 * (e >> 2) + 4 * half + (e & 3);
+            if (dim < d) put_at(a.out, at + dim, l == 0.0f ? 0.0f : o[c][e] * inv, a.dtype);
+        }
+    if (a.lse && half == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(m == -kInf ? 0.0f : m, l);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
@@ -681,20 +704,24 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
 struct Split {
     uint32_t splits, each;
 };
-uint32_t most_splits(uint32_t seqs, uint32_t kv_heads, uint32_t tiles) {
-    const uint64_t groups = (uint64_t)seqs * kv_heads;
-    uint64_t n = groups >= kWorkgroups ? 1 : div_up(kWorkgroups, groups);
-    if (n > div_up(tiles, 4)) n = div_up(tiles, 4);  // a tile for each wavefront
-    return n > kMostSplits ? kMostSplits : (uint32_t)n;
+bool few_rows(uint64_t rows) { return rows <= 32; }
+// Tiles that one workgroup of eight wavefronts does in one launch.  Measured at 8 heads of 128: one sequence of 777 tokens
+// 10.7 us that way and 10.2 shared out, of 2000 16.6 and 10.6; 16 sequences of 1000 12.7 and 15.9; 24 of 1000 (four heads) 11.9 and 14.7.
+uint32_t short_tiles(uint32_t seqs, uint32_t kv_heads) { return (uint64_t)seqs * kv_heads < 64 ? 8 : 32; }
+// rows: of a sequence and head.  With many rows a workgroup is worth four tiles too, and the chip is full with fewer.
+uint32_t most_splits(uint32_t seqs, uint32_t kv_heads, uint64_t rows, uint32_t tiles) {
+    const uint64_t groups = (uint64_t)seqs * kv_heads * (few_rows(rows) ? 1 : div_up(rows, kRows));
+    uint64_t n = groups >= (few_rows(rows) ? kWorkgroups : kWorkgroups / 2) ? 1 : div_up(kWorkgroups, groups);
+    if (n > div_up(tiles, 4)) n = div_up(tiles, 4);  // few rows: a tile for each wavefront
+    if (n > kMostSplits) n = kMostSplits;
+    return n * seqs > 65535 ? 65535 / seqs : (uint32_t)n;
 }
-Split split_of(uint32_t seqs, uint32_t kv_heads, uint32_t tiles) {
-    if (tiles <= kShort) return {1, tiles};
-    const uint32_t each = (uint32_t)align_up(div_up(tiles, most_splits(seqs, kv_heads, tiles)), 4);
+Split split_of(uint32_t seqs, uint32_t kv_heads, uint64_t rows, uint32_t tiles) {
+    if (few_rows(rows) && tiles <= short_tiles(seqs, kv_heads)) return {1, tiles};
+    const uint32_t each = (uint32_t)align_up(div_up(tiles, most_splits(seqs, kv_heads, rows, tiles)), 4);
     return {(uint32_t)div_up(tiles, each), each};
 }
 uint32_t tiles_for(uint32_t len) { return len ? (uint32_t)div_up(len, kTile) : 1; }
-
-bool few_rows(uint64_t rows) { return rows <= 32; }
 
 template <int NJ, int RT, int W>
 int launch_few(const Args& a, hipStream_t stream) {
@@ -710,7 +737,8 @@ template <int DT>
 int launch_many(const Args& a, hipStream_t stream) {
     const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
     if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_many<DT>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs), dim3(kBlock), lds, stream, a);
+    hipLaunchKernelGGL((k_attend_many<DT>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs * a.splits), dim3(kBlock), lds, stream, a);
+    if (a.splits > 1) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -735,9 +763,11 @@ extern "C" size_t kvcache_attention_workspace_bytes(uint32_t seqs, uint32_t rows
     if (!kv_heads || q_heads % kv_heads || !seqs || !rows || !max_new) return 0;
     const uint64_t most = rows_most(rows, max_new, q_heads / kv_heads);
     const uint32_t tiles = tiles_for(max_len);
-    if (!few_rows(most) || tiles <= kShort) return 0;
+    if (few_rows(most) && tiles <= short_tiles(seqs, kv_heads)) return 0;
     // a window makes tiles and workgroups fewer, never more
-    const size_t parts = (size_t)seqs * kv_heads * most_splits(seqs, kv_heads, tiles) * most;
+    const uint32_t splits = most_splits(seqs, kv_heads, most, tiles);
+    if (splits == 1) return 0;
+    const size_t parts = (size_t)seqs * kv_heads * splits * most;
     Carver cv(nullptr, 0);
     cv.take(parts * head_dim * sizeof(float));
     cv.take(parts * sizeof(float2));
@@ -756,8 +786,7 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     if (div_up(most, kRows) > 65535) return ZK_E_BADARG;
     // what a window lets a sequence's rows see, with a tile that it ends in
     const uint64_t seen = window ? (uint64_t)window + seqs->max_new + kTile : seqs->max_len;
-    const Split sp = few_rows(most) ? split_of(seqs->seqs, cache->kv_heads, tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len))
-                                    : Split{1, 1};
+    const Split sp = split_of(seqs->seqs, cache->kv_heads, most, tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len));
     Args a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -773,6 +802,7 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     a.group = group;
     a.page_log = (uint32_t)log2_floor(cache->page_tokens);
     a.dtype = dtype;
+    a.few = few_rows(most);
     a.wide = aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0;
     a.rows_most = (uint32_t)most;
     a.splits = sp.splits;

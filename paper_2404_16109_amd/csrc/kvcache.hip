@@ -5,8 +5,8 @@
 // number), settles the page's exponent, and writes: new codes, and the old ones where the exponent grew.  Multiplying
 // by a power of two is exact, so rint(x * 2^-e) is the only rounding of a new code, and rint(c * 2^-shift) of an old one.
 //
-// Bound by bytes for prompts (the new values are read twice, the second time from the L2, and one byte of each is
-// written), by the chain of four dependent loads for single tokens.
+// Bound by bytes for prompts (pages that begin are read once, others twice, the second time from the L2, and one byte of each
+// value is written), by the chain of four dependent loads for single tokens.
 #include "kvcache.h"
 
 namespace zkmi {
@@ -63,7 +63,99 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float factor) {
     return r;
 }
 
+// Bytes i of four words as a word, i = 0..3.
+__device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&out)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+    const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// A page that begins with this call, its 4 x 8 (tokens x dimensions) pieces held in registers from the first look to the
+// codes: kPieces to a thread, pages of at most kPageInRegs codes.  Values go through LDS to lie by dimension.
+static const int kPieces = 2;
+static const uint32_t kPageInRegs = kPieces * kBlock * 32;
 template <int DT>
+__device__ void append_page(const Fresh& f, size_t x0, size_t row_stride, int hi, uint32_t T, uint32_t d, bool values, int8_t* codes,
+                            int8_t* exps, uint32_t* most, char* lds) {
+    constexpr int words = DT == ZK_F32 ? 2 : 1;
+    const uint32_t tid = threadIdx.x, d8 = d >> 3, pieces = (T >> 2) * d8;
+    v4u raw[kPieces][4][words];
+    uint32_t amax = 0;
+    auto value = [&](int p, int t, int e) -> float {
+        if constexpr (DT == ZK_F32) return bits_float(raw[p][t][e >> 2][e & 3]);
+        else return half_of<DT>(raw[p][t][0][e >> 1], e & 1);
+    };
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        const uint32_t i = tid + kBlock * p, c = i % d8 * 8, t0 = i / d8 * 4;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int w = 0; w < words; ++w) {
+                raw[p][t][w] = v4u{0, 0, 0, 0};
+                if (i < pieces && (int)t0 + t < hi)
+                    raw[p][t][w] = ((const v4u*)((const char*)f.x + (x0 + (size_t)(t0 + t) * row_stride + c) * (DT == ZK_F32 ? 4 : 2)))[w];
+            }
+    }
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t a = float_bits(value(p, t, e)) & 0x7fffffffu;
+                amax = a > amax ? a : amax;
+            }
+    amax = wave_max(amax);
+    if ((tid & 63) == 0) most[tid >> 6] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kBlock / 64; ++w) amax = most[w] > amax ? most[w] : amax;
+    const int e = exponent_for(amax);
+    if (tid == 0) *exps = (int8_t)e;
+    const bool fine = e != ZK_EXP_NAN;
+    const float step = fine ? pow2(-e) : 0.0f;
+    const uint32_t vrow = T + 4;  // in LDS
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        const uint32_t i = tid + kBlock * p, c = i % d8 * 8, t0 = i / d8 * 4;
+        if (i >= pieces) continue;
+        uint32_t w[2][4];  // [half][token]
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                w[half][t] = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[half][t] |= (fine ? (uint32_t)code_of(value(p, t, 4 * half + k), step) & 255u : 0u) << (8 * k);
+            }
+        if (!values) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) *(uint2*)(codes + (size_t)(t0 + t) * d + c) = make_uint2(w[0][t], w[1][t]);
+        } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t by[4];
+                transpose4(w[half], by);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) *(uint32_t*)(lds + (c + 4 * half + k) * vrow + t0) = by[k];
+            }
+        }
+    }
+    if (!values) return;
+    __syncthreads();
+    const uint32_t t16 = T >> 4;
+    for (uint32_t i = tid; i < d * t16; i += kBlock) {
+        const uint32_t* at = (const uint32_t*)(lds + i / t16 * vrow + i % t16 * 16);
+        ((v4u*)codes)[i] = v4u{at[0], at[1], at[2], at[3]};
+    }
+}
+
+// PAGES: calls that may fill pages, 256 threads.
+template <int DT, bool PAGES>
 __global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, Fresh fv, kv_seqs s, uint32_t page_log) {
     __shared__ uint32_t most[4];
     const uint32_t tid = threadIdx.x, T = 1u << page_log, d = cache.head_dim, H = cache.kv_heads;
@@ -94,6 +186,13 @@ __global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, F
     const int64_t row0 = (int64_t)q.row0 + from - first;
     auto at = [&](int t) -> size_t { return (size_t)(row0 + t) * f.row_stride + x0; };
 
+    if constexpr (PAGES) {
+        __shared__ uint32_t lds[(kPageInRegs + 4 * 256) / 4];
+        if (lo == 0 && hi >= 16 && f.wide && T * d <= kPageInRegs) {
+            append_page<DT>(f, (size_t)row0 * f.row_stride + x0, f.row_stride, hi, T, d, values, codes, exps, most, (char*)lds);
+            return;
+        }
+    }
     const uint32_t d16 = d >> 4;
     uint32_t amax = 0;
     for (uint32_t i = tid; i < (uint32_t)(hi - lo) * d16; i += blockDim.x) {
@@ -105,11 +204,7 @@ __global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, F
             amax = a > amax ? a : amax;
         }
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        const uint32_t other = __shfl_xor(amax, o);
-        amax = other > amax ? other : amax;
-    }
+    amax = wave_max(amax);
     if ((tid & 63) == 0) most[tid >> 6] = amax;
     __syncthreads();
     for (uint32_t w = 0; w < blockDim.x >> 6; ++w) amax = most[w] > amax ? most[w] : amax;
@@ -199,7 +294,8 @@ int append(const kvcache_i8& cache, const Fresh& fk, const Fresh& fv, const kv_s
     const unsigned pages = (unsigned)(((size_t)T - 1 + span - 1) / T + 1);  // with the first slot the page's last
     // one wavefront has enough to do with a head of a single token; beyond 16 values to each of its lanes, four
     const unsigned threads = (size_t)(span < T ? span : T) * cache.head_dim <= 1024 ? 64 : kBlock;
-    hipLaunchKernelGGL((k_append<DT>), dim3(pages, 2 * cache.kv_heads, s.seqs), dim3(threads), 0, stream, cache, fk, fv, s, log);
+    auto* kernel = threads == kBlock ? k_append<DT, true> : k_append<DT, false>;
+    hipLaunchKernelGGL(kernel, dim3(pages, 2 * cache.kv_heads, s.seqs), dim3(threads), 0, stream, cache, fk, fv, s, log);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
