@@ -25,7 +25,14 @@ static const int kStep = 128;                      // inputs a wavefront takes a
 static const int kWaves = 8;
 static const uint32_t kStageHalves = 32768;        // 64 KiB of x in LDS
 static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of columns
-static const uint32_t kWide = 16384;               // outputs from which a workgroup of the many-column kernel has 128
+// More columns than 16: blocks of 16 that each read the weights again (out of the caches), or the kernel for many columns, whose
+// workgroups have 64 or 128 outputs and are too few for a short matrix.  Measured, the first against the second, us: 32
+// vectors of bf16 by 4096 x 11008 18 and 42, by 8192 x 4096 (20 of them) 18.2 and 20.8, by 13824 x 5120 30 and 26, by 32001 x
+// 5120 63 and 39; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x 4096 28 and 25.
+static const uint32_t kManyOutputs = 10240, kBlocksOfFew = 6;
+// Outputs from which a workgroup of the kernel for many columns has 128, not 64: 64 by 13824 x 5120 42 us with 128 and 33 with 64,
+// 32 of 32 bits by 32001 x 5120 62 and 86.
+static const uint32_t kWide = 16384;
 
 template <int DT>
 struct Kind {
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
     const Buffer weights = weights_of(codes, n, k, n0, 16);
     constexpr int ahead = STAGED ? 3 : 2;
     v4u w[ahead], xa[ahead][4];
-    const Buffer operands = buffer_of(xf, STAGED ? 0 : (size_t)steps * 4096);
+    const Buffer operands = buffer_of(xf + (size_t)blockIdx.y * steps * 256, STAGED ? 0 : (size_t)steps * 4096);
     auto fetch_x = [&](uint32_t j, v4u(&to)[4]) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) to[q] = load16(operands, j * 4096 + q * 1024 + lane * 16);
@@ -353,10 +360,10 @@ struct ManyLds {
     static constexpr uint32_t meet = 4 * NT * CT * 64 * 16;  // also the outputs, C * N floats
     static constexpr uint32_t all = 2 * bytes > meet ? 2 * bytes : meet;
 };
-template <int DT, int CT, int NT>
+template <int DT, int CT, int NT, int GL>
 __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, size_t rows, const uint8_t* codes,
-                                                 const uint16_t* scales, uint32_t n, uint32_t k, uint32_t group_log, uint32_t vectors,
-                                                 float unit2) {
+                                                 const uint16_t* scales, uint32_t n, uint32_t k, uint32_t vectors, float unit2) {
+    constexpr uint32_t group_log = GL;
     using L = ManyLds<CT, NT>;
     constexpr uint32_t C = L::C, N = L::N;
     extern __shared__ v4u shared[];
@@ -366,27 +373,23 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
     const uint32_t steps = (k + kStep - 1) / kStep, k8_all = steps * (kStep / 8), chunks = (steps + 1) / 2;
     const uint32_t groups = (k + (1u << group_log) - 1) >> group_log, all_groups = k8_all >> (group_log - 3), each = 256u >> group_log;
 
+    // What a thread brings of a chunk lies in a row with what its neighbours bring; behind the last input everything reads as 0.
+    const Buffer operands = buffer_of(xf + (size_t)block * k8_all * C, (size_t)k8_all * C * 16);
+    const Buffer offsets = buffer_of(sums + (size_t)block * all_groups * C, (size_t)all_groups * C * 4);
+    const Buffer factors = buffer_of(scales + (size_t)n0 * groups, (size_t)(n - n0 < N ? n - n0 : N) * groups * 2);
     v4u xr[CT];
     float br[2];
-    uint16_t sr[2 * NT];
+    uint16_t sr[NT];
     auto ask = [&](uint32_t chunk) {
 #pragma unroll
-        for (int i = 0; i < CT; ++i) {
-            const uint32_t p = tid + 512 * i, k8 = chunk * 32 + p / C;
-            xr[i] = v4u{0, 0, 0, 0};
-            if (k8 < k8_all) xr[i] = xf[((size_t)block * k8_all + k8) * C + p % C];
-        }
+        for (int i = 0; i < CT; ++i) xr[i] = load16(operands, (chunk * 32 * C + tid + 512 * i) * 16);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t p = tid + 512 * i, gr = chunk * each + p / C;
-            br[i] = 0.0f;
-            if (p < each * C && gr < all_groups) br[i] = sums[((size_t)block * all_groups + gr) * C + p % C];
-        }
+        for (int i = 0; i < 2; ++i)
+            br[i] = bits_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(offsets, (int)((chunk * each * C + tid + 512 * i) * 4), 0, 0));
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            const uint32_t p = tid + 512 * i, gr = chunk * each + p / N, o = n0 + p % N;
-            sr[i] = 0;
-            if (p < each * N && gr < groups && o < n) sr[i] = scales[(size_t)o * groups + gr];
+            const uint32_t p = tid + 512 * i, gr = chunk * each + p / N;
+            sr[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(factors, (int)(gr < groups ? (p % N * groups + gr) * 2 : kNowhere), 0, 0);
         }
     };
     auto put = [&](uint32_t buf) {
@@ -439,37 +442,39 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
         const uint16_t* ss = (const uint16_t*)(at + L::x + L::sums) + nw * 16 * NT + i16;
         v4f acc[NT][CT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int c = 0; c < CT; ++c) acc[t][c] = v4f{0, 0, 0, 0};
-#pragma unroll
         for (int q = 0; q < 4; ++q) {
+            const uint32_t gr = (kw * kStep + q * 32) >> group_log;
+            if (q == 0 || (q == 2 && group_log <= 6) || group_log == 5) {
+                // a group's sums start at what the codes' offset takes off
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    acc[0][c] = *(const v4f*)(bs + gr * C + 16 * c);
+#pragma unroll
+                    for (int t = 1; t < NT; ++t) acc[t][c] = acc[0][c];
+                }
+            }
             v4u f[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) f[t] = widen<DT>(r[t][q]);
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                const v4u a = xs[q * 4 * C + 16 * c];
+                const v4u x = xs[q * 4 * C + 16 * c];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t][c] = product<DT>(a, f[t], acc[t][c]);
+                for (int t = 0; t < NT; ++t) acc[t][c] = product<DT>(x, f[t], acc[t][c]);
             }
             if (q == 3 || (q & 1 && group_log <= 6) || group_log == 5) {
-                const uint32_t gr = (kw * kStep + q * 32) >> group_log;
 #pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const v4f b = *(const v4f*)(bs + gr * C + 16 * c);
+                for (int t = 0; t < NT; ++t) {
+                    const uint32_t s = ss[gr * N + 16 * t];
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const uint32_t s = ss[gr * N + 16 * t];
-                        const v4f whole = acc[t][c] + b;
+                    for (int c = 0; c < CT; ++c) {
                         if constexpr (DT == ZK_I16) {
 #pragma unroll
                             for (int v = 0; v < 2; ++v)
-                                itotal[t][c][v] += (int64_t)((int)(whole[2 * v] * 2.0f) * 256 + (int)(whole[2 * v + 1] * 2.0f)) * (int64_t)s;
+                                itotal[t][c][v] += (int64_t)((int)(acc[t][c][2 * v] * 2.0f) * 256 + (int)(acc[t][c][2 * v + 1] * 2.0f)) * (int64_t)s;
                         } else {
-                            total[t][c] += whole * (float)s;
+                            total[t][c] += acc[t][c] * (float)s;
                         }
-                        acc[t][c] = v4f{0, 0, 0, 0};
                     }
                 }
             }
@@ -554,14 +559,15 @@ struct Way {
     size_t operands, sums;      // in the workspace, bytes
 };
 template <int DT>
-Way way_of(size_t rows, uint32_t k) {
+Way way_of(size_t rows, uint32_t n, uint32_t k) {
     constexpr uint32_t parts = Kind<DT>::parts;
     Way w = {};
     w.k8 = (uint32_t)align_up(k, kStep) / 8;
-    if (rows <= (size_t)Kind<DT>::vectors) {
-        w.blocks = w.tiles = 1;
+    if (rows <= (size_t)Kind<DT>::vectors || (n < kManyOutputs && rows * parts <= 16 * kBlocksOfFew)) {
+        w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
-        w.staged = (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
+        w.blocks = (uint32_t)div_up(rows, w.vectors);
+        w.staged = w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
     } else {
         // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
         const size_t most = 96 / parts;
@@ -595,14 +601,20 @@ struct Call {
     hipStream_t stream;
 };
 
-template <int DT, int CT, int NT>
+template <int DT, int CT, int NT, int GL>
 int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
     const size_t lds = ManyLds<CT, NT>::all;
-    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_w4_many<DT, CT, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_w4_many<DT, CT, NT>), dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf,
-                       sums, c.rows, c.codes, c.scales, c.n, c.k, c.group_log, w.vectors, c.unit * 2.0f);
+    auto* kernel = k_w4_many<DT, CT, NT, GL>;
+    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, c.rows,
+                       c.codes, c.scales, c.n, c.k, w.vectors, c.unit * 2.0f);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
+}
+template <int DT, int CT, int NT>
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums)
+                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums);
 }
 template <int DT, int CT>
 int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
@@ -611,7 +623,7 @@ int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
 
 template <int DT>
 int run(const Call& c) {
-    const Way w = way_of<DT>(c.rows, c.k);
+    const Way w = way_of<DT>(c.rows, c.n, c.k);
     v4u* xf = nullptr;
     float* sums = nullptr;
     if (w.operands) {
@@ -626,10 +638,10 @@ int run(const Call& c) {
         ZK_HIP_TRY(hipGetLastError());
     }
     if (w.tiles == 1) {
-        const uint32_t cols = (uint32_t)c.rows * Kind<DT>::parts;
+        const uint32_t cols = (uint32_t)c.rows * Kind<DT>::parts;  // of a call that stages x
         size_t lds = (w.staged ? (size_t)w.k8 * cols * 16 : 0) + (size_t)(w.k8 >> (c.group_log - 3)) * 32;
         if (lds < 8192) lds = 8192;  // the sums at the end
-        const dim3 grid((unsigned)div_up(c.n, 16), 1);
+        const dim3 grid((unsigned)div_up(c.n, 16), w.blocks);
         auto* kernel = w.staged ? (c.group_log == 5 ? k_w4_few<DT, true, 5> : c.group_log == 6 ? k_w4_few<DT, true, 6> : k_w4_few<DT, true, 7>)
                                 : (c.group_log == 5 ? k_w4_few<DT, false, 5> : c.group_log == 6 ? k_w4_few<DT, false, 6> : k_w4_few<DT, false, 7>);
         if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
@@ -652,13 +664,21 @@ bool weights_ok(const uint8_t* codes, const uint16_t* scales, size_t n, size_t k
 
 using namespace zkmi;
 
+namespace {
+template <int DT>
+size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs
+    const size_t few = way_bytes(way_of<DT>(rows, 1, k)), many = way_bytes(way_of<DT>(rows, 1u << 24, k));
+    return few > many ? few : many;
+}
+}  // namespace
+
 extern "C" size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k) {
     if (!dtype_bytes(dtype) || rows == 0 || rows > kMostRows || !inputs_ok(k)) return 0;
     switch (dtype) {
-        case ZK_F32: return way_bytes(way_of<ZK_F32>(rows, (uint32_t)k));
-        case ZK_F16: return way_bytes(way_of<ZK_F16>(rows, (uint32_t)k));
-        case ZK_BF16: return way_bytes(way_of<ZK_BF16>(rows, (uint32_t)k));
-        default: return way_bytes(way_of<ZK_I16>(rows, (uint32_t)k));
+        case ZK_F32: return workspace<ZK_F32>(rows, (uint32_t)k);
+        case ZK_F16: return workspace<ZK_F16>(rows, (uint32_t)k);
+        case ZK_BF16: return workspace<ZK_BF16>(rows, (uint32_t)k);
+        default: return workspace<ZK_I16>(rows, (uint32_t)k);
     }
 }
 
