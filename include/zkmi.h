@@ -552,7 +552,7 @@ typedef struct {
  * at position lens[b] - (cu[b+1]-cu[b]) + i.  A row whose position is negative is no
  * token: nothing is stored for it, and as a query it sees no key.  Token t lies in
  * page table[b * table_stride + t / page_tokens]; entries that no token needs are
- * not read.  cu, lens and table are device arrays.  max_new: the most rows any
+ * not used.  cu, lens and table are device arrays.  max_new: the most rows any
  * sequence has (host; at least 1).  max_len: about the longest lens[b] (host; it
  * decides how the work is spread, not what is computed).
  *

@@ -41,6 +41,8 @@ struct Args {
     uint32_t window, group, page_log, splits, each;  // group: query heads of a head of the cache
     int dtype;
     bool few;   // which kernel leaves the parts
+    bool crowd;  // sequences and heads enough for workgroups of four wavefronts
+    uint32_t shared;  // workgroups of k_attend_shared, 0 if it is not used
     bool wide;  // q's rows and heads are 16-byte aligned
     float* parts;  // of (sequence, head, split, row): head_dim sums; after all of them (M, l)
     float2* parts_ml;
@@ -186,10 +188,10 @@ __device__ __forceinline__ uint32_t part_of(const Args& a, const Tiles& t) {
 }
 
 // The page of a token, as the table has it: what it is worth is looked at when it is used, not while it is on its way.
-// Tokens behind the sequence have the last one's.  len > 0.
-__device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t b, uint32_t token, uint32_t len) {
-    const uint32_t last = token < len ? token : len - 1;
-    return (uint32_t)a.s.table[(size_t)b * a.s.table_stride + (last >> a.page_log)];
+// Tokens behind the sequence have what the table holds there, or its last entry.
+__device__ __forceinline__ uint32_t page_of(const Args& a, uint32_t b, uint32_t token) {
+    const uint32_t at = token >> a.page_log, last = a.s.table_pages - 1;
+    return (uint32_t)a.s.table[(size_t)b * a.s.table_stride + (at < last ? at : last)];
 }
 __device__ __forceinline__ uint32_t page_or_0(const Args& a, uint32_t page) { return page < a.cache.pages ? page : 0; }
 
@@ -210,23 +212,26 @@ struct FewLds {
     static constexpr int row = 64 * NJ + 4;  // of sums, padded
     static size_t bytes(uint32_t rows) { return (2 * (size_t)W * 16 * RT + (size_t)W * rows * row) * sizeof(float); }
 };
+
+// The pages of a wavefront's first and second tile, once asked for.
+struct Asked {
+    uint32_t k, v, k_next, v_next;
+};
+__device__ __forceinline__ Asked ask_pages(const Args& a, uint32_t b, uint32_t t, uint32_t step) {
+    const uint32_t lane = threadIdx.x & 63, k = 16 * ((lane & 15) >> 2), v = 16 * (lane >> 4);
+    return Asked{page_of(a, b, t * kTile + k), page_of(a, b, t * kTile + v), page_of(a, b, (t + step) * kTile + k),
+                 page_of(a, b, (t + step) * kTile + v)};
+}
+
+// Tiles [t_first, t_end) of a sequence and head; `pages` are those of tile t_first + wavefront and the next.  What comes out are
+// the rows' outputs if that is all they see, else sums from row part0 of the workspace on.
 template <int NJ, int RT, int W>
-__global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
+__device__ __forceinline__ void attend_part(const Args& a, float* sh, const SeqView& v, uint32_t b, uint32_t h, uint32_t t_first, uint32_t t_end,
+                                            const Asked& pages, bool whole_row, size_t part0) {
     constexpr int DT = 4 * NJ;  // tiles of 16 dimensions
-    extern __shared__ float sh[];
-    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, i16 = lane & 15;
-    const uint32_t split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads;
-    const SeqView v = seq_view(a.s, b, a.page_log);
-    if (!v.ok) {
-        if (a.splits == 1) not_a_number(a, b, h);
-        return;
-    }
-    if (v.rows == 0) return;
-    const uint32_t R = (uint32_t)v.rows * a.group;
-    const Tiles tiles = tiles_of(a, v, 0, v.rows - 1);
-    const uint32_t each = part_of(a, tiles);
-    const uint32_t t_first = tiles.first + split * each, t_end = t_first + each < tiles.end ? t_first + each : tiles.end;
-    if (a.splits > 1 && t_first >= t_end) return;  // k_attend_join knows
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, i16 = lane & 15, rk = i16 >> 2;
+    const uint32_t d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads, R = (uint32_t)v.rows * a.group;
+    uint32_t pk_next = pages.k_next, pv_next = pages.v_next;
 
     v4u raw[RT][2 * NJ];  // q as it lies in memory; asked for first, since loads come back in order
 #pragma unroll
@@ -242,9 +247,9 @@ __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_atte
         }
     }
 
-    // Every load is made: tokens behind the sequence read some page of it, pages that are none page 0, dimensions behind
-    // head_dim the row's first (q is 0 there).  All are numbers, and nothing of them is kept.
-    const uint32_t len = (uint32_t)v.len, rk = i16 >> 2;
+    // Every load is made: tokens behind the sequence read some page, pages that are none page 0, dimensions behind head_dim
+    // the row's first (q is 0 there).  All are numbers, and nothing of them is kept.
+    const uint32_t len = (uint32_t)v.len;
     const size_t page_stride = (size_t)T * d;
     v4u kr[4][NJ], vr[DT];
     auto load_k = [&](uint32_t page, uint32_t t) {
@@ -283,14 +288,10 @@ __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_atte
     }
 
     uint32_t t = t_first + wave;
-    uint32_t pk_next = 0, pv_next = 0;
     if (t < t_end) {
-        const uint32_t pk = page_of(a, b, t * kTile + 16 * rk, len), pv = page_of(a, b, t * kTile + 16 * g, len);
-        pk_next = page_of(a, b, (t + W) * kTile + 16 * rk, len);
-        pv_next = page_of(a, b, (t + W) * kTile + 16 * g, len);
-        load_k(pk, t);
-        load_e(pv);
-        load_v(pv, t);
+        load_k(pages.k, t);
+        load_e(pages.v);
+        load_v(pages.v, t);
     }
     // q, scaled by a power of two; qmul takes that back and brings the units of log2
     v8h qf[RT][2 * NJ];
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_atte
 
     for (; t < t_end; t += W) {
         const bool more = t + W < t_end;
-        const uint32_t pk_after = page_of(a, b, (t + 2 * W) * kTile + 16 * rk, len), pv_after = page_of(a, b, (t + 2 * W) * kTile + 16 * g, len);
+        const uint32_t pk_after = page_of(a, b, (t + 2 * W) * kTile + 16 * rk), pv_after = page_of(a, b, (t + 2 * W) * kTile + 16 * g);
         v4f s[RT][4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -422,58 +423,184 @@ __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_atte
             l_all += ls[w * 16 * RT + r] * f;
             sum += *(const v4f*)(sums + (size_t)(w * R + r) * D + c) * f;
         }
-        if (a.splits == 1) {
+        if (whole_row) {
             const size_t at = row_at(a, v, h, r, a.orow, a.ohead) + c;
             const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
 #pragma unroll
             for (int e = 0; e < 4; ++e) put_at(a.out, at + e, l_all == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
             if (a.lse && c == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l_all);
         } else {
-            const size_t part = (((size_t)b * H + h) * a.splits + split) * a.rows_most + r;
+            const size_t part = part0 + r;
             *(v4f*)(a.parts + part * d + c) = sum;
             if (c == 0) a.parts_ml[part] = make_float2(all, l_all);
         }
     }
 }
 
-// A workgroup: one row of one sequence and head.  Threads hold four dimensions each; what is left of 256 takes splits
-// apart, and LDS adds them up.
+template <int NJ, int RT, int W>
+__global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
+    extern __shared__ float sh[];
+    const uint32_t split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, wave = uniform(threadIdx.x >> 6);
+    // The part begins where the caller's lengths put it, but for windows: its pages are asked for beside the lengths.
+    const uint32_t guess = split * a.each + wave;
+    Asked pages = ask_pages(a, b, guess, W);
+    const SeqView v = seq_view(a.s, b, a.page_log);
+    if (!v.ok) {
+        if (a.splits == 1) not_a_number(a, b, h);
+        return;
+    }
+    if (v.rows == 0) return;
+    const Tiles tiles = tiles_of(a, v, 0, v.rows - 1);
+    const uint32_t each = part_of(a, tiles);
+    const uint32_t t_first = tiles.first + split * each, t_end = t_first + each < tiles.end ? t_first + each : tiles.end;
+    if (a.splits > 1 && t_first >= t_end) return;  // k_attend_join knows
+    if (t_first + wave != guess) pages = ask_pages(a, b, t_first + wave, W);
+    attend_part<NJ, RT, W>(a, sh, v, b, h, t_first, t_end, pages, a.splits == 1,
+                           (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most);
+}
+
+// Sequences of unlike lengths: the tiles of all of them and of all heads lie in one row, sequence by sequence, head by head,
+// and every workgroup has as many of them, `quota`, wherever they begin and end.  A sequence and head that lies
+// in one workgroup is done there; of others a workgroup has an end as its first piece, a beginning as its last, or all it does
+// lies within one: two pieces of sums at most.
+// A sequence and head counts kPiece tiles more than it has, for what a piece costs however short it is (some 5 us to its first
+// scores and from its last, when four tiles take 2.3).
+static const uint32_t kMostShared = 256;  // sequences, a thread each
+static const uint32_t kPiece = 8;
+struct Row {
+    uint32_t tiles[kMostShared], before[kMostShared], sums[4];
+};
+struct Share {
+    uint32_t total, quota;
+};
+__device__ __forceinline__ Share share_out(const Args& a, Row& row) {
+    const uint32_t tid = threadIdx.x, lane = tid & 63;
+    uint32_t n = 0;
+    if (tid < a.s.seqs) {
+        const SeqView v = seq_view(a.s, tid, a.page_log);
+        if (v.ok && v.rows > 0) {
+            const Tiles t = tiles_of(a, v, 0, v.rows - 1);
+            n = t.end - t.first;
+        }
+    }
+    const uint32_t cost = n ? n + kPiece : 0;
+    uint32_t sum = cost;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t other = __shfl_up(sum, o);
+        if (lane >= (uint32_t)o) sum += other;
+    }
+    if (lane == 63) row.sums[tid >> 6] = sum;
+    __syncthreads();
+    uint32_t before = sum - cost, total = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < 4; ++w) {
+        if (w < tid >> 6) before += row.sums[w];
+        total += row.sums[w];
+    }
+    row.tiles[tid] = n;
+    row.before[tid] = before;
+    __syncthreads();
+    Share s;
+    s.total = uniform(total) * a.cache.kv_heads;
+    const uint32_t need = (s.total + a.shared - 1) / a.shared;
+    s.quota = need < 4 ? 4 : (need + 3) & ~3u;
+    return s;
+}
+
+template <int NJ, int RT>
+__global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_shared(Args a) {
+    extern __shared__ float sh[];
+    __shared__ Row row;
+    __shared__ uint32_t found;
+    const uint32_t tid = threadIdx.x, wave = uniform(tid >> 6), H = a.cache.kv_heads;
+    const Share s = share_out(a, row);
+    const uint32_t start = blockIdx.x * s.quota, end = start + s.quota < s.total ? start + s.quota : s.total;
+    if (start >= end) return;
+    const uint32_t first = row.before[tid] * H;
+    if (row.tiles[tid] && first <= start && start - first < (row.tiles[tid] + kPiece) * H) found = tid;
+    __syncthreads();
+    uint32_t b = uniform(found);
+    for (uint32_t at = start; at < end;) {
+        const uint32_t n = uniform(row.tiles[b]), cost = n + kPiece, in = at - uniform(row.before[b]) * H, h = in / cost, tile = in - h * cost;
+        const uint32_t stop = at + (cost - tile) < end ? at + (cost - tile) : end;
+        if (tile < n) {
+            const uint32_t there = tile + (stop - at) < n ? stop - at : n - tile;
+            const SeqView v = seq_view(a.s, b, a.page_log);
+            const uint32_t t_first = tiles_of(a, v, 0, v.rows - 1).first + tile;
+            attend_part<NJ, RT, 4>(a, sh, v, b, h, t_first, t_first + there, ask_pages(a, b, t_first + wave, 4), there == n,
+                                   ((size_t)blockIdx.x * 2 + (at == start ? 0 : 1)) * a.rows_most);
+            __syncthreads();
+        }
+        at = stop;
+        if (at < end && in + (cost - tile) == cost * H)  // the last head
+            do ++b;
+            while (uniform(row.tiles[b]) == 0);
+    }
+}
+
+// A workgroup: one row of one sequence and head.  Threads hold four dimensions each; what is left of 256 takes parts
+// in turn, and LDS adds them up.
 static const uint32_t kMostSplits = 256;
 __global__ __launch_bounds__(kBlock) void k_attend_join(Args a) {
-    __shared__ float weight[kMostSplits];
+    __shared__ Row row;
+    __shared__ float weight[2 * kMostSplits + 8];
     __shared__ float red[4], red_l[4];
     __shared__ v4f sums[kBlock];
     const uint32_t r = blockIdx.x, h = blockIdx.y, b = blockIdx.z, d = a.cache.head_dim, H = a.cache.kv_heads, tid = threadIdx.x;
+    // where the parts of the row lie: the first, the others from `next` on, `stride` apart
+    uint32_t used;
+    size_t part0, next, stride;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
         if (r == 0) not_a_number(a, b, h);
         return;
     }
     if (r >= (uint32_t)v.rows * a.group) return;
-    const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / kRows * kRows);
-    const uint32_t each = part_of(a, tiles), used = (tiles.end - tiles.first + each - 1) / each;
-    const size_t part0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
-    const float2 ml = tid < used ? a.parts_ml[part0 + (size_t)tid * a.rows_most] : make_float2(-kInf, 0.0f);
-    float top = ml.x;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (a.shared) {
+        const Share s = share_out(a, row);
+        const uint32_t n = uniform(row.tiles[b]), from = uniform(row.before[b]) * H + h * (n + kPiece);
+        const uint32_t w0 = from / s.quota, w1 = n ? (from + n - 1) / s.quota : w0;
+        if (n && w0 == w1) return;  // done where it lies
+        used = n ? w1 - w0 + 1 : 0;
+        part0 = ((size_t)w0 * 2 + (from == w0 * s.quota ? 0 : 1)) * a.rows_most + r;
+        next = (size_t)(w0 + 1) * 2 * a.rows_most + r;
+        stride = 2 * (size_t)a.rows_most;
+    } else {
+        const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / kRows * kRows);
+        const uint32_t each = part_of(a, tiles);
+        used = (tiles.end - tiles.first + each - 1) / each;
+        part0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
+        next = part0 + a.rows_most;
+        stride = a.rows_most;
+    }
+    auto part = [&](uint32_t s) -> size_t { return s ? next + (s - 1) * stride : part0; };
+    float top = -kInf;
+    for (uint32_t s = tid; s < used; s += kBlock) {
+        const float m = a.parts_ml[part(s)].x;
+        weight[s] = m;
+        top = fmaxf(top, m);
+    }
+    top = wave_max(top);
     if ((tid & 63) == 0) red[tid >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float ref = top == -kInf ? 0.0f : top, f = exp2_of(ml.x - ref);
-    weight[tid] = f;
-    float l = ml.y * f;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+    const float ref = top == -kInf ? 0.0f : top;
+    float l = 0.0f;
+    for (uint32_t s = tid; s < used; s += kBlock) {
+        const float f = exp2_of(weight[s] - ref);
+        weight[s] = f;
+        l += a.parts_ml[part(s)].y * f;
+    }
+    l = wave_add(l);
     if ((tid & 63) == 0) red_l[tid >> 6] = l;
     __syncthreads();
     l = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
     const uint32_t quads = d >> 2, ways = kBlock / quads, way = tid / quads, c = tid - way * quads;
     v4f sum = {0, 0, 0, 0};
     if (way < ways) {
-        const v4f* at = (const v4f*)a.parts + part0 * quads + c;
 #pragma unroll 8
-        for (uint32_t s = way; s < used; s += ways) sum += at[(size_t)s * a.rows_most * quads] * weight[s];
+        for (uint32_t s = way; s < used; s += ways) sum += ((const v4f*)a.parts)[part(s) * quads + c] * weight[s];
     }
     sums[tid] = sum;
     __syncthreads();
@@ -599,8 +726,8 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     if (tiles.first < tiles.end) {
         uint32_t page[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = page_of(a, b, tiles.first * kTile + 16 * i, len);
-        if (tid < 4) my_page = page_of(a, b, (tiles.first + 1) * kTile + 16 * tid, len);
+        for (int i = 0; i < 4; ++i) page[i] = page_of(a, b, tiles.first * kTile + 16 * i);
+        if (tid < 4) my_page = page_of(a, b, (tiles.first + 1) * kTile + 16 * tid);
         fetch(tiles.first, page);
     }
     for (uint32_t t = tiles.first; t < tiles.end; ++t) {
@@ -609,7 +736,7 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         if (tid < 4) pages[buf][tid] = my_page;
         __syncthreads();
         if (t + 1 < tiles.end) {
-            if (tid < 4) my_page = page_of(a, b, (t + 2) * kTile + 16 * tid, len);
+            if (tid < 4) my_page = page_of(a, b, (t + 2) * kTile + 16 * tid);
             fetch(t + 1, pages[buf]);
         }
         const char* kb = lds + buf * L::bytes;
@@ -726,9 +853,17 @@ uint32_t tiles_for(uint32_t len) { return len ? (uint32_t)div_up(len, kTile) : 1
 template <int NJ, int RT, int W>
 int launch_few(const Args& a, hipStream_t stream) {
     const size_t lds = FewLds<NJ, RT, W>::bytes(a.rows_most);
-    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, W>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_few<NJ, RT, W>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(64 * W), lds, stream, a);
-    if (a.splits > 1) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
+    if constexpr (W == 4) {
+        if (a.shared) {
+            if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_shared<NJ, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            hipLaunchKernelGGL((k_attend_shared<NJ, RT>), dim3(a.shared), dim3(kBlock), lds, stream, a);
+        }
+    }
+    if (!a.shared) {
+        if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, W>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL((k_attend_few<NJ, RT, W>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(64 * W), lds, stream, a);
+    }
+    if (a.splits > 1 || a.shared) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -745,9 +880,23 @@ int launch_many(const Args& a, hipStream_t stream) {
 
 template <int NJ>
 int launch(const Args& a, hipStream_t stream) {
-    if (a.rows_most <= 16) return a.splits == 1 ? launch_few<NJ, 1, 8>(a, stream) : launch_few<NJ, 1, 4>(a, stream);
+    if (a.rows_most <= 16) return a.splits == 1 && !a.shared && !a.crowd ? launch_few<NJ, 1, 8>(a, stream) : launch_few<NJ, 1, 4>(a, stream);
     if (few_rows(a.rows_most)) return launch_few<NJ, 2, 4>(a, stream);
     return a.cache.head_dim > 64 * NJ - 32 ? launch_many<2 * NJ>(a, stream) : launch_many<2 * NJ - 1>(a, stream);
+}
+
+// Whether sequences share their workgroups out by tiles, not by parts of like size of each.  Measured, us, shared out and in parts,
+// lengths spread evenly up to the longest, 8 heads of 128: 32 sequences of 4096 39.4 and 43.8, 16 of 8000 38.5 and 43.1, 8 of
+// 30000 68 and 76, 64 of 4096 65 and 68; 100 of 3000 84 and 83 (800 pairs: not shared out); 32 of 4096 all alike 63 and 59.
+bool shared_out(uint32_t seqs, uint32_t kv_heads, uint64_t rows, uint32_t tiles) {
+    const uint64_t groups = (uint64_t)seqs * kv_heads;
+    return few_rows(rows) && seqs > 1 && seqs <= kMostShared && groups >= 64 && groups <= kWorkgroups && tiles > short_tiles(seqs, kv_heads);
+}
+size_t parts_bytes(size_t parts, uint32_t head_dim) {
+    Carver cv(nullptr, 0);
+    cv.take(parts * head_dim * sizeof(float));
+    cv.take(parts * sizeof(float2));
+    return cv.used();
 }
 
 // Rows of a sequence and head at most.
@@ -766,12 +915,9 @@ extern "C" size_t kvcache_attention_workspace_bytes(uint32_t seqs, uint32_t rows
     if (few_rows(most) && tiles <= short_tiles(seqs, kv_heads)) return 0;
     // a window makes tiles and workgroups fewer, never more
     const uint32_t splits = most_splits(seqs, kv_heads, most, tiles);
-    if (splits == 1) return 0;
-    const size_t parts = (size_t)seqs * kv_heads * splits * most;
-    Carver cv(nullptr, 0);
-    cv.take(parts * head_dim * sizeof(float));
-    cv.take(parts * sizeof(float2));
-    return cv.used();
+    size_t parts = splits == 1 ? 0 : (size_t)seqs * kv_heads * splits * most;
+    if (shared_out(seqs, kv_heads, most, tiles) && parts < 2 * (size_t)kWorkgroups * most) parts = 2 * (size_t)kWorkgroups * most;
+    return parts ? parts_bytes(parts, head_dim) : 0;
 }
 
 extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
@@ -786,7 +932,11 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     if (div_up(most, kRows) > 65535) return ZK_E_BADARG;
     // what a window lets a sequence's rows see, with a tile that it ends in
     const uint64_t seen = window ? (uint64_t)window + seqs->max_new + kTile : seqs->max_len;
-    const Split sp = split_of(seqs->seqs, cache->kv_heads, most, tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len));
+    const uint32_t tiles = tiles_for(seen < seqs->max_len ? (uint32_t)seen : seqs->max_len);
+    const Split sp = split_of(seqs->seqs, cache->kv_heads, most, tiles);
+    // what the table has room for decides whether tiles can be counted in 32 bits: the lengths are on the device
+    const bool countable = (uint64_t)seqs->seqs * cache->kv_heads * ((uint64_t)seqs->table_pages * cache->page_tokens / kTile + 2 + kPiece) < 0x7fffffffu;
+    const bool shared = countable && shared_out(seqs->seqs, cache->kv_heads, most, tiles);
     Args a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -805,10 +955,12 @@ extern "C" int kvcache_attention(const kvcache_i8* cache, const void* q, size_t 
     a.few = few_rows(most);
     a.wide = aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0;
     a.rows_most = (uint32_t)most;
-    a.splits = sp.splits;
+    a.splits = shared ? 1 : sp.splits;
     a.each = sp.each;
-    if (sp.splits > 1) {
-        const size_t parts = (size_t)seqs->seqs * cache->kv_heads * sp.splits * most;
+    a.shared = shared ? kWorkgroups : 0;
+    a.crowd = (uint64_t)seqs->seqs * cache->kv_heads >= kWorkgroups;
+    if (shared || sp.splits > 1) {
+        const size_t parts = shared ? 2 * (size_t)kWorkgroups * most : (size_t)seqs->seqs * cache->kv_heads * sp.splits * most;
         if (!ws) return ZK_E_BUFSZ;
         Carver cv(ws, ws_bytes);
         a.parts = (float*)cv.take(parts * cache->head_dim * sizeof(float));

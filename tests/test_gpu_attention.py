@@ -86,6 +86,35 @@ def test_spread_as_the_caller_says(zk, new, lens, heads, H, d):
         check(zk, cache, q, cu, lens, table, d ** -0.5, 0, max_new, max_len)
 
 
+@pytest.mark.parametrize("seqs,most_new,longest,heads,H,d,T,window", [
+    (2, 1, 3000, 2, 1, 64, 64, 0), (5, 1, 900, 4, 2, 128, 16, 0), (20, 1, 1200, 5, 1, 80, 32, 0), (33, 3, 700, 4, 4, 64, 128, 0),
+    (17, 2, 4000, 16, 1, 128, 64, 0), (9, 1, 2500, 6, 3, 256, 16, 0), (40, 1, 2300, 4, 2, 64, 16, 1500), (256, 1, 700, 1, 1, 32, 16, 0),
+    (257, 1, 650, 1, 1, 32, 16, 0), (130, 1, 2200, 4, 4, 48, 32, 0), (70, 2, 2700, 2, 1, 64, 16, 0), (64, 1, 4000, 5, 1, 128, 64, 2300), (16, 1, 5000, 8, 4, 128, 32, 0), (3, 1, 17000, 17, 1, 128, 256, 0)])
+def test_sequences_of_unlike_lengths(zk, seqs, most_new, longest, heads, H, d, T, window):
+    """Lengths from none to the longest, sequences without a row and with more rows than tokens among them."""
+    g = torch.Generator().manual_seed(seqs + longest)
+    new = torch.randint(0, most_new + 1, (seqs,), generator=g).tolist() if most_new > 1 else [1] * seqs
+    lens = [int(longest * x ** 3) for x in torch.rand(seqs, generator=g).tolist()]
+    new[0], lens[0] = most_new, longest
+    if seqs > 4:
+        new[2], lens[2], new[-1], lens[-1] = 0, 100, 1, 0
+    cache, q, cu, table, _ = make(zk, new, lens, heads, H, d, T, torch.bfloat16, seqs)
+    out, lse = check(zk, cache, q, cu, lens, table, d ** -0.5, window)
+    rc, again, alse = zk.kvcache_attention(cache, q, *device(cu, lens, table), max(new), max(lens), d ** -0.5, window=window)
+    assert torch.equal(again, out) and torch.equal(alse, lse)
+    if seqs > 4:
+        # a sequence that is refused does not disturb the others
+        bad = list(lens)
+        bad[1] = 10 ** 6
+        fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+        rc, some, slse = zk.kvcache_attention(cache, q, *device(cu, bad, table), max(new), max(lens), d ** -0.5, window=window, fault=fault)
+        rows = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+        rows[cu[1]:cu[2]] = False
+        assert rc == zk.ZK_OK and fault.item() == zk.ZK_FAULT_LENGTH and some[~rows].isnan().all()
+        # parts end elsewhere then: the same sums in another order
+        assert not some[rows].isnan().any() and torch.allclose(some[rows].float(), out[rows].float(), atol=0.25, rtol=0.02)
+
+
 @pytest.mark.parametrize("new,lens", [([3], [2]), ([40], [7]), ([2, 50, 1], [0, 3, 0]), ([1], [0]), ([33], [0])])
 def test_rows_that_see_nothing(zk, new, lens):
     """More rows than tokens: the first see no key, their output is zero and lse is -inf."""
