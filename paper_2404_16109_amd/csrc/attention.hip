@@ -14,11 +14,17 @@
 //     second's operand without a move between lanes: a lane gets the scores of tokens that lie side by side, because
 //     the rows of K are handed in that order, and V lies in the cache by dimension.
 //
-// Few rows (k_attend_few: up to 32 of a sequence and head of the cache, the query heads that share it among them): the
-// cache is read once, straight into registers, and is what bounds the call.  A wavefront takes 64 tokens at a time, four
-// wavefronts share a workgroup's part of the sequence, and `splits` workgroups the sequence; k_attend_join adds up.
-// Many rows (k_attend_many: 128 to a workgroup): codes are widened once and shared through LDS; bound by the
-// matrix cores and the exponentials.
+// Few rows (up to 32 of a sequence and head of the cache, the query heads that share it among them): the cache is read once,
+// straight into registers, a tile ahead of its use, and is what bounds the call.  A wavefront takes 64 tokens at a time: 16
+// loads of 1 KiB, so that the eight wavefronts of a CU have 128 KiB on the way.  k_attend_few: four wavefronts share a
+// workgroup's part of a sequence, `splits` workgroups the sequence, or eight wavefronts have all of a short one; k_attend_shared:
+// as many workgroups as the chip holds share all sequences; k_attend_join adds up.  Measured: one sequence of 131071
+// tokens, 8 heads of 128 (268 MB) 60 us, 4.5 TB/s, where a copy of that size reaches 4.8; one of 777 tokens 10.1 us, of which
+// 1.7 are the launch and some 6 three trips to memory, one after the other, and the CU's 64 bytes a clock.
+// Many rows (k_attend_many: 128 to a workgroup): codes are widened once and shared through LDS, a tile ahead; bound by the
+// vector ALU (per row and key some 13 of its cycles, the exponential among them, beside 8 of the matrix cores).  Row tiles
+// are taken with those that see most first, over all heads: 84 us for a prompt of 2048 tokens and 40 heads (43 GFLOP,
+// 515 TFLOP/s; head by head it was 160), 600 TFLOP/s for four such prompts.
 #include "kvcache.h"
 
 namespace zkmi {

@@ -7,6 +7,8 @@
 //
 // Bound by bytes for prompts (pages that begin are read once, others twice, the second time from the L2, and one byte of each
 // value is written), by the chain of four dependent loads for single tokens.
+// Measured: 7 prompts of up to 2048 tokens, 40 heads of 128 (235 MB) 56 us, 4.2 TB/s (read a second time and transposed by
+// two-byte loads: 88); a token of each of 32 sequences 4.5 us.
 #include "kvcache.h"
 
 namespace zkmi {

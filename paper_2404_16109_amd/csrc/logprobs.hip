@@ -12,7 +12,9 @@
 // of 64-bit keys (value, then lower index).  Where too many reach the bound (ties, rows that allow less than `top`
 // tokens, NaN) the keys are taken out one after the other instead.
 //
-// Bound by the bytes of the logits.
+// Bound by the bytes of the logits, and for 16-bit ones by the vector ALU: some 13 of its operations a value.  Measured:
+// 2048 rows of 50257 floats, 20 alternatives (412 MB) 112 us, 3.7 TB/s (a copy: 4.8); 4096 rows of 32001 bf16 95 us; 8 rows of
+// 32001, one launch, 8.4 us, the latency of a dozen dependent steps.
 #include "serve_dev.h"
 
 namespace zkmi {

@@ -8,7 +8,9 @@
 // added by one more matrix instruction whose second operand is the constant -12.  What is accumulated is three times the
 // size of the result's terms at most, so nothing is lost of 32-bit sums.  Types:
 //   ZK_F16   x as it is.            ZK_BF16  x as it is.
-//   ZK_F32   x as the sum of three bf16 (8 + 8 + 8 bits: exact), three columns.
+//   ZK_F32   x as the sum of three bf16 (8 + 8 + 8 bits: exact), three columns; where x is laid out beforehand, as the sum of
+//            two f16 (11 + 11 bits) after a power of two has brought the vector's largest to just below 2^15: what
+//            they miss is at most 2^-23 of an element or 2^-40 of the largest, a rounding's size.
 //   ZK_I16   x = 256 h + l, two columns of whole numbers below 2^8; a group's sums are below 2^20 halves, exact in 32
 //            bits, and everything after that is in 64-bit integers.
 //
@@ -16,6 +18,10 @@
 // of 128.  An instruction wants inputs 8 g .. 8 g + 7 of ONE block of 32 in lane row g, so that what it adds up belongs
 // to one group: four exchanges of lane rows transpose the 4 x 4 words.  Of a word's eight half bytes i and i + 4 come to
 // lie in one register, so x is kept in the order 0 4 1 5 2 6 3 7.
+//
+// Bound by the weights' bytes where they are many and the vectors few, by latency below some 20 MB, by LDS and the vector ALU
+// for many columns.  Measured: one vector of bf16 by 5120 x 5120 (13.5 MB) 7.9 us, by 32001 x 5120 (84 MB) 22 us, 3.8 TB/s; 8 of
+// 16-bit integers by 4096 x 11008 15.5 us; 64 of bf16 by 32001 x 5120 45 us, 465 TFLOP/s; 32 of 32 bits 55 us.
 #include "serve_dev.h"
 
 namespace zkmi {
@@ -34,11 +40,16 @@ static const uint32_t kManyOutputs = 10240, kBlocksOfFew = 6;
 // 32 of 32 bits by 32001 x 5120 62 and 86.
 static const uint32_t kWide = 16384;
 
+// 32-bit floats where x is laid out by k_w4_columns, as two 16-bit ones.
+static const int kPair = 100;
+
 template <int DT>
 struct Kind {
-    static constexpr int parts = DT == ZK_F32 ? 3 : DT == ZK_I16 ? 2 : 1;  // columns of a vector
+    static constexpr bool wide = DT == ZK_F32 || DT == kPair;              // 32 bits to a value of x
+    static constexpr int parts = DT == ZK_F32 ? 3 : DT == ZK_I16 || DT == kPair ? 2 : 1;  // columns of a vector
     static constexpr int vectors = 16 / parts;                             // vectors of a call's 16 columns
-    static constexpr bool f16 = DT == ZK_F16;
+    static constexpr bool f16 = DT == ZK_F16 || DT == kPair;
+    static constexpr int out = DT == kPair ? ZK_F32 : DT;
 };
 
 template <int DT>
@@ -70,19 +81,19 @@ __device__ __forceinline__ void transpose_rows(v4u& r) {
 // Inputs k .. k+7 of a vector as they lie in memory, and as its columns' operands, in the order 0 4 1 5 2 6 3 7.
 template <int DT>
 struct Eight {
-    static constexpr int words = DT == ZK_F32 ? 2 : 1;
+    static constexpr int words = Kind<DT>::wide ? 2 : 1;
     v4u r[words];
 };
 template <int DT>
 __device__ __forceinline__ Eight<DT> load_eight(const void* x, size_t at) {
     Eight<DT> e;
-    const v4u* p = (const v4u*)((const char*)x + at * (DT == ZK_F32 ? 4 : 2));
+    const v4u* p = (const v4u*)((const char*)x + at * (Kind<DT>::wide ? 4 : 2));
 #pragma unroll
     for (int i = 0; i < Eight<DT>::words; ++i) e.r[i] = p[i];
     return e;
 }
 template <int DT>
-__device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<DT>::parts]) {
+__device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<DT>::parts], float up = 1.0f) {
     if constexpr (DT == ZK_F16 || DT == ZK_BF16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -98,6 +109,14 @@ __device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<D
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) out[p][i] = part(i, p) | (part(i + 4, p) << 16);
+    } else if constexpr (DT == kPair) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = bits_float(x.r[0][i]) * up, b = bits_float(x.r[1][i]) * up;
+            const uint32_t ah = half_bits<ZK_F16>(a), bh = half_bits<ZK_F16>(b);
+            out[0][i] = ah | (bh << 16);
+            out[1][i] = half_bits<ZK_F16>(a - half_of<ZK_F16>(ah, 0)) | ((uint32_t)half_bits<ZK_F16>(b - half_of<ZK_F16>(bh, 0)) << 16);
+        }
     } else {
         float r[8];
 #pragma unroll
@@ -146,7 +165,7 @@ __host__ __device__ __forceinline__ uint32_t threads_across(uint32_t vectors) { 
 // LDS where all of it fits there (STAGED), else from `xf`, where k_w4_columns has laid out the operands [k / 8][16]: a
 // wavefront then reads a kilobyte of them for each instruction, out of the L2, and nothing waits for anything in the loop.
 template <int DT, bool STAGED, int GL>
-__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, size_t rows,
+__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, const float2* powers, size_t rows,
                                                         const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
                                                         float unit2) {
     constexpr int parts = Kind<DT>::parts;
@@ -314,17 +333,41 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
                 for (int p = 0; p < parts; ++p)
 #pragma unroll
                     for (int v = 0; v < kWaves; ++v) sum += red[(v * 16 + m * parts + p) * 16 + o];
-                store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
+                store_one<Kind<DT>::out>(y, (m0 + m) * ystride + n0 + o, DT == kPair ? sum * unit2 * powers[m0 + m].y : sum * unit2);
             }
         }
     }
+}
+
+// The power of two that brings a vector's largest to just below 2^15, and the one that takes it back; NaN if a value is not
+// finite.  Workgroup: one vector.
+__global__ __launch_bounds__(kBlock) void k_w4_powers(float2* powers, const float* x, size_t xstride, uint32_t k) {
+    __shared__ uint32_t most[4];
+    const uint32_t* row = (const uint32_t*)x + blockIdx.x * xstride;
+    uint32_t bits = 0;
+    for (uint32_t i = threadIdx.x * 4; i < k; i += kBlock * 4) {
+        const v4u r = *(const v4u*)(row + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bits = (r[e] & 0x7fffffffu) > bits ? r[e] & 0x7fffffffu : bits;
+    }
+    bits = wave_max(bits);
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = bits;
+    __syncthreads();
+    if (threadIdx.x) return;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) bits = most[w] > bits ? most[w] : bits;
+    // 2^e > the largest; a vector of zeros, or of less than 2^-100, is scaled as if that were its largest
+    int e = (int)(bits >> 23) - 126;
+    e = e < -100 ? -100 : e;
+    const bool fine = bits < 0x7f800000u;
+    powers[blockIdx.x] = fine ? make_float2(ldexpf(1.0f, 15 - e), ldexpf(1.0f, e - 15)) : make_float2(__builtin_nanf(""), __builtin_nanf(""));
 }
 
 // x as operands: xf[block][k / 8][columns of a block], zero behind the last column and the last input (up to a step's end);
 // with sums, -12 times the sum over each group of inputs, [block][group][columns of a block].  A block has `vectors`
 // vectors.  Workgroup: one group, or eight of 16 bytes where nobody asks for sums.
 template <int DT>
-__global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, const void* x, size_t xstride, size_t rows, uint32_t k,
+__global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, const float2* powers, const void* x, size_t xstride, size_t rows, uint32_t k,
                                                        uint32_t k8_all, uint32_t columns, uint32_t vectors, uint32_t group_log) {
     constexpr int parts = Kind<DT>::parts;
     const uint32_t block = blockIdx.y, per = sums ? 1u << (group_log - 3) : 8;  // pieces of eight inputs of a workgroup, 4, 8 or 16
@@ -334,7 +377,8 @@ __global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, con
         v4u c[parts];
 #pragma unroll
         for (int p = 0; p < parts; ++p) c[p] = v4u{0, 0, 0, 0};
-        if (m < vectors && m0 + m < rows && k8 * 8 < k) columns_of<DT>(load_eight<DT>(x, (m0 + m) * xstride + k8 * 8), c);
+        if (m < vectors && m0 + m < rows && k8 * 8 < k)
+            columns_of<DT>(load_eight<DT>(x, (m0 + m) * xstride + k8 * 8), c, DT == kPair ? powers[m0 + m].x : 1.0f);
 #pragma unroll
         for (int p = 0; p < parts; ++p) {
             const uint32_t col = m * parts + p;
@@ -361,7 +405,7 @@ struct ManyLds {
     static constexpr uint32_t all = 2 * bytes > meet ? 2 * bytes : meet;
 };
 template <int DT, int CT, int NT, int GL>
-__global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, size_t rows, const uint8_t* codes,
+__global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, const float2* powers, size_t rows, const uint8_t* codes,
                                                  const uint16_t* scales, uint32_t n, uint32_t k, uint32_t vectors, float unit2) {
     constexpr uint32_t group_log = GL;
     using L = ManyLds<CT, NT>;
@@ -531,7 +575,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
             float sum = 0.0f;
 #pragma unroll
             for (int p = 0; p < Kind<DT>::parts; ++p) sum += tile[(m * Kind<DT>::parts + p) * N + o];
-            store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
+            store_one<Kind<DT>::out>(y, (m0 + m) * ystride + n0 + o, DT == kPair ? sum * unit2 * powers[m0 + m].y : sum * unit2);
         }
     }
 }
@@ -556,7 +600,7 @@ struct Way {
     uint32_t blocks, vectors;   // of columns, and the vectors of each
     uint32_t tiles;             // of 16 columns of a block; 1: few columns
     uint32_t k8;                // pieces of eight inputs, whole steps
-    size_t operands, sums;      // in the workspace, bytes
+    size_t operands, sums, powers;  // in the workspace, bytes
 };
 template <int DT>
 Way way_of(size_t rows, uint32_t n, uint32_t k) {
@@ -567,7 +611,7 @@ Way way_of(size_t rows, uint32_t n, uint32_t k) {
         w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
         w.blocks = (uint32_t)div_up(rows, w.vectors);
-        w.staged = w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
+        w.staged = DT != kPair && w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
     } else {
         // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
         const size_t most = 96 / parts;
@@ -577,6 +621,7 @@ Way way_of(size_t rows, uint32_t n, uint32_t k) {
         w.blocks = (uint32_t)div_up(rows, v);
     }
     if (!w.staged) w.operands = (size_t)w.blocks * w.k8 * w.tiles * 256;
+    if (DT == kPair) w.powers = rows * sizeof(float2);
     if (w.tiles > 1) w.sums = (size_t)w.blocks * (w.k8 / 4) * w.tiles * 64;  // of the shortest groups
     return w;
 }
@@ -584,6 +629,7 @@ size_t way_bytes(const Way& w) {
     Carver cv(nullptr, 0);
     cv.take(w.operands);
     cv.take(w.sums);
+    cv.take(w.powers);
     return w.operands ? cv.used() : 0;
 }
 
@@ -602,28 +648,33 @@ struct Call {
 };
 
 template <int DT, int CT, int NT, int GL>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
     const size_t lds = ManyLds<CT, NT>::all;
     auto* kernel = k_w4_many<DT, CT, NT, GL>;
     if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, c.rows,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, powers, c.rows,
                        c.codes, c.scales, c.n, c.k, w.vectors, c.unit * 2.0f);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
 template <int DT, int CT, int NT>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
-    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums)
-                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums);
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
+    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums, powers) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums, powers)
+                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums, powers);
 }
 template <int DT, int CT>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
-    return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums) : run_many<DT, CT, 1>(c, w, xf, sums);
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
+    return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums, powers) : run_many<DT, CT, 1>(c, w, xf, sums, powers);
 }
 
 template <int DT>
+int run(const Call& c);
+template <int DT>
 int run(const Call& c) {
     const Way w = way_of<DT>(c.rows, c.n, c.k);
+    if constexpr (DT == ZK_F32)
+        if (!w.staged) return run<kPair>(c);
+    float2* powers = nullptr;
     v4u* xf = nullptr;
     float* sums = nullptr;
     if (w.operands) {
@@ -631,9 +682,12 @@ int run(const Call& c) {
         Carver cv(c.ws, c.ws_bytes);
         xf = (v4u*)cv.take(w.operands);
         if (w.sums) sums = (float*)cv.take(w.sums);
-        if (cv.overflow() || !xf || (w.sums && !sums)) return ZK_E_BUFSZ;
+        if (w.powers) powers = (float2*)cv.take(w.powers);
+        if (cv.overflow() || !xf || (w.sums && !sums) || (w.powers && !powers)) return ZK_E_BUFSZ;
+        if (w.powers)
+            hipLaunchKernelGGL(k_w4_powers, dim3((unsigned)c.rows), dim3(kBlock), 0, c.stream, powers, (const float*)c.x, c.xstride, c.k);
         const uint32_t per = sums ? 1u << (c.group_log - 3) : 8;
-        hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, c.x, c.xstride,
+        hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, powers, c.x, c.xstride,
                            c.rows, c.k, w.k8, w.tiles * 16, w.vectors, c.group_log);
         ZK_HIP_TRY(hipGetLastError());
     }
@@ -645,12 +699,12 @@ int run(const Call& c) {
         auto* kernel = w.staged ? (c.group_log == 5 ? k_w4_few<DT, true, 5> : c.group_log == 6 ? k_w4_few<DT, true, 6> : k_w4_few<DT, true, 7>)
                                 : (c.group_log == 5 ? k_w4_few<DT, false, 5> : c.group_log == 6 ? k_w4_few<DT, false, 6> : k_w4_few<DT, false, 7>);
         if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, c.rows, c.codes, c.scales, c.n,
+        hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, powers, c.rows, c.codes, c.scales, c.n,
                            c.k, c.unit * 2.0f);
         ZK_HIP_TRY(hipGetLastError());
         return ZK_OK;
     }
-    return w.tiles == 2 ? run_many<DT, 2>(c, w, xf, sums) : w.tiles == 4 ? run_many<DT, 4>(c, w, xf, sums) : run_many<DT, 6>(c, w, xf, sums);
+    return w.tiles == 2 ? run_many<DT, 2>(c, w, xf, sums, powers) : w.tiles == 4 ? run_many<DT, 4>(c, w, xf, sums, powers) : run_many<DT, 6>(c, w, xf, sums, powers);
 }
 
 bool inputs_ok(size_t k) { return k >= 32 && k <= ((size_t)1 << 20) && k % 32 == 0; }
@@ -675,7 +729,7 @@ size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs
 extern "C" size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k) {
     if (!dtype_bytes(dtype) || rows == 0 || rows > kMostRows || !inputs_ok(k)) return 0;
     switch (dtype) {
-        case ZK_F32: return workspace<ZK_F32>(rows, (uint32_t)k);
+        case ZK_F32: return way_of<ZK_F32>(rows, 1, (uint32_t)k).staged ? 0 : workspace<kPair>(rows, (uint32_t)k);
         case ZK_F16: return workspace<ZK_F16>(rows, (uint32_t)k);
         case ZK_BF16: return workspace<ZK_BF16>(rows, (uint32_t)k);
         default: return workspace<ZK_I16>(rows, (uint32_t)k);
