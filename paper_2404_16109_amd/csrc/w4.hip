@@ -21,7 +21,7 @@
 //
 // Bound by the weights' bytes where they are many and the vectors few, by latency below some 20 MB, by LDS and the vector ALU
 // for many columns.  Measured: one vector of bf16 by 5120 x 5120 (13.5 MB) 7.9 us, by 32001 x 5120 (84 MB) 22 us, 3.8 TB/s; 8 of
-// 16-bit integers by 4096 x 11008 15.5 us; 64 of bf16 by 32001 x 5120 45 us, 465 TFLOP/s; 32 of 32 bits 55 us.
+// 16-bit integers by 4096 x 11008 15.5 us; 64 of bf16 by 32001 x 5120 45 us, 465 TFLOP/s; 32 of 32 bits 48 us.
 #include "serve_dev.h"
 
 namespace zkmi {
@@ -36,8 +36,8 @@ static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of colu
 // vectors of bf16 by 4096 x 11008 18 and 42, by 8192 x 4096 (20 of them) 18.2 and 20.8, by 13824 x 5120 30 and 26, by 32001 x
 // 5120 63 and 39; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x 4096 28 and 25.
 static const uint32_t kManyOutputs = 10240, kBlocksOfFew = 6;
-// Outputs from which a workgroup of the kernel for many columns has 128, not 64: 64 by 13824 x 5120 42 us with 128 and 33 with 64,
-// 32 of 32 bits by 32001 x 5120 62 and 86.
+// Outputs from which a workgroup of the kernel for many columns has 128, not 64.  Measured, 128 and 64, us: 64 vectors of bf16 by
+// 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 50 and 57.
 static const uint32_t kWide = 16384;
 
 // 32-bit floats where x is laid out by k_w4_columns, as two 16-bit ones.
@@ -340,22 +340,23 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
 }
 
 // The power of two that brings a vector's largest to just below 2^15, and the one that takes it back; NaN if a value is not
-// finite.  Workgroup: one vector.
-__global__ __launch_bounds__(kBlock) void k_w4_powers(float2* powers, const float* x, size_t xstride, uint32_t k) {
-    __shared__ uint32_t most[4];
+// finite.  Workgroup: one vector, all of a usual one on its way at once (256 threads: 4.6 us for 5120 inputs, in turn).
+static const int kPowers = 1024;
+__global__ __launch_bounds__(kPowers) void k_w4_powers(float2* powers, const float* x, size_t xstride, uint32_t k) {
+    __shared__ uint32_t most[kPowers / 64];
     const uint32_t* row = (const uint32_t*)x + blockIdx.x * xstride;
     uint32_t bits = 0;
-    for (uint32_t i = threadIdx.x * 4; i < k; i += kBlock * 4) {
-        const v4u r = *(const v4u*)(row + i);
+    for (uint32_t i = threadIdx.x * 4; i < k; i += kPowers * 8) {
+        const v4u r0 = *(const v4u*)(row + i), r1 = *(const v4u*)(row + (i + kPowers * 4 < k ? i + kPowers * 4 : i));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bits = (r[e] & 0x7fffffffu) > bits ? r[e] & 0x7fffffffu : bits;
+        for (int e = 0; e < 4; ++e) bits = max(bits, max(r0[e] & 0x7fffffffu, r1[e] & 0x7fffffffu));
     }
     bits = wave_max(bits);
     if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = bits;
     __syncthreads();
     if (threadIdx.x) return;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) bits = most[w] > bits ? most[w] : bits;
+    for (int w = 0; w < kPowers / 64; ++w) bits = max(bits, most[w]);
     // 2^e > the largest; a vector of zeros, or of less than 2^-100, is scaled as if that were its largest
     int e = (int)(bits >> 23) - 126;
     e = e < -100 ? -100 : e;
@@ -685,7 +686,7 @@ int run(const Call& c) {
         if (w.powers) powers = (float2*)cv.take(w.powers);
         if (cv.overflow() || !xf || (w.sums && !sums) || (w.powers && !powers)) return ZK_E_BUFSZ;
         if (w.powers)
-            hipLaunchKernelGGL(k_w4_powers, dim3((unsigned)c.rows), dim3(kBlock), 0, c.stream, powers, (const float*)c.x, c.xstride, c.k);
+            hipLaunchKernelGGL(k_w4_powers, dim3((unsigned)c.rows), dim3(kPowers), 0, c.stream, powers, (const float*)c.x, c.xstride, c.k);
         const uint32_t per = sums ? 1u << (c.group_log - 3) : 8;
         hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, powers, c.x, c.xstride,
                            c.rows, c.k, w.k8, w.tiles * 16, w.vectors, c.group_log);
