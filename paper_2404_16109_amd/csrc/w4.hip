@@ -33,11 +33,12 @@ static const uint32_t kStageHalves = 32768;        // 64 KiB of x in LDS
 static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of columns
 // More columns than 16: blocks of 16 that each read the weights again (out of the caches), or the kernel for many columns, whose
 // workgroups have 64 or 128 outputs and are too few for a short matrix.  Measured, the first against the second, us: 32
-// vectors of bf16 by 4096 x 11008 18 and 42, by 8192 x 4096 (20 of them) 18.2 and 20.8, by 13824 x 5120 30 and 26, by 32001 x
-// 5120 63 and 39; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x 4096 28 and 25.
-static const uint32_t kManyOutputs = 10240, kBlocksOfFew = 6;
+// vectors of bf16 by 4096 x 11008 18.7 and 34.8, by 5120 x 5120 15.0 and 18.7, by 8192 x 4096 18.4 and 16.2, by 9000 x 5120 (24
+// of them) 23.2 and 19.3, by 13824 x 5120 30 and 19.5; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x
+// 4096 28 and 25.
+static const uint32_t kManyOutputs = 8192, kBlocksOfFew = 6;
 // Outputs from which a workgroup of the kernel for many columns has 128, not 64.  Measured, 128 and 64, us: 64 vectors of bf16 by
-// 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 50 and 57.
+// 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 48 and 55.
 static const uint32_t kWide = 16384;
 
 // 32-bit floats where x is laid out by k_w4_columns, as two 16-bit ones.
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, con
 // ---- many columns ----------------------------------------------------------------------------------------------------
 
 // Workgroup: 64 NT outputs by 16 CT columns, chunks of two steps.  Wavefront w: outputs 16 NT (w mod 4) .., step w / 4 of a
-// chunk.  Operands and sums come from k_w4_columns into LDS, one chunk ahead.
+// chunk.  Operands and sums come from k_w4_columns through registers, one or two chunks ahead, into LDS.
 template <int CT, int NT>
 struct ManyLds {
     static constexpr uint32_t C = 16 * CT, N = 64 * NT, x = 32 * C * 16, sums = 8 * C * 4, scales = 8 * N * 2, bytes = x + sums + scales;
@@ -422,42 +423,50 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
     const Buffer operands = buffer_of(xf + (size_t)block * k8_all * C, (size_t)k8_all * C * 16);
     const Buffer offsets = buffer_of(sums + (size_t)block * all_groups * C, (size_t)all_groups * C * 4);
     const Buffer factors = buffer_of(scales + (size_t)n0 * groups, (size_t)(n - n0 < N ? n - n0 : N) * groups * 2);
-    v4u xr[CT];
-    float br[2];
-    uint16_t sr[NT];
-    auto ask = [&](uint32_t chunk) {
+    struct Load {
+        v4u x[CT];
+        float b[2];
+        uint16_t s[NT];
+    };
+    // Chunks under way ahead of the one at work.  Two and one, us, 32001 x 5120: 32 vectors of bf16 33.3 and 38.5, 64 45.6 and
+    // 44.7 (groups of 32: 66 and 50, registers spill), 32 of 32 bits 49.9 and 48.3: with four tiles the work is the longer part.
+    constexpr int D = CT <= 2 ? 2 : 1;
+    Load load[D];
+    auto ask = [&](Load& to, uint32_t chunk) {
 #pragma unroll
-        for (int i = 0; i < CT; ++i) xr[i] = load16(operands, (chunk * 32 * C + tid + 512 * i) * 16);
+        for (int i = 0; i < CT; ++i) to.x[i] = load16(operands, (chunk * 32 * C + tid + 512 * i) * 16);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            br[i] = bits_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(offsets, (int)((chunk * each * C + tid + 512 * i) * 4), 0, 0));
+            to.b[i] = bits_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(offsets, (int)((chunk * each * C + tid + 512 * i) * 4), 0, 0));
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const uint32_t p = tid + 512 * i, gr = chunk * each + p / N;
-            sr[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(factors, (int)(gr < groups ? (p % N * groups + gr) * 2 : kNowhere), 0, 0);
+            to.s[i] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(factors, (int)(gr < groups ? (p % N * groups + gr) * 2 : kNowhere), 0, 0);
         }
     };
-    auto put = [&](uint32_t buf) {
+    auto put = [&](const Load& from, uint32_t buf) {
         char* at = lds + buf * L::bytes;
 #pragma unroll
-        for (int i = 0; i < CT; ++i) ((v4u*)at)[tid + 512 * i] = xr[i];
+        for (int i = 0; i < CT; ++i) ((v4u*)at)[tid + 512 * i] = from.x[i];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (tid + 512 * i < each * C) ((float*)(at + L::x))[tid + 512 * i] = br[i];
+            if (tid + 512 * i < each * C) ((float*)(at + L::x))[tid + 512 * i] = from.b[i];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
-            if (tid + 512 * i < each * N) ((uint16_t*)(at + L::x + L::sums))[tid + 512 * i] = sr[i];
+            if (tid + 512 * i < each * N) ((uint16_t*)(at + L::x + L::sums))[tid + 512 * i] = from.s[i];
     };
     Row row[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) row[t] = row_of((nw * NT + t) * 16 + i16, k, g);
     const Buffer weights = weights_of(codes, n, k, n0, N);
-    v4u w[2][NT];
-    ask(0);
+    v4u w[D][NT];
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+    for (int p = 0; p < D; ++p) {
+        ask(load[p], p);
 #pragma unroll
         for (int t = 0; t < NT; ++t) w[p][t] = fetch(weights, row[t], kw + 2 * p);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 
     v4f total[NT][CT];
     int64_t itotal[NT][CT][2];
@@ -468,19 +477,21 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
             total[t][c] = v4f{0, 0, 0, 0};
             itotal[t][c][0] = itotal[t][c][1] = 0;
         }
-    for (uint32_t chunk = 0; chunk < chunks; ++chunk) {
-        const uint32_t buf = chunk & 1;
-        put(buf);
+    auto work = [&](uint32_t chunk, const int buf) {
+        put(load[buf % D], buf);
         __syncthreads();
-        if (chunk + 1 < chunks) ask(chunk + 1);
+        ask(load[buf % D], chunk + D);
         v4u r[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            r[t] = w[0][t];
-            w[0][t] = w[1][t];
-            w[1][t] = fetch(weights, row[t], (chunk + 2) * 2 + kw);
-            transpose_rows(r[t]);
+            // moved, not renamed: the next load's registers are then the loop's own, and nothing waits for it at the loop's end
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm("v_mov_b32 %0, %1" : "=v"(r[t][i]) : "v"(w[buf % D][t][i]));
+            w[buf % D][t] = fetch(weights, row[t], (chunk + D) * 2 + kw);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) transpose_rows(r[t]);
         const char* at = lds + buf * L::bytes;
         const v4u* xs = (const v4u*)at + (kw * 16 + g) * C + i16;
         const float* bs = (const float*)(at + L::x) + 4 * g;
@@ -524,6 +535,11 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
                 }
             }
         }
+    };
+    // in pairs, without a question between them (what is behind the last chunk is zeros), so that a wait names its own loads
+    for (uint32_t chunk = 0; chunk < chunks; chunk += 2) {
+        work(chunk, 0);
+        work(chunk + 1, 1);
     }
 
     // the two halves of the inputs, then the columns of a vector
