@@ -31,7 +31,10 @@ def make(n, k, group, seed):
 
 SHAPES = [(1, 1, 32, 32), (1, 17, 64, 128), (2, 16, 160, 128), (3, 100, 96, 64), (5, 33, 1024, 32), (6, 31, 1056, 128), (8, 48, 2080, 64),
           (9, 15, 4128, 32), (16, 129, 512, 128), (17, 64, 1312, 64), (33, 20, 17440, 128), (70, 65, 544, 32), (1, 5000, 64, 64),
-          (40, 300, 2048, 128), (130, 257, 1184, 64)]
+          (40, 300, 2048, 128), (130, 257, 1184, 64),
+          # many outputs: two, four and six tiles of columns, 64 and 128 outputs to a workgroup, one to five chunks of inputs
+          (17, 8200, 160, 64), (31, 8199, 544, 32), (32, 9000, 1056, 128), (18, 16500, 416, 64), (25, 16390, 544, 128), (60, 8193, 672, 64),
+          (33, 16400, 96, 32), (50, 16450, 1184, 128), (90, 8200, 288, 64), (70, 16385, 672, 32)]
 
 
 @pytest.mark.parametrize("rows,n,k,group", SHAPES)
