@@ -25,6 +25,7 @@
 // vector ALU (per row and key some 13 of its cycles, the exponential among them, beside 8 of the matrix cores).  Row tiles
 // are taken with those that see most first, over all heads: 84 us for a prompt of 2048 tokens and 40 heads (43 GFLOP,
 // 515 TFLOP/s; head by head it was 160), 600 TFLOP/s for four such prompts.
+#include "attend_pieces.h"
 #include "kvcache.h"
 
 namespace zkmi {
@@ -679,11 +680,11 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     uint32_t k_run[PIECES], k_at[PIECES], v_run[PIECES], v_at[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const uint32_t p = tid + kBlock * i < 128 * DT ? tid + kBlock * i : tid, slot = p / (2 * DT), c = p % (2 * DT) * 16, dim = p >> 2;
-        k_run[i] = slot >> 4;
-        k_at[i] = (slot & 15) * d + (c < d ? c : 0);
-        v_run[i] = p & 3;
-        v_at[i] = (dim < d ? dim : 0) << a.page_log;
+        const AttendPiece p = attend_piece<DT>(tid, kBlock, i);
+        k_run[i] = p.slot >> 4;
+        k_at[i] = (p.slot & 15) * d + (16 * p.c < d ? 16 * p.c : 0);
+        v_run[i] = p.run;
+        v_at[i] = (p.dim < d ? p.dim : 0) << a.page_log;
     }
     v4u kr[PIECES], vr[PIECES];
     float my_exp = 0.0f;  // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens
@@ -709,14 +710,15 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         char* vb = kb + L::k_bytes;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t p = tid + kBlock * i, slot = p / (2 * DT), c = p % (2 * DT), x = slot & 31;
-            if (p >= 128 * DT) continue;
+            if (!attend_piece_kept<DT>(tid, kBlock, i)) continue;
+            const AttendPiece p = attend_piece<DT>(tid, kBlock, i);
+            const uint32_t x = p.slot & 31;
             // the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
-            const uint32_t row = (slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3);
-            v8h* k16 = (v8h*)(kb + row * L::krow + c * 32);
+            const uint32_t row = (p.slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3);
+            v8h* k16 = (v8h*)(kb + row * L::krow + p.c * 32);
             k16[0] = widen(kr[i][0], kr[i][1]);
             k16[1] = widen(kr[i][2], kr[i][3]);
-            v8h* v16 = (v8h*)(vb + (p >> 2) * L::vrow + (p & 3) * 32);
+            v8h* v16 = (v8h*)(vb + p.dim * L::vrow + p.run * 32);
             v16[0] = widen(vr[i][0], vr[i][1]);
             v16[1] = widen(vr[i][2], vr[i][3]);
         }
