@@ -37,6 +37,10 @@ static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of colu
 // of them) 23.2 and 19.3, by 13824 x 5120 30 and 19.5; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x
 // 4096 28 and 25.
 static const uint32_t kManyOutputs = 8192, kBlocksOfFew = 6;
+// What a CU has of LDS.  The kernel for few columns keeps the scales of all groups there, 32 bytes to a group: of more inputs than
+// 163840 (groups of 32), 327680 (64) or 655360 (128) a call of whatever rows goes to the kernel for many columns, which keeps
+// those of a chunk.
+static const size_t kMostLds = 163840;
 // Outputs from which a workgroup of the kernel for many columns has 128, not 64.  Measured, 128 and 64, us: 64 vectors of bf16 by
 // 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 48 and 55.
 static const uint32_t kWide = 16384;
@@ -619,12 +623,14 @@ struct Way {
     uint32_t k8;                // pieces of eight inputs, whole steps
     size_t operands, sums, powers;  // in the workspace, bytes
 };
+size_t scales_bytes(uint32_t k8, uint32_t group_log) { return (size_t)(k8 >> (group_log - 3)) * 32; }  // of 16 outputs
 template <int DT>
-Way way_of(size_t rows, uint32_t n, uint32_t k) {
+Way way_of(size_t rows, uint32_t n, uint32_t k, uint32_t group_log) {
     constexpr uint32_t parts = Kind<DT>::parts;
     Way w = {};
     w.k8 = (uint32_t)align_up(k, kStep) / 8;
-    if (rows <= (size_t)Kind<DT>::vectors || (n < kManyOutputs && rows * parts <= 16 * kBlocksOfFew)) {
+    if (scales_bytes(w.k8, group_log) <= kMostLds &&
+        (rows <= (size_t)Kind<DT>::vectors || (n < kManyOutputs && rows * parts <= 16 * kBlocksOfFew))) {
         w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
         w.blocks = (uint32_t)div_up(rows, w.vectors);
@@ -688,7 +694,7 @@ template <int DT>
 int run(const Call& c);
 template <int DT>
 int run(const Call& c) {
-    const Way w = way_of<DT>(c.rows, c.n, c.k);
+    const Way w = way_of<DT>(c.rows, c.n, c.k, c.group_log);
     if constexpr (DT == ZK_F32)
         if (!w.staged) return run<kPair>(c);
     float2* powers = nullptr;
@@ -710,7 +716,7 @@ int run(const Call& c) {
     }
     if (w.tiles == 1) {
         const uint32_t cols = (uint32_t)c.rows * Kind<DT>::parts;  // of a call that stages x
-        size_t lds = (w.staged ? (size_t)w.k8 * cols * 16 : 0) + (size_t)(w.k8 >> (c.group_log - 3)) * 32;
+        size_t lds = (w.staged ? (size_t)w.k8 * cols * 16 : 0) + scales_bytes(w.k8, c.group_log);
         if (lds < 8192) lds = 8192;  // the sums at the end
         const dim3 grid((unsigned)div_up(c.n, 16), w.blocks);
         auto* kernel = w.staged ? (c.group_log == 5 ? k_w4_few<DT, true, 5> : c.group_log == 6 ? k_w4_few<DT, true, 6> : k_w4_few<DT, true, 7>)
@@ -737,16 +743,21 @@ using namespace zkmi;
 
 namespace {
 template <int DT>
-size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs
-    const size_t few = way_bytes(way_of<DT>(rows, 1, k)), many = way_bytes(way_of<DT>(rows, 1u << 24, k));
-    return few > many ? few : many;
+size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs and the groups
+    size_t most = 0;
+    for (uint32_t n : {1u, 1u << 24})
+        for (uint32_t group_log : {5u, 7u}) {  // where scales are the longest and the shortest
+            const size_t need = way_bytes(way_of<DT>(rows, n, k, group_log));
+            most = need > most ? need : most;
+        }
+    return most;
 }
 }  // namespace
 
 extern "C" size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k) {
     if (!dtype_bytes(dtype) || rows == 0 || rows > kMostRows || !inputs_ok(k)) return 0;
     switch (dtype) {
-        case ZK_F32: return way_of<ZK_F32>(rows, 1, (uint32_t)k).staged ? 0 : workspace<kPair>(rows, (uint32_t)k);
+        case ZK_F32: return way_of<ZK_F32>(rows, 1, (uint32_t)k, 5).staged ? 0 : workspace<kPair>(rows, (uint32_t)k);
         case ZK_F16: return workspace<ZK_F16>(rows, (uint32_t)k);
         case ZK_BF16: return workspace<ZK_BF16>(rows, (uint32_t)k);
         default: return workspace<ZK_I16>(rows, (uint32_t)k);
