@@ -8,9 +8,9 @@
 // added by one more matrix instruction whose second operand is the constant -12.  What is accumulated is three times the
 // size of the result's terms at most, so nothing is lost of 32-bit sums.  Types:
 //   ZK_F16   x as it is.            ZK_BF16  x as it is.
-//   ZK_F32   x as the sum of three bf16 (8 + 8 + 8 bits: exact), three columns; where x is laid out beforehand, as the sum of
-//            two f16 (11 + 11 bits) after a power of two has brought the vector's largest to just below 2^15: what
-//            they miss is at most 2^-23 of an element or 2^-40 of the largest, a rounding's size.
+//   ZK_F32   x as the sum of three bf16 (8 + 8 + 8 bits: exact, whatever stands beside it), three columns.  (Two f16 of a
+//            vector scaled to its largest are fewer columns, but miss 2^-40 of the largest in every element: more than a
+//            rounding where an outlier meets small weights.)
 //   ZK_I16   x = 256 h + l, two columns of whole numbers below 2^8; a group's sums are below 2^20 halves, exact in 32
 //            bits, and everything after that is in 64-bit integers.
 //
@@ -30,7 +30,7 @@ namespace {
 static const int kStep = 128;                      // inputs a wavefront takes at a time
 static const int kWaves = 8;
 static const uint32_t kStageHalves = 32768;        // 64 KiB of x in LDS
-static const size_t kMostRows = (size_t)1 << 20;    // some 33000 blocks of columns
+static const size_t kMostRows = (size_t)1 << 20;    // 32768 blocks of columns at most, those of 32-bit floats
 // More columns than 16: blocks of 16 that each read the weights again (out of the caches), or the kernel for many columns, whose
 // workgroups have 64 or 128 outputs and are too few for a short matrix.  Measured, the first against the second, us: 32
 // vectors of bf16 by 4096 x 11008 18.7 and 34.8, by 5120 x 5120 15.0 and 18.7, by 8192 x 4096 18.4 and 16.2, by 9000 x 5120 (24
@@ -45,16 +45,12 @@ static const size_t kMostLds = 163840;
 // 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 48 and 55.
 static const uint32_t kWide = 16384;
 
-// 32-bit floats where x is laid out by k_w4_columns, as two 16-bit ones.
-static const int kPair = 100;
-
 template <int DT>
 struct Kind {
-    static constexpr bool wide = DT == ZK_F32 || DT == kPair;              // 32 bits to a value of x
-    static constexpr int parts = DT == ZK_F32 ? 3 : DT == ZK_I16 || DT == kPair ? 2 : 1;  // columns of a vector
+    static constexpr bool wide = DT == ZK_F32;                              // 32 bits to a value of x
+    static constexpr int parts = DT == ZK_F32 ? 3 : DT == ZK_I16 ? 2 : 1;  // columns of a vector
     static constexpr int vectors = 16 / parts;                             // vectors of a call's 16 columns
-    static constexpr bool f16 = DT == ZK_F16 || DT == kPair;
-    static constexpr int out = DT == kPair ? ZK_F32 : DT;
+    static constexpr bool f16 = DT == ZK_F16;
 };
 
 template <int DT>
@@ -98,7 +94,7 @@ __device__ __forceinline__ Eight<DT> load_eight(const void* x, size_t at) {
     return e;
 }
 template <int DT>
-__device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<DT>::parts], float up = 1.0f) {
+__device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<DT>::parts]) {
     if constexpr (DT == ZK_F16 || DT == ZK_BF16) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -114,14 +110,6 @@ __device__ __forceinline__ void columns_of(const Eight<DT>& x, v4u (&out)[Kind<D
         for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) out[p][i] = part(i, p) | (part(i + 4, p) << 16);
-    } else if constexpr (DT == kPair) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = bits_float(x.r[0][i]) * up, b = bits_float(x.r[1][i]) * up;
-            const uint32_t ah = half_bits<ZK_F16>(a), bh = half_bits<ZK_F16>(b);
-            out[0][i] = ah | (bh << 16);
-            out[1][i] = half_bits<ZK_F16>(a - half_of<ZK_F16>(ah, 0)) | ((uint32_t)half_bits<ZK_F16>(b - half_of<ZK_F16>(bh, 0)) << 16);
-        }
     } else {
         float r[8];
 #pragma unroll
@@ -170,7 +158,7 @@ __host__ __device__ __forceinline__ uint32_t threads_across(uint32_t vectors) { 
 // LDS where all of it fits there (STAGED), else from `xf`, where k_w4_columns has laid out the operands [k / 8][16]: a
 // wavefront then reads a kilobyte of them for each instruction, out of the L2, and nothing waits for anything in the loop.
 template <int DT, bool STAGED, int GL>
-__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, const float2* powers, size_t rows,
+__global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, size_t rows,
                                                         const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
                                                         float unit2) {
     constexpr int parts = Kind<DT>::parts;
@@ -338,42 +326,17 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
                 for (int p = 0; p < parts; ++p)
 #pragma unroll
                     for (int v = 0; v < kWaves; ++v) sum += red[(v * 16 + m * parts + p) * 16 + o];
-                store_one<Kind<DT>::out>(y, (m0 + m) * ystride + n0 + o, DT == kPair ? sum * unit2 * powers[m0 + m].y : sum * unit2);
+                store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
             }
         }
     }
-}
-
-// The power of two that brings a vector's largest to just below 2^15, and the one that takes it back; NaN if a value is not
-// finite.  Workgroup: one vector, all of a usual one on its way at once (256 threads: 4.6 us for 5120 inputs, in turn).
-static const int kPowers = 1024;
-__global__ __launch_bounds__(kPowers) void k_w4_powers(float2* powers, const float* x, size_t xstride, uint32_t k) {
-    __shared__ uint32_t most[kPowers / 64];
-    const uint32_t* row = (const uint32_t*)x + blockIdx.x * xstride;
-    uint32_t bits = 0;
-    for (uint32_t i = threadIdx.x * 4; i < k; i += kPowers * 8) {
-        const v4u r0 = *(const v4u*)(row + i), r1 = *(const v4u*)(row + (i + kPowers * 4 < k ? i + kPowers * 4 : i));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bits = max(bits, max(r0[e] & 0x7fffffffu, r1[e] & 0x7fffffffu));
-    }
-    bits = wave_max(bits);
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = bits;
-    __syncthreads();
-    if (threadIdx.x) return;
-#pragma unroll
-    for (int w = 0; w < kPowers / 64; ++w) bits = max(bits, most[w]);
-    // 2^e > the largest; a vector of zeros, or of less than 2^-100, is scaled as if that were its largest
-    int e = (int)(bits >> 23) - 126;
-    e = e < -100 ? -100 : e;
-    const bool fine = bits < 0x7f800000u;
-    powers[blockIdx.x] = fine ? make_float2(ldexpf(1.0f, 15 - e), ldexpf(1.0f, e - 15)) : make_float2(__builtin_nanf(""), __builtin_nanf(""));
 }
 
 // x as operands: xf[block][k / 8][columns of a block], zero behind the last column and the last input (up to a step's end);
 // with sums, -12 times the sum over each group of inputs, [block][group][columns of a block].  A block has `vectors`
 // vectors.  Workgroup: one group, or eight of 16 bytes where nobody asks for sums.
 template <int DT>
-__global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, const float2* powers, const void* x, size_t xstride, size_t rows, uint32_t k,
+__global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, const void* x, size_t xstride, size_t rows, uint32_t k,
                                                        uint32_t k8_all, uint32_t columns, uint32_t vectors, uint32_t group_log) {
     constexpr int parts = Kind<DT>::parts;
     const uint32_t block = blockIdx.y, per = sums ? 1u << (group_log - 3) : 8;  // pieces of eight inputs of a workgroup, 4, 8 or 16
@@ -384,7 +347,7 @@ __global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, con
 #pragma unroll
         for (int p = 0; p < parts; ++p) c[p] = v4u{0, 0, 0, 0};
         if (m < vectors && m0 + m < rows && k8 * 8 < k)
-            columns_of<DT>(load_eight<DT>(x, (m0 + m) * xstride + k8 * 8), c, DT == kPair ? powers[m0 + m].x : 1.0f);
+            columns_of<DT>(load_eight<DT>(x, (m0 + m) * xstride + k8 * 8), c);
 #pragma unroll
         for (int p = 0; p < parts; ++p) {
             const uint32_t col = m * parts + p;
@@ -411,7 +374,7 @@ struct ManyLds {
     static constexpr uint32_t all = 2 * bytes > meet ? 2 * bytes : meet;
 };
 template <int DT, int CT, int NT, int GL>
-__global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, const float2* powers, size_t rows, const uint8_t* codes,
+__global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, size_t rows, const uint8_t* codes,
                                                  const uint16_t* scales, uint32_t n, uint32_t k, uint32_t vectors, float unit2) {
     constexpr uint32_t group_log = GL;
     using L = ManyLds<CT, NT>;
@@ -596,7 +559,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
             float sum = 0.0f;
 #pragma unroll
             for (int p = 0; p < Kind<DT>::parts; ++p) sum += tile[(m * Kind<DT>::parts + p) * N + o];
-            store_one<Kind<DT>::out>(y, (m0 + m) * ystride + n0 + o, DT == kPair ? sum * unit2 * powers[m0 + m].y : sum * unit2);
+            store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
         }
     }
 }
@@ -621,7 +584,7 @@ struct Way {
     uint32_t blocks, vectors;   // of columns, and the vectors of each
     uint32_t tiles;             // of 16 columns of a block; 1: few columns
     uint32_t k8;                // pieces of eight inputs, whole steps
-    size_t operands, sums, powers;  // in the workspace, bytes
+    size_t operands, sums;      // in the workspace, bytes
 };
 size_t scales_bytes(uint32_t k8, uint32_t group_log) { return (size_t)(k8 >> (group_log - 3)) * 32; }  // of 16 outputs
 template <int DT>
@@ -634,7 +597,7 @@ Way way_of(size_t rows, uint32_t n, uint32_t k, uint32_t group_log) {
         w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
         w.blocks = (uint32_t)div_up(rows, w.vectors);
-        w.staged = DT != kPair && w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
+        w.staged = w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
     } else {
         // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
         const size_t most = 96 / parts;
@@ -644,7 +607,6 @@ Way way_of(size_t rows, uint32_t n, uint32_t k, uint32_t group_log) {
         w.blocks = (uint32_t)div_up(rows, v);
     }
     if (!w.staged) w.operands = (size_t)w.blocks * w.k8 * w.tiles * 256;
-    if (DT == kPair) w.powers = rows * sizeof(float2);
     if (w.tiles > 1) w.sums = (size_t)w.blocks * (w.k8 / 4) * w.tiles * 64;  // of the shortest groups
     return w;
 }
@@ -652,7 +614,6 @@ size_t way_bytes(const Way& w) {
     Carver cv(nullptr, 0);
     cv.take(w.operands);
     cv.take(w.sums);
-    cv.take(w.powers);
     return w.operands ? cv.used() : 0;
 }
 
@@ -671,33 +632,28 @@ struct Call {
 };
 
 template <int DT, int CT, int NT, int GL>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
     const size_t lds = ManyLds<CT, NT>::all;
     auto* kernel = k_w4_many<DT, CT, NT, GL>;
     if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, powers, c.rows,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, c.rows,
                        c.codes, c.scales, c.n, c.k, w.vectors, c.unit * 2.0f);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
 template <int DT, int CT, int NT>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
-    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums, powers) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums, powers)
-                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums, powers);
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums)
+                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums);
 }
 template <int DT, int CT>
-int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums, const float2* powers) {
-    return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums, powers) : run_many<DT, CT, 1>(c, w, xf, sums, powers);
+int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums) : run_many<DT, CT, 1>(c, w, xf, sums);
 }
 
 template <int DT>
-int run(const Call& c);
-template <int DT>
 int run(const Call& c) {
     const Way w = way_of<DT>(c.rows, c.n, c.k, c.group_log);
-    if constexpr (DT == ZK_F32)
-        if (!w.staged) return run<kPair>(c);
-    float2* powers = nullptr;
     v4u* xf = nullptr;
     float* sums = nullptr;
     if (w.operands) {
@@ -705,12 +661,9 @@ int run(const Call& c) {
         Carver cv(c.ws, c.ws_bytes);
         xf = (v4u*)cv.take(w.operands);
         if (w.sums) sums = (float*)cv.take(w.sums);
-        if (w.powers) powers = (float2*)cv.take(w.powers);
-        if (cv.overflow() || !xf || (w.sums && !sums) || (w.powers && !powers)) return ZK_E_BUFSZ;
-        if (w.powers)
-            hipLaunchKernelGGL(k_w4_powers, dim3((unsigned)c.rows), dim3(kPowers), 0, c.stream, powers, (const float*)c.x, c.xstride, c.k);
+        if (cv.overflow() || !xf || (w.sums && !sums)) return ZK_E_BUFSZ;
         const uint32_t per = sums ? 1u << (c.group_log - 3) : 8;
-        hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, powers, c.x, c.xstride,
+        hipLaunchKernelGGL((k_w4_columns<DT>), dim3((unsigned)div_up(w.k8, per), w.blocks), dim3(kBlock), 0, c.stream, xf, sums, c.x, c.xstride,
                            c.rows, c.k, w.k8, w.tiles * 16, w.vectors, c.group_log);
         ZK_HIP_TRY(hipGetLastError());
     }
@@ -722,12 +675,12 @@ int run(const Call& c) {
         auto* kernel = w.staged ? (c.group_log == 5 ? k_w4_few<DT, true, 5> : c.group_log == 6 ? k_w4_few<DT, true, 6> : k_w4_few<DT, true, 7>)
                                 : (c.group_log == 5 ? k_w4_few<DT, false, 5> : c.group_log == 6 ? k_w4_few<DT, false, 6> : k_w4_few<DT, false, 7>);
         if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, powers, c.rows, c.codes, c.scales, c.n,
+        hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, c.rows, c.codes, c.scales, c.n,
                            c.k, c.unit * 2.0f);
         ZK_HIP_TRY(hipGetLastError());
         return ZK_OK;
     }
-    return w.tiles == 2 ? run_many<DT, 2>(c, w, xf, sums, powers) : w.tiles == 4 ? run_many<DT, 4>(c, w, xf, sums, powers) : run_many<DT, 6>(c, w, xf, sums, powers);
+    return w.tiles == 2 ? run_many<DT, 2>(c, w, xf, sums) : w.tiles == 4 ? run_many<DT, 4>(c, w, xf, sums) : run_many<DT, 6>(c, w, xf, sums);
 }
 
 bool inputs_ok(size_t k) { return k >= 32 && k <= ((size_t)1 << 20) && k % 32 == 0; }
@@ -757,7 +710,7 @@ size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs a
 extern "C" size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k) {
     if (!dtype_bytes(dtype) || rows == 0 || rows > kMostRows || !inputs_ok(k)) return 0;
     switch (dtype) {
-        case ZK_F32: return way_of<ZK_F32>(rows, 1, (uint32_t)k, 5).staged ? 0 : workspace<kPair>(rows, (uint32_t)k);
+        case ZK_F32: return workspace<ZK_F32>(rows, (uint32_t)k);
         case ZK_F16: return workspace<ZK_F16>(rows, (uint32_t)k);
         case ZK_BF16: return workspace<ZK_BF16>(rows, (uint32_t)k);
         default: return workspace<ZK_I16>(rows, (uint32_t)k);

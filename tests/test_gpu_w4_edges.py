@@ -56,3 +56,57 @@ def test_workspace_of_long_vectors(zk):
     assert rc == zk.ZK_E_BUFSZ
     rc, _ = zk.w4_matvec(x, codes, scales, group, ws=torch.empty(need, dtype=torch.uint8, device="cuda"))
     assert rc == zk.ZK_OK
+
+
+def bound(x, codes, scales, group, unit):
+    """test_gpu_w4's bound on the sums' error, elementwise: 8 * 2^-24 * 55 * unit * sqrt(groups) * max over groups of s * sum |x|."""
+    k, groups = x.shape[1], scales.shape[1]
+    xa = torch.nn.functional.pad(x.double().abs(), (0, groups * group - k)).reshape(x.shape[0], groups, group).sum(2)
+    return 8 * 2.0 ** -24 * 55 * (xa[:, None, :] * scales.double()[None]).amax(2) * unit * math.sqrt(groups)
+
+
+# rows and outputs that x in LDS, x laid out, and blocks of many columns have
+WAYS = [(3, 40, 256), (5, 300, 2080), (6, 40, 320), (20, 500, 1056), (31, 8200, 416), (40, 9000, 320), (33, 16400, 288)]
+
+
+@pytest.mark.parametrize("rows,n,k", WAYS)
+def test_f32_beside_an_outlier(zk, rows, n, k):
+    """One input far above the others that no output weighs: the others count with all their bits, in every number of vectors."""
+    group, unit = 32, 2.0 ** -14
+    gen, codes, scales = make(n, k, group, rows + n)
+    scales[:, 1] = 0
+    x = torch.randn(rows, k, generator=gen, device="cuda")
+    x[:, 40] = 10.0 ** torch.linspace(4, 15, rows, device="cuda")
+    rc, y = zk.w4_matvec(x, codes, scales, group, unit)
+    assert rc == zk.ZK_OK
+    want = x.double() @ (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
+    tol = bound(x, codes, scales, group, unit) + 2.0 ** -24 * want.abs()
+    assert ((y.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("rows,n,k", WAYS)
+def test_rows_of_unlike_size(zk, rows, n, k):
+    """Every row is as exact as if it stood alone: rows of 2^-80 and of 2^80, of zeros, of an infinity or a NaN side by side."""
+    group, unit = 64, 2.0 ** -14
+    gen, codes, scales = make(n, k, group, rows * n)
+    size = torch.exp2(torch.randint(-80, 81, (rows, 1), generator=gen, device="cuda").float())
+    base = torch.randn(rows, k, generator=gen, device="cuda")
+    w = (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
+    for dtype in (torch.float32, torch.bfloat16):
+        x = (base * size).to(dtype)
+        x[rows // 2] = 0
+        rc, y = zk.w4_matvec(x, codes, scales, group, unit)
+        assert rc == zk.ZK_OK
+        want = x.double() @ w
+        tol = bound(x, codes, scales, group, unit) + torch.finfo(dtype).eps / 2 * want.abs()
+        assert ((y.double() - want).abs() <= tol).all() and not y[rows // 2].any()
+        hurt = x.clone()
+        hurt[0, k - 1], hurt[rows - 1, 3] = math.nan, -math.inf
+        if rows > 5:
+            hurt[3, 100] = math.inf
+        rc, z = zk.w4_matvec(hurt, codes, scales, group, unit)
+        assert rc == zk.ZK_OK
+        bad = torch.tensor([r for r in range(rows) if r in (0, rows - 1) or (r == 3 and rows > 5)], device="cuda")
+        kept = torch.ones(rows, dtype=torch.bool, device="cuda")
+        kept[bad] = False
+        assert z[bad].isnan().all() and torch.equal(z[kept], y[kept])
