@@ -3,10 +3,13 @@
 //   y[m][n] = unit * sum_g s[n][g] * sum_{k in g} c[n][k] x[m][k],   c = u - 8,  u a half byte.
 //
 // The sums over a group run on the matrix cores (16 x 16 x 32).  The first operand is x, a column of it to a row of the
-// operand; the second holds 16 outputs' weights.  A half byte becomes a 16-bit float without a table or a subtraction:
-// put into the top of the mantissa of 8.0 it is 8 + u/2 = (c + 24) / 2, exact in both 16-bit types, and -12 sum x is
-// added by one more matrix instruction whose second operand is the constant -12.  What is accumulated is three times the
-// size of the result's terms at most, so nothing is lost of 32-bit sums.  Types:
+// operand; the second holds 16 outputs' weights.  For 16-bit x a half byte becomes a 16-bit float without a table or a
+// subtraction: put into the top of the mantissa of 8.0 it is 8 + u/2 = (c + 24) / 2, exact in both 16-bit types, and -12 sum x
+// is added by one more matrix instruction whose second operand is the constant -12.  A term c x is then carried at up to
+// (|c| + 24) |x| in 32-bit sums, which leaves up to 1e-5 of the results' size as error (measured at 5120 positive inputs, codes
+// of deviation 1.5) where a 16-bit output itself rounds to 2.4e-4 (f16) or 2e-3 (bf16).  A 32-bit output would show it: there
+// weights are widened to 16 c, without an offset, for twice the vector instructions; the error is 1.3e-7 then, whatever
+// the codes and the inputs (a library's product of 32-bit floats: 1.1e-6).  Types:
 //   ZK_F16   x as it is.            ZK_BF16  x as it is.
 //   ZK_F32   x as the sum of three bf16 (8 + 8 + 8 bits: exact, whatever stands beside it), three columns.  (Two f16 of a
 //            vector scaled to its largest are fewer columns, but miss 2^-40 of the largest in every element: more than a
@@ -51,6 +54,8 @@ struct Kind {
     static constexpr int parts = DT == ZK_F32 ? 3 : DT == ZK_I16 ? 2 : 1;  // columns of a vector
     static constexpr int vectors = 16 / parts;                             // vectors of a call's 16 columns
     static constexpr bool f16 = DT == ZK_F16;
+    static constexpr bool offset = DT != ZK_F32;                            // weights enter as (c + 24) / 2, else as 16 c
+    static constexpr float step = offset ? 2.0f : 0.0625f;                  // what takes that back
 };
 
 template <int DT>
@@ -59,9 +64,18 @@ __device__ __forceinline__ v4f product(v4u a, v4u b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
 }
 
-// Eight half bytes as 8 + u/2.
+// Eight half bytes as 8 + u/2, or as 16 c: with its top bit flipped a half byte is c in two's complement, in the upper half of a
+// byte 16 c, which converts to a float whose lower 16 bits are zero.
 template <int DT>
 __device__ __forceinline__ v4u widen(uint32_t w) {
+    if constexpr (!Kind<DT>::offset) {
+        const uint32_t t = w ^ 0x88888888u, even = (t << 4) & 0xf0f0f0f0u, odd = t & 0xf0f0f0f0u;
+        auto two = [](uint32_t x, int at) {  // of bytes at and at + 2
+            const float lo = (float)(int8_t)(x >> (8 * at)), hi = (float)(int8_t)(x >> (8 * at + 16));
+            return __builtin_amdgcn_perm(float_bits(hi), float_bits(lo), 0x07060302u);
+        };
+        return v4u{two(even, 0), two(odd, 0), two(even, 1), two(odd, 1)};
+    }
     if constexpr (Kind<DT>::f16) {
         const uint32_t mask = 0x03c003c0u, eight = 0x48004800u;
         return v4u{((w << 6) & mask) | eight, ((w << 2) & mask) | eight, ((w >> 2) & mask) | eight, ((w >> 6) & mask) | eight};
@@ -160,7 +174,7 @@ __host__ __device__ __forceinline__ uint32_t threads_across(uint32_t vectors) { 
 template <int DT, bool STAGED, int GL>
 __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride, const void* x, size_t xstride, const v4u* xf, size_t rows,
                                                         const uint8_t* codes, const uint16_t* scales, uint32_t n, uint32_t k,
-                                                        float unit2) {
+                                                        float step_unit) {
     constexpr int parts = Kind<DT>::parts;
     constexpr uint32_t group_log = GL;
     extern __shared__ v4u shared[];
@@ -273,16 +287,19 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
         if (group_log == 5) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4f p = product<DT>(a[q], widen<DT>(r[q]), product<DT>(a[q], back, v4f{0, 0, 0, 0}));
-                add_group(p, gr + q);
+                v4f p = {0, 0, 0, 0};
+                if constexpr (Kind<DT>::offset) p = product<DT>(a[q], back, p);
+                add_group(product<DT>(a[q], widen<DT>(r[q]), p), gr + q);
             }
         } else {
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
-                acc[f] = product<DT>(a[2 * f], back, v4f{0, 0, 0, 0});
-                acc[f] = product<DT>(a[2 * f], widen<DT>(r[2 * f]), acc[f]);
-                acc[f] = product<DT>(a[2 * f + 1], back, acc[f]);
-                acc[f] = product<DT>(a[2 * f + 1], widen<DT>(r[2 * f + 1]), acc[f]);
+                acc[f] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int q = 2 * f; q < 2 * f + 2; ++q) {
+                    if constexpr (Kind<DT>::offset) acc[f] = product<DT>(a[q], back, acc[f]);
+                    acc[f] = product<DT>(a[q], widen<DT>(r[q]), acc[f]);
+                }
             }
             if (group_log == 6) {
                 add_group(acc[0], gr);
@@ -326,7 +343,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_w4_few(void* y, size_t ystride,
                 for (int p = 0; p < parts; ++p)
 #pragma unroll
                     for (int v = 0; v < kWaves; ++v) sum += red[(v * 16 + m * parts + p) * 16 + o];
-                store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
+                store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * step_unit);
             }
         }
     }
@@ -367,17 +384,18 @@ __global__ __launch_bounds__(kBlock) void k_w4_columns(v4u* xf, float* sums, con
 
 // Workgroup: 64 NT outputs by 16 CT columns, chunks of two steps.  Wavefront w: outputs 16 NT (w mod 4) .., step w / 4 of a
 // chunk.  Operands and sums come from k_w4_columns through registers, one or two chunks ahead, into LDS.
-template <int CT, int NT>
+template <int CT, int NT, bool OFFSET>
 struct ManyLds {
-    static constexpr uint32_t C = 16 * CT, N = 64 * NT, x = 32 * C * 16, sums = 8 * C * 4, scales = 8 * N * 2, bytes = x + sums + scales;
+    static constexpr uint32_t C = 16 * CT, N = 64 * NT, x = 32 * C * 16, sums = OFFSET ? 8 * C * 4 : 0, scales = 8 * N * 2, bytes = x + sums + scales;
     static constexpr uint32_t meet = 4 * NT * CT * 64 * 16;  // also the outputs, C * N floats
     static constexpr uint32_t all = 2 * bytes > meet ? 2 * bytes : meet;
 };
 template <int DT, int CT, int NT, int GL>
 __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const v4u* xf, const float* sums, size_t rows, const uint8_t* codes,
-                                                 const uint16_t* scales, uint32_t n, uint32_t k, uint32_t vectors, float unit2) {
+                                                 const uint16_t* scales, uint32_t n, uint32_t k, uint32_t vectors, float step_unit) {
     constexpr uint32_t group_log = GL;
-    using L = ManyLds<CT, NT>;
+    constexpr bool offset = Kind<DT>::offset;
+    using L = ManyLds<CT, NT, offset>;
     constexpr uint32_t C = L::C, N = L::N;
     extern __shared__ v4u shared[];
     char* lds = (char*)shared;
@@ -388,7 +406,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
 
     // What a thread brings of a chunk lies in a row with what its neighbours bring; behind the last input everything reads as 0.
     const Buffer operands = buffer_of(xf + (size_t)block * k8_all * C, (size_t)k8_all * C * 16);
-    const Buffer offsets = buffer_of(sums + (size_t)block * all_groups * C, (size_t)all_groups * C * 4);
+    const Buffer offsets = buffer_of(sums + (offset ? (size_t)block * all_groups * C : 0), offset ? (size_t)all_groups * C * 4 : 0);
     const Buffer factors = buffer_of(scales + (size_t)n0 * groups, (size_t)(n - n0 < N ? n - n0 : N) * groups * 2);
     struct Load {
         v4u x[CT];
@@ -403,7 +421,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
 #pragma unroll
         for (int i = 0; i < CT; ++i) to.x[i] = load16(operands, (chunk * 32 * C + tid + 512 * i) * 16);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; offset && i < 2; ++i)
             to.b[i] = bits_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b32(offsets, (int)((chunk * each * C + tid + 512 * i) * 4), 0, 0));
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -416,7 +434,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
 #pragma unroll
         for (int i = 0; i < CT; ++i) ((v4u*)at)[tid + 512 * i] = from.x[i];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; offset && i < 2; ++i)
             if (tid + 512 * i < each * C) ((float*)(at + L::x))[tid + 512 * i] = from.b[i];
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -471,7 +489,8 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
                 // a group's sums start at what the codes' offset takes off
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
-                    acc[0][c] = *(const v4f*)(bs + gr * C + 16 * c);
+                    if constexpr (offset) acc[0][c] = *(const v4f*)(bs + gr * C + 16 * c);
+                    else acc[0][c] = v4f{0, 0, 0, 0};
 #pragma unroll
                     for (int t = 1; t < NT; ++t) acc[t][c] = acc[0][c];
                 }
@@ -559,7 +578,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
             float sum = 0.0f;
 #pragma unroll
             for (int p = 0; p < Kind<DT>::parts; ++p) sum += tile[(m * Kind<DT>::parts + p) * N + o];
-            store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * unit2);
+            store_one<DT>(y, (m0 + m) * ystride + n0 + o, sum * step_unit);
         }
     }
 }
@@ -607,7 +626,7 @@ Way way_of(size_t rows, uint32_t n, uint32_t k, uint32_t group_log) {
         w.blocks = (uint32_t)div_up(rows, v);
     }
     if (!w.staged) w.operands = (size_t)w.blocks * w.k8 * w.tiles * 256;
-    if (w.tiles > 1) w.sums = (size_t)w.blocks * (w.k8 / 4) * w.tiles * 64;  // of the shortest groups
+    if (w.tiles > 1 && Kind<DT>::offset) w.sums = (size_t)w.blocks * (w.k8 / 4) * w.tiles * 64;  // of the shortest groups
     return w;
 }
 size_t way_bytes(const Way& w) {
@@ -633,11 +652,11 @@ struct Call {
 
 template <int DT, int CT, int NT, int GL>
 int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
-    const size_t lds = ManyLds<CT, NT>::all;
+    const size_t lds = ManyLds<CT, NT, Kind<DT>::offset>::all;
     auto* kernel = k_w4_many<DT, CT, NT, GL>;
     if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL(kernel, dim3((unsigned)div_up(c.n, 64 * NT), w.blocks), dim3(512), lds, c.stream, c.y, c.ystride, xf, sums, c.rows,
-                       c.codes, c.scales, c.n, c.k, w.vectors, c.unit * 2.0f);
+                       c.codes, c.scales, c.n, c.k, w.vectors, c.unit * Kind<DT>::step);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -676,7 +695,7 @@ int run(const Call& c) {
                                 : (c.group_log == 5 ? k_w4_few<DT, false, 5> : c.group_log == 6 ? k_w4_few<DT, false, 6> : k_w4_few<DT, false, 7>);
         if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
         hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), lds, c.stream, c.y, c.ystride, c.x, c.xstride, xf, c.rows, c.codes, c.scales, c.n,
-                           c.k, c.unit * 2.0f);
+                           c.k, c.unit * Kind<DT>::step);
         ZK_HIP_TRY(hipGetLastError());
         return ZK_OK;
     }

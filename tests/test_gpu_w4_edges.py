@@ -110,3 +110,42 @@ def test_rows_of_unlike_size(zk, rows, n, k):
         kept = torch.ones(rows, dtype=torch.bool, device="cuda")
         kept[bad] = False
         assert z[bad].isnan().all() and torch.equal(z[kept], y[kept])
+
+
+@pytest.mark.parametrize("rows,n,k", WAYS)
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_f32_weights_of_zero_cost_nothing(zk, rows, n, k, group):
+    """Codes of zero add nothing, not even a rounding, however large the inputs they meet.  One weight to an output: x's parts
+    times a code of 4 bits times a scale of 12 are exact, three of them are added and the unit is a power of two: 3 * 2^-24.
+    None at all: zero."""
+    unit = 2.0 ** -14
+    gen, codes, scales = make(n, k, group, rows + n + group)
+    at = torch.randint(0, k, (n,), generator=gen, device="cuda")
+    c = torch.randint(-8, 8, (n,), generator=gen, device="cuda")
+    c[::7] = 0
+    nibbles = torch.full((n, k), 8, dtype=torch.int64, device="cuda")
+    nibbles[torch.arange(n, device="cuda"), at] = c + 8
+    codes = (nibbles[:, 0::2] | (nibbles[:, 1::2] << 4)).to(torch.uint8)
+    x = torch.rand(rows, k, generator=gen, device="cuda") * 5 + 1
+    rc, y = zk.w4_matvec(x, codes, scales, group, unit)
+    assert rc == zk.ZK_OK
+    want = x.double() @ (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
+    assert ((y.double() - want).abs() <= 3 * 2.0 ** -24 * want.abs()).all()
+    assert not y[:, ::7].any()
+
+
+@pytest.mark.parametrize("rows,n", [(1, 64), (5, 64), (6, 64), (32, 64), (32, 8200), (17, 16400)])
+def test_f32_of_few_weights(zk, rows, n):
+    """Inputs of one sign, one weight in 64 not zero.  Relative to the sum of |w x|: four instructions of a group at two roundings
+    of 2^-23 each, products with the scales and their sums in a wavefront (40 at most), wavefronts and parts (27): under 96 * 2^-24."""
+    k, group, unit = 5120, 128, 2.0 ** -14
+    gen, codes, scales = make(n, k, group, rows)
+    keep = torch.rand(n, k, generator=gen, device="cuda") < 1 / 64
+    nibbles = torch.where(keep, torch.randint(0, 16, (n, k), generator=gen, device="cuda"), 8)
+    codes = (nibbles[:, 0::2] | (nibbles[:, 1::2] << 4)).to(torch.uint8)
+    x = torch.randn(rows, k, generator=gen, device="cuda") * 0.1 + 3
+    rc, y = zk.w4_matvec(x, codes, scales, group, unit)
+    assert rc == zk.ZK_OK
+    w = (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
+    size = x.double() @ w.abs()
+    assert ((y.double() - x.double() @ w).abs() <= 96 * 2.0 ** -24 * size).all()
