@@ -45,7 +45,10 @@ static const uint32_t kManyOutputs = 8192, kBlocksOfFew = 6;
 // those of a chunk.
 static const size_t kMostLds = 163840;
 // Outputs from which a workgroup of the kernel for many columns has 128, not 64.  Measured, 128 and 64, us: 64 vectors of bf16 by
-// 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 48 and 55.
+// 13824 x 5120 38 and 30, by 20000 x 5120 38.4 and 39.7, by 32001 x 5120 45 and 49; 32 of 32 bits by 32001 x 5120 52 and 67, 10 of
+// them 29 and 32.  But 64 for six tiles of columns and groups of 32, whose sums do not fit the registers with 128: 96 vectors of
+// bf16 by 32001 x 5120 192 and 92, 70 by 20000 x 4096 140 and 67, 40 of 16-bit integers by it 149 and 79, 32 of 32 bits by 32001 x
+// 5120 153 and 80.
 static const uint32_t kWide = 16384;
 
 template <int DT>
@@ -662,11 +665,14 @@ int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
 }
 template <int DT, int CT, int NT>
 int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
-    return c.group_log == 5 ? run_many<DT, CT, NT, 5>(c, w, xf, sums) : c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums)
-                                                                                          : run_many<DT, CT, NT, 7>(c, w, xf, sums);
+    if constexpr (CT < 6)
+        if (c.group_log == 5) return run_many<DT, CT, NT, 5>(c, w, xf, sums);
+    return c.group_log == 6 ? run_many<DT, CT, NT, 6>(c, w, xf, sums) : run_many<DT, CT, NT, 7>(c, w, xf, sums);
 }
 template <int DT, int CT>
 int run_many(const Call& c, const Way& w, const v4u* xf, const float* sums) {
+    if constexpr (CT == 6)
+        if (c.group_log == 5) return run_many<DT, CT, 1, 5>(c, w, xf, sums);
     return c.n >= kWide ? run_many<DT, CT, 2>(c, w, xf, sums) : run_many<DT, CT, 1>(c, w, xf, sums);
 }
 
