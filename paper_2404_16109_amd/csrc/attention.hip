@@ -168,14 +168,20 @@ __device__ void not_a_number(const Args& a, uint32_t b, uint32_t h) {
         }
 }
 
+// The first key that row i of a sequence sees, or any of the later rows.
+__device__ __forceinline__ uint32_t first_seen(const Args& a, const SeqView& v, int32_t i) {
+    const int64_t low = a.window ? (int64_t)v.len - v.rows + i - (int64_t)a.window + 1 : 0;
+    return low > 0 ? (uint32_t)low : 0;
+}
+
 // Tiles [first, end) of the keys that rows [i0, i1] of a sequence see.
 struct Tiles {
     uint32_t first, end;
 };
 __device__ __forceinline__ Tiles tiles_of(const Args& a, const SeqView& v, int32_t i0, int32_t i1) {
-    const int64_t past = (int64_t)v.len - v.rows, last = past + i1, low = a.window ? past + i0 - (int64_t)a.window + 1 : 0;
+    const int64_t last = (int64_t)v.len - v.rows + i1;
     Tiles t;
-    t.first = low > 0 ? (uint32_t)(low / kTile) : 0;
+    t.first = first_seen(a, v, i0) / kTile;
     t.end = last < 0 ? t.first : (uint32_t)(last / kTile) + 1;
     return t;
 }
@@ -256,7 +262,7 @@ __device__ __forceinline__ void attend_part(const Args& a, float* sh, const SeqV
 
     // Every load is made: tokens behind the sequence read some page, pages that are none page 0, dimensions behind head_dim
     // the row's first (q is 0 there).  All are numbers, and nothing of them is kept.
-    const uint32_t len = (uint32_t)v.len;
+    const uint32_t len = (uint32_t)v.len, seen_from = first_seen(a, v, 0);  // a tile may begin before what any row sees
     const size_t page_stride = (size_t)T * d;
     v4u kr[4][NJ], vr[DT];
     auto load_k = [&](uint32_t page, uint32_t t) {
@@ -332,7 +338,7 @@ __device__ __forceinline__ void attend_part(const Args& a, float* sh, const SeqV
         if (more) load_k(pk_next, t + W);
         // a page that is none has a score that is none
         const float kscale = none ? __builtin_nanf("") : exp2_of(exponent_value(ke)), vadd = none ? 0.0f : exponent_value(ve), vback = back_of(vadd);
-        if (none && t * kTile + 16 * g < len) report(a.s, ZK_FAULT_PAGE);
+        if (none && t * kTile + 16 * g < len && t * kTile + 16 * g + 16 > seen_from) report(a.s, ZK_FAULT_PAGE);
         if (more) load_e(pv_next);
 
         const int32_t base = (int32_t)(t * kTile);
@@ -656,7 +662,7 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         if (tiles.first >= tiles.end) return;  // k_attend_join knows
         tiles.end = tiles.first + each < tiles.end ? tiles.first + each : tiles.end;
     }
-    const uint32_t r = r0 + wave * 32 + i32, len = (uint32_t)v.len;
+    const uint32_t r = r0 + wave * 32 + i32, seen_from = first_seen(a, v, tok0);
 
     v8h qf[2 * DT];
     float qmul;
@@ -700,7 +706,8 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
         if (tid < 8) {
             const uint32_t it = page[tid & 3];
             const bool none = it >= a.cache.pages;
-            if (none && t * kTile + 16 * (tid & 3) < len) report(a.s, ZK_FAULT_PAGE);
+            const uint32_t key = t * kTile + 16 * (tid & 3);
+            if (none && (int32_t)key <= pos_last && key + 16 > seen_from) report(a.s, ZK_FAULT_PAGE);
             const size_t at = (size_t)page_or_0(a, it) * H + h;
             my_exp = none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at]);
         }
