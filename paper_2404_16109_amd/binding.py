@@ -832,8 +832,20 @@ LOGPROBS_MAX_TOP = 32
 _DTYPES = {torch.float32: ZK_F32, torch.float16: ZK_F16, torch.bfloat16: ZK_BF16, torch.int16: ZK_I16}
 
 
-def _optional(t):
-    return None if t is None else t.data_ptr()
+def _fault(t):
+    # the kernels write there: an address of the host's, or a word that is not one, must not get that far
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.numel() == 1 and t.is_cuda, "fault: an int32 tensor of one element on the GPU"
+    return t.data_ptr()
+
+
+def _workspace(t):
+    """(address, bytes) of a workspace that a caller gave, or of none."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.is_contiguous(), "ws: a contiguous tensor on the GPU"
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 class KvCache:
@@ -861,7 +873,7 @@ def _kv_seqs(cu, lens, table, rows, max_new, max_len, fault):
     seqs = lens.shape[0]
     assert cu.shape[0] == seqs + 1 and cu.is_contiguous() and lens.is_contiguous()
     assert table.shape[0] == seqs and (table.stride(1) == 1 or table.shape[1] == 1)
-    return kv_seqs(cu.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1], seqs, rows, max_new, max_len, _optional(fault))
+    return kv_seqs(cu.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0), table.shape[1], seqs, rows, max_new, max_len, _fault(fault))
 
 
 def kvcache_append(cache, k, v, cu, lens, table, max_new, fault=None):
@@ -892,7 +904,7 @@ def kvcache_attention(cache, q, cu, lens, table, max_new, max_len, scale, window
         ws = _ws(_lib.kvcache_attention_workspace_bytes(s.seqs, rows, max_new, heads, cache.c.kv_heads, dim, max_len))
     rc = _lib.kvcache_attention(ctypes.byref(cache.c), q.data_ptr(), q.stride(0), q.stride(1), _DTYPES[q.dtype], heads,
                                 ctypes.byref(s), scale, window, out.data_ptr(), out.stride(0), out.stride(1),
-                                lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+                                lse.data_ptr(), *_workspace(ws), _stream())
     return rc, out, lse
 
 
@@ -900,7 +912,7 @@ def kvcache_read(cache, pages, tokens, fault=None):
     """Returns (rc, k_codes, v_codes): int32 (tokens, kv_heads, head_dim) of the sequence whose pages are given."""
     assert pages.dtype == torch.int32 and pages.is_cuda and pages.is_contiguous() and pages.numel() * cache.c.page_tokens >= tokens
     k, v = (torch.empty(tokens, cache.c.kv_heads, cache.c.head_dim, dtype=torch.int32, device=pages.device) for _ in range(2))
-    rc = _lib.kvcache_read(ctypes.byref(cache.c), pages.data_ptr(), tokens, k.data_ptr(), v.data_ptr(), _optional(fault), _stream())
+    rc = _lib.kvcache_read(ctypes.byref(cache.c), pages.data_ptr(), tokens, k.data_ptr(), v.data_ptr(), _fault(fault), _stream())
     return rc, k, v
 
 
@@ -925,7 +937,7 @@ def w4_matvec(x, codes, scales, group, unit=1.0, out=None, ws=None):
     if ws is None and need:
         ws = _ws(need)
     rc = _lib.w4_matvec(out.data_ptr(), out.stride(0), x.data_ptr(), x.stride(0), dtype, rows, codes.data_ptr(),
-                        scales.data_ptr(), n, k, group, unit, _optional(ws), ws.numel() if ws is not None else 0, _stream())
+                        scales.data_ptr(), n, k, group, unit, *_workspace(ws), _stream())
     return rc, out
 
 
@@ -962,6 +974,6 @@ def logprobs(logits, targets=None, top=0, ws=None):
     need = _lib.logprobs_workspace_bytes(rows, vocab, top)
     if ws is None and need:
         ws = _ws(need)
-    rc = _lib.logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab, _optional(targets), top,
-                       ctypes.byref(o), _optional(ws), ws.numel() if ws is not None else 0, _stream())
+    rc = _lib.logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab,
+                       targets.data_ptr() if given else None, top, ctypes.byref(o), *_workspace(ws), _stream())
     return rc, r

@@ -327,7 +327,8 @@ extern "C" int kvcache_read(const kvcache_i8* cache, const int32_t* pages, size_
                             uint32_t* fault, void* stream) {
     if (!cache_ok(cache) || tokens >= 0x80000000u) return ZK_E_BADARG;
     if (tokens == 0) return ZK_OK;
-    if (!pages || !k_codes || !v_codes || !aligned(pages, 4) || !aligned(k_codes, 4) || !aligned(v_codes, 4)) return ZK_E_BADARG;
+    if (!pages || !k_codes || !v_codes || !aligned(pages, 4) || !aligned(k_codes, 4) || !aligned(v_codes, 4) || (fault && !aligned(fault, 4)))
+        return ZK_E_BADARG;
     hipLaunchKernelGGL(k_read, dim3((unsigned)tokens), dim3(kBlock), 0, as_stream(stream), *cache, pages,
                        (uint32_t)log2_floor(cache->page_tokens), k_codes, v_codes, fault);
     ZK_HIP_TRY(hipGetLastError());
