@@ -620,10 +620,12 @@ int kvcache_read(const kvcache_i8* cache, const int32_t* pages, size_t tokens, i
  * step of the whole matrix.  n <= 2^24; k is a multiple of 32, at most 2^20.
  *
  * y[m][i] = unit * sum_j w[i][j] x[m][j] for `rows` vectors x (rows x k, y: rows x n, the
- * rows' strides given; x's rows 16-byte aligned).  ZK_F32, ZK_F16, ZK_BF16: y has the type of x; sums are
- * accumulated in 32 bits.  A row of x with a value that is not finite gives NaN.  ZK_I16: x are 16-bit integers, y are
+ * rows' strides given; x's rows 16-byte aligned), 0 <= rows <= 2^20.  ZK_F32, ZK_F16, ZK_BF16: y has the type of x;
+ * weights and x (32-bit ones from 2^-100 on) enter exactly, whatever stands beside them, and sums are accumulated
+ * in 32 bits.  Those of |x| < 2^88 stay finite; beyond, y may be an infinity or NaN where the sum itself could be held.  A row of x
+ * with a value that is not finite gives NaN.  ZK_I16: x are 16-bit integers, y are
  * int64_t and the sums themselves, exactly (unit is ignored): the Y that
- * matmul_sumcheck_prove_i16 proves for X = x and W = w4_expand_i16.   |x| < 2^120, else NaN.  0 <= rows <= 2^20.
+ * matmul_sumcheck_prove_i16 proves for X = x and W = w4_expand_i16.
  * ws: device, w4_matvec_workspace_bytes(dtype, rows, k) (0 for few rows and inputs: ws may be NULL then). */
 size_t w4_matvec_workspace_bytes(int dtype, size_t rows, size_t k);
 int w4_matvec(void* y, size_t y_row_stride, const void* x, size_t x_row_stride, int dtype, size_t rows, const uint8_t* codes,

@@ -149,3 +149,25 @@ def test_f32_of_few_weights(zk, rows, n):
     w = (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
     size = x.double() @ w.abs()
     assert ((y.double() - x.double() @ w).abs() <= 96 * 2.0 ** -24 * size).all()
+
+
+@pytest.mark.parametrize("rows,n,k,group", [(1, 40, 4096, 128), (6, 40, 4096, 32), (40, 9000, 320, 64), (40, 16400, 288, 32), (2, 20, 1 << 20, 128),
+                                            (20, 20, 1 << 20, 32)])
+def test_as_large_as_x_may_be(zk, rows, n, k, group):
+    """The largest bf16 below 2^88 by codes of one sign, -8 and 4: with 2^20 of them, what is summed comes nearest to 2^128.
+    With scales of 2^11 every partial sum is 255 times a whole number of at most 2^20 / 32, times a power of two: 23 bits, so the
+    result is exact in whatever order.  With scales of 4095 it is finite."""
+    codes = torch.full((n, k // 2), 0xcc, dtype=torch.uint8, device="cuda")
+    codes[1::2] = 0
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.full((rows, k), 255 * 2.0 ** 80, dtype=dtype, device="cuda")
+        x[1::2] *= -1
+        for scale in (2048, 4095):
+            scales = torch.full((n, -(-k // group)), scale, dtype=torch.int16, device="cuda")
+            rc, y = zk.w4_matvec(x, codes, scales, group, 2.0 ** -18)
+            assert rc == zk.ZK_OK
+            want = x.double() @ (serve_ref.weights(codes, scales, group).double().t() * 2.0 ** -18).contiguous()
+            if scale == 2048:
+                assert torch.equal(y, want.to(dtype))
+            else:
+                assert y.isfinite().all() and torch.equal(y.sign().double(), want.sign())
