@@ -273,19 +273,22 @@ __global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, F
     }
 }
 
-// A workgroup: one token; keys and values, in order of head and dimension.
-__global__ __launch_bounds__(kBlock) void k_read(kvcache_i8 cache, const int32_t* pages, uint32_t page_log, int32_t* k, int32_t* v,
+// A workgroup: one token, and of more tokens than a grid of them has workgroups the next after as many; keys and values, in order
+// of head and dimension.
+static const uint32_t kReadGrid = 1u << 20;  // a launch ends at 2^32 threads
+__global__ __launch_bounds__(kBlock) void k_read(kvcache_i8 cache, const int32_t* pages, uint32_t page_log, size_t tokens, int32_t* k, int32_t* v,
                                                  uint32_t* fault) {
-    const size_t t = blockIdx.x;
-    const uint32_t T = 1u << page_log, d = cache.head_dim, H = cache.kv_heads, slot = (uint32_t)t & (T - 1);
-    const uint32_t page = (uint32_t)pages[t >> page_log];
-    const bool ok = page < cache.pages;
-    if (!ok && threadIdx.x == 0 && fault) atomicOr(fault, (uint32_t)ZK_FAULT_PAGE);
-    for (uint32_t i = threadIdx.x; i < H * d; i += kBlock) {
-        const uint32_t h = i / d, c = i % d;
-        const size_t at = ((size_t)page * H + h) * T * d;
-        k[t * H * d + i] = ok ? cache.k[at + (size_t)slot * d + c] : 0;
-        v[t * H * d + i] = ok ? cache.v[at + ((size_t)c << page_log) + slot] : 0;
+    const uint32_t T = 1u << page_log, d = cache.head_dim, H = cache.kv_heads;
+    for (size_t t = blockIdx.x; t < tokens; t += gridDim.x) {
+        const uint32_t slot = (uint32_t)t & (T - 1), page = (uint32_t)pages[t >> page_log];
+        const bool ok = page < cache.pages;
+        if (!ok && threadIdx.x == 0 && fault) atomicOr(fault, (uint32_t)ZK_FAULT_PAGE);
+        for (uint32_t i = threadIdx.x; i < H * d; i += kBlock) {
+            const uint32_t h = i / d, c = i % d;
+            const size_t at = ((size_t)page * H + h) * T * d;
+            k[t * H * d + i] = ok ? cache.k[at + (size_t)slot * d + c] : 0;
+            v[t * H * d + i] = ok ? cache.v[at + ((size_t)c << page_log) + slot] : 0;
+        }
     }
 }
 
@@ -329,8 +332,8 @@ extern "C" int kvcache_read(const kvcache_i8* cache, const int32_t* pages, size_
     if (tokens == 0) return ZK_OK;
     if (!pages || !k_codes || !v_codes || !aligned(pages, 4) || !aligned(k_codes, 4) || !aligned(v_codes, 4) || (fault && !aligned(fault, 4)))
         return ZK_E_BADARG;
-    hipLaunchKernelGGL(k_read, dim3((unsigned)tokens), dim3(kBlock), 0, as_stream(stream), *cache, pages,
-                       (uint32_t)log2_floor(cache->page_tokens), k_codes, v_codes, fault);
+    hipLaunchKernelGGL(k_read, dim3(tokens < kReadGrid ? (unsigned)tokens : kReadGrid), dim3(kBlock), 0, as_stream(stream), *cache, pages,
+                       (uint32_t)log2_floor(cache->page_tokens), tokens, k_codes, v_codes, fault);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
