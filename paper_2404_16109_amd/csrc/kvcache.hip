@@ -156,9 +156,9 @@ __device__ void append_page(const Fresh& f, size_t x0, size_t row_stride, int hi
     }
 }
 
-// PAGES: calls that may fill pages, 256 threads.
+// PAGES: calls that may fill pages, 256 threads.  page0: of each sequence's pages, the launch's first.
 template <int DT, bool PAGES>
-__global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, Fresh fv, kv_seqs s, uint32_t page_log) {
+__global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, Fresh fv, kv_seqs s, uint32_t page_log, uint32_t page0) {
     __shared__ uint32_t most[4];
     const uint32_t tid = threadIdx.x, T = 1u << page_log, d = cache.head_dim, H = cache.kv_heads;
     const bool values = blockIdx.y >= H;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kBlock) void k_append(kvcache_i8 cache, Fresh fk, F
         return;
     }
     const int32_t first = q.len - q.rows, start = first > 0 ? first : 0;
-    const int64_t p = (int64_t)(start >> page_log) + blockIdx.x;
+    const int64_t p = (int64_t)(start >> page_log) + page0 + blockIdx.x;
     const int64_t from = p << page_log, to = from + T;
     const int lo = from > start ? 0 : (int)(start - from), hi = (int)((to < q.len ? to : q.len) - from);  // the page's new slots
     if (hi <= lo) return;
@@ -296,11 +296,14 @@ template <int DT>
 int append(const kvcache_i8& cache, const Fresh& fk, const Fresh& fv, const kv_seqs& s, hipStream_t stream) {
     const uint32_t T = cache.page_tokens, log = (uint32_t)log2_floor(T);
     const uint32_t span = s.max_new < s.rows ? s.max_new : s.rows;
-    const unsigned pages = (unsigned)(((size_t)T - 1 + span - 1) / T + 1);  // with the first slot the page's last
+    const uint32_t pages = (uint32_t)(((size_t)T - 1 + span - 1) / T + 1);  // with the first slot the page's last
     // one wavefront has enough to do with a head of a single token; beyond 16 values to each of its lanes, four
     const unsigned threads = (size_t)(span < T ? span : T) * cache.head_dim <= 1024 ? 64 : kBlock;
     auto* kernel = threads == kBlock ? k_append<DT, true> : k_append<DT, false>;
-    hipLaunchKernelGGL(kernel, dim3(pages, 2 * cache.kv_heads, s.seqs), dim3(threads), 0, stream, cache, fk, fv, s, log);
+    const uint32_t most = 1u << 20;  // pages: a launch ends at 2^32 threads across
+    for (uint32_t page0 = 0; page0 < pages; page0 += most)
+        hipLaunchKernelGGL(kernel, dim3(pages - page0 < most ? pages - page0 : most, 2 * cache.kv_heads, s.seqs), dim3(threads), 0, stream, cache, fk,
+                           fv, s, log, page0);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
