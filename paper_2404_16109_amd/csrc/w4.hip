@@ -40,6 +40,12 @@ static const size_t kMostRows = (size_t)1 << 20;    // 32768 blocks of columns a
 // of them) 23.2 and 19.3, by 13824 x 5120 30 and 19.5; 64 by 5120 x 5120 21 and 29, by 13824 x 5120 49 and 30; 100 by 4096 x
 // 4096 28 and 25.
 static const uint32_t kManyOutputs = 8192, kBlocksOfFew = 6;
+// Of 32-bit vectors, whose blocks of 16 columns are five vectors, four blocks and more lose against the other kernel sooner, if that
+// makes up for few outputs with blocks of two tiles, ten vectors.  Measured, us, blocks of five against blocks of ten (and of 32):
+// 16 vectors by 5120 x 5120 22.6 and 18.3 (25.2), 32 33.9 and 27.9 (33.2), 32 by 4096 x 11008 48.8 and 36.2 (68.8), 20 by 8000 x 4096 31.6
+// and 15.8 (21.2), 32 by 3000 x 5120 24.3 and 18.8 (33.0); but 16 by 2000 x 8192 16.5 and 24.9, 32 by 1000 x 5120 13.3 and 18.1, and 6
+// by 5120 x 5120 15.5 and 17.6.
+static const uint32_t kTens = 10, kTensOutputs = 2560;
 // What a CU has of LDS.  The kernel for few columns keeps the scales of all groups there, 32 bytes to a group: of more inputs than
 // 163840 (groups of 32), 327680 (64) or 655360 (128) a call of whatever rows goes to the kernel for many columns, which keeps
 // those of a chunk.
@@ -614,15 +620,16 @@ Way way_of(size_t rows, uint32_t n, uint32_t k, uint32_t group_log) {
     constexpr uint32_t parts = Kind<DT>::parts;
     Way w = {};
     w.k8 = (uint32_t)align_up(k, kStep) / 8;
-    if (scales_bytes(w.k8, group_log) <= kMostLds &&
-        (rows <= (size_t)Kind<DT>::vectors || (n < kManyOutputs && rows * parts <= 16 * kBlocksOfFew))) {
+    const bool between = n < kManyOutputs && rows * parts <= 16 * kBlocksOfFew;
+    const bool tens = DT == ZK_F32 && between && rows > kTens && n >= kTensOutputs;
+    if (scales_bytes(w.k8, group_log) <= kMostLds && (rows <= (size_t)Kind<DT>::vectors || (between && !tens))) {
         w.tiles = 1;
         w.vectors = Kind<DT>::vectors;
         w.blocks = (uint32_t)div_up(rows, w.vectors);
         w.staged = w.blocks == 1 && (size_t)w.k8 * 8 * rows * parts <= kStageHalves;
     } else {
         // blocks of at most 96 columns, as like as they can be, two, four or six tiles each
-        const size_t most = 96 / parts;
+        const size_t most = tens ? kTens : 96 / parts;
         const size_t blocks = div_up(rows, most), v = div_up(rows, blocks);
         w.tiles = v * parts <= 32 ? 2 : v * parts <= 64 ? 4 : 6;
         w.vectors = (uint32_t)v;
@@ -723,7 +730,7 @@ namespace {
 template <int DT>
 size_t workspace(size_t rows, uint32_t k) {  // whatever the number of outputs and the groups
     size_t most = 0;
-    for (uint32_t n : {1u, 1u << 24})
+    for (uint32_t n : {1u, kTensOutputs, 1u << 24})
         for (uint32_t group_log : {5u, 7u}) {  // where scales are the longest and the shortest
             const size_t need = way_bytes(way_of<DT>(rows, n, k, group_log));
             most = need > most ? need : most;

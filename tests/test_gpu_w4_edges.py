@@ -171,3 +171,19 @@ def test_as_large_as_x_may_be(zk, rows, n, k, group):
                 assert torch.equal(y, want.to(dtype))
             else:
                 assert y.isfinite().all() and torch.equal(y.sign().double(), want.sign())
+
+
+@pytest.mark.parametrize("n", [2559, 2560, 3001, 8191, 8192])
+@pytest.mark.parametrize("rows", [10, 11, 21, 32, 33])
+def test_f32_by_outputs_between(zk, rows, n):
+    """Where calls change from blocks of five vectors to blocks of ten, and to all in one; tolerance as in test_gpu_w4."""
+    for k, group in ((416, 32), (1056, 128)):
+        unit = 2.0 ** -14
+        gen, codes, scales = make(n, k, group, rows + n)
+        x = torch.randn(rows, k, generator=gen, device="cuda")
+        ws = torch.empty(zk.w4_matvec_workspace_bytes(torch.float32, rows, k), dtype=torch.uint8, device="cuda")
+        rc, y = zk.w4_matvec(x, codes, scales, group, unit, ws=ws)
+        assert rc == zk.ZK_OK
+        want = x.double() @ (serve_ref.weights(codes, scales, group).double().t() * unit).contiguous()
+        tol = bound(x, codes, scales, group, unit) + 2.0 ** -24 * want.abs()
+        assert ((y.double() - want).abs() <= tol).all()
