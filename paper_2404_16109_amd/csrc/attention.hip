@@ -4,9 +4,11 @@
 // over the keys j that a query sees.  One pass over the keys with a running maximum:
 //   * in units of log2: t_j = s_j log2(e) + b_j, M = max t_j - 14, P_j = 2^(t_j - M).  The scale of V is an exponent and
 //     joins the score's, so the weights of all pages enter ONE accumulator of products with the codes as they are, whatever
-//     their scales; the sum of the weights is l = sum_j P_j 2^-b_j.  P is at most 2^14: as a 16-bit float with its 11 bits
-//     it reaches 29 binades below the largest at full precision and 10 more at less.  Exponents lie in [-40, 40], so a
-//     score that matters is never below what a 32-bit P holds.
+//     their scales; the sum of the weights is l = sum_j P_j 2^-b_j, in 32 bits.  For the product P is rounded to 11 bits, a
+//     16-bit float, as the matrix cores take it beside codes that are exact there: bf16 outputs lose nothing by it (1.6e-3 of their
+//     size, the rounding of the output alone), f16 outputs up to 2.8e-4 where that alone is 2.0e-4.  P is at most
+//     2^14: it reaches 29 binades below the largest at full precision and 10 more at less.  Exponents lie in [-40, 40], so
+//     a score that matters is never below what a 32-bit P holds.
 //   * codes become 16-bit floats by putting the byte (with its top bit flipped) under the exponent of 1024 and taking 1152
 //     off: exact, five instructions for four codes.  q is scaled by a power of two to just below 2^15, which a 16-bit float
 //     holds exactly but for elements 2^-29 of the row's largest.
@@ -19,12 +21,13 @@
 // loads of 1 KiB, so that the eight wavefronts of a CU have 128 KiB on the way.  k_attend_few: four wavefronts share a
 // workgroup's part of a sequence, `splits` workgroups the sequence, or eight wavefronts have all of a short one; k_attend_shared:
 // as many workgroups as the chip holds share all sequences; k_attend_join adds up.  Measured: one sequence of 131071
-// tokens, 8 heads of 128 (268 MB) 60 us, 4.5 TB/s, where a copy of that size reaches 4.8; one of 777 tokens 10.1 us, of which
-// 1.7 are the launch and some 6 three trips to memory, one after the other, and the CU's 64 bytes a clock.
-// Many rows (k_attend_many: 128 to a workgroup): codes are widened once and shared through LDS, a tile ahead; bound by the
-// vector ALU (per row and key some 13 of its cycles, the exponential among them, beside 8 of the matrix cores).  Row tiles
-// are taken with those that see most first, over all heads: 84 us for a prompt of 2048 tokens and 40 heads (43 GFLOP,
-// 515 TFLOP/s; head by head it was 160), 600 TFLOP/s for four such prompts.
+// tokens, 8 heads of 128 (268 MB) 59 us, 4.5 TB/s, where a copy of that size reaches 4.8; one of 777 tokens 10.1 us, four workgroups
+// to a head and then the join: latency, of the lengths and pages, the keys, the values, and of the parts in a second launch.
+// Many rows (k_attend_many: 128 to a workgroup): codes are widened once and shared through LDS, a tile ahead.  A wavefront's 32
+// rows and 64 keys take 466 vector instructions (1860 cycles; exponentials, roundings, scales, masks) and 1020 cycles of the matrix
+// cores; at two wavefronts to a SIMD little of one hides behind the other: vector ALU 50% busy, matrix cores 26%, LDS 24%.  Row
+// tiles are taken with those that see most first, over all heads: 82 us for a prompt of 2048 tokens and 40 heads (43 GFLOP,
+// 523 TFLOP/s; head by head it was 160), 600 TFLOP/s for four such prompts.
 #include "attend_pieces.h"
 #include "kvcache.h"
 

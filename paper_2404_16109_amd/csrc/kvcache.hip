@@ -6,9 +6,10 @@
 // by a power of two is exact, so rint(x * 2^-e) is the only rounding of a new code, and rint(c * 2^-shift) of an old one.
 //
 // Bound by bytes for prompts (pages that begin are read once, others twice, the second time from the L2, and one byte of each
-// value is written), by the chain of four dependent loads for single tokens.
-// Measured: 7 prompts of up to 2048 tokens, 40 heads of 128 (235 MB) 56 us, 4.2 TB/s (read a second time and transposed by
-// two-byte loads: 88); a token of each of 32 sequences 4.5 us.
+// value is written; the vector ALU is 81% busy then), by the chain of four dependent loads for single tokens.
+// Measured: 7 prompts of up to 2048 tokens, 40 heads of 128 (235 MB) 56 us, 4.2 TB/s; a token of each of 32 sequences 4.5 us.  Pages
+// of more than kPageInRegs codes, and rows that no wide load takes, are read a second time and transposed by two-byte loads: 88 us
+// where the other way takes 56.
 #include "kvcache.h"
 
 namespace zkmi {

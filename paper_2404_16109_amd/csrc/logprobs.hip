@@ -12,9 +12,10 @@
 // of 64-bit keys (value, then lower index).  Where too many reach the bound (ties, rows that allow less than `top`
 // tokens, NaN) the keys are taken out one after the other instead.
 //
-// Bound by the bytes of the logits, and for 16-bit ones by the vector ALU: some 13 of its operations a value.  Measured:
-// 2048 rows of 50257 floats, 20 alternatives (412 MB) 112 us, 3.7 TB/s (a copy: 4.8); 4096 rows of 32001 bf16 95 us; 8 rows of
-// 32001, one launch, 8.4 us, the latency of a dozen dependent steps.
+// Bound by the vector ALU, 91% busy (31 instructions a value with 20 alternatives of 32-bit logits), the more so for 16-bit ones, of
+// half the bytes.  Measured: 2048 rows of 50257 floats, 20 alternatives (412 MB) 112 us, 3.7 TB/s (a copy: 4.8), but 550 where all
+// but 50 of a row's tokens are -inf, and the keys are taken out one after the other; 4096 rows of 32001 bf16 106 us with 5
+// alternatives, 81 without; 8 rows of 32001, one launch, 8.4 us, the latency of a dozen dependent steps.
 #include "serve_dev.h"
 
 namespace zkmi {

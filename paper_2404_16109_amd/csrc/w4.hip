@@ -22,9 +22,11 @@
 // to one group: four exchanges of lane rows transpose the 4 x 4 words.  Of a word's eight half bytes i and i + 4 come to
 // lie in one register, so x is kept in the order 0 4 1 5 2 6 3 7.
 //
-// Bound by the weights' bytes where they are many and the vectors few, by latency below some 20 MB, by LDS and the vector ALU
-// for many columns.  Measured: one vector of bf16 by 5120 x 5120 (13.5 MB) 7.9 us, by 32001 x 5120 (84 MB) 22 us, 3.8 TB/s; 8 of
-// 16-bit integers by 4096 x 11008 15.5 us; 64 of bf16 by 32001 x 5120 45 us, 465 TFLOP/s; 32 of 32 bits 48 us.
+// Bound by the weights' bytes where they are many and the vectors few, by latency below some 20 MB.  For many columns nothing is
+// full (96 columns of 32-bit vectors: vector ALU 50% busy, matrix cores 29%, LDS 25%): two wavefronts to a SIMD, in step with each
+// other, hide little.  Measured: one vector of bf16 by 5120 x 5120 (13.5 MB) 7.5 us, by 32001 x 5120 (84 MB) 22 us, 3.8 TB/s; 8 of
+// 16-bit integers by 4096 x 11008 14.7 us; 64 of bf16 by 32001 x 5120 45 us, 465 TFLOP/s; 32 of 32 bits 51 us; 512 of bf16 by 5120
+// x 5120 78 us, 346 TFLOP/s, of 16-bit integers 141.
 #include "serve_dev.h"
 
 namespace zkmi {
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(512) void k_w4_many(void* y, size_t ystride, const 
         uint16_t s[NT];
     };
     // Chunks under way ahead of the one at work.  Two and one, us, 32001 x 5120: 32 vectors of bf16 33.3 and 38.5, 64 45.6 and
-    // 44.7 (groups of 32: 66 and 50, registers spill), 32 of 32 bits 49.9 and 48.3: with four tiles the work is the longer part.
+    // 44.7 (groups of 32: 66 and 50, registers spill): with four tiles the work is the longer part.
     constexpr int D = CT <= 2 ? 2 : 1;
     Load load[D];
     auto ask = [&](Load& to, uint32_t chunk) {
