@@ -638,7 +638,7 @@ int w4_expand_i16(int16_t* W, const uint8_t* codes, const uint16_t* scales, size
 /* What an answer is reported with, from rows x vocab logits (vocab <= 2^19): per
  * row, with p = softmax(logits),
  *   lse      log sum exp(logits)
- *   target   log p of the given token: logits[targets[r]] - lse; NaN if targets[r] is no token
+ *   target   log p of the given token: logits[targets[r]] - lse, lse not rounded before; NaN if targets[r] is no token
  *   rank     how many tokens come before it, by larger logit, among equals by lower index; -1 if no token
  *   entropy  -sum p log p
  *   top_ids, top   the `top` (0 <= top <= LOGPROBS_MAX_TOP, at most vocab) first tokens in

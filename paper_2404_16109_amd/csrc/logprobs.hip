@@ -1,10 +1,10 @@
 // Log probabilities of given tokens, with rank, entropy and the first alternatives.
 //
 // With m the largest of a row's logits x_i, l = sum exp(x_i - m) and t = sum exp(x_i - m) (x_i - m):
-//   lse = m + log l,   log p_i = x_i - lse,   -sum p log p = log l - t / l,
-// so one pass over the row is enough.  A row is cut into segments; a workgroup holds its segment in registers (128 bytes
-// to a thread), takes the largest first and then the sums relative to it, and leaves (m, l, t), the count for the rank and
-// its `top` first values; a wavefront per row joins the segments.
+//   lse = m + log l,   log p_i = (x_i - m) - log l,   -sum p log p = log l - t / l,
+// so one pass over the row is enough (and what all logits have in common costs log p no bits).  A row is cut into segments; a
+// workgroup holds its segment in registers (128 bytes to a thread), takes the largest first and then the sums relative to it, and
+// leaves (m, l, t), the count for the rank and its `top` first values; a wavefront per row joins the segments.
 //
 // The first `top` of a segment: of W wavefronts each finds, among its 64 largest-of-a-thread, the (top / W)-th largest; at
 // least `top` values reach the smallest of these bounds.  The values that reach it,
@@ -60,20 +60,19 @@ struct Results {
 __device__ void row_results(const Results& r, size_t row, const Part& p, uint32_t vocab, float xt) {
     const float base = fabsf(p.m) == kInf ? 0.0f : p.m;
     const float logl = logf(p.l);
-    const float lse = base + logl;
     const bool none = p.l == 0.0f;
-    if (r.out.lse) r.out.lse[row] = lse;
+    if (r.out.lse) r.out.lse[row] = base + logl;
     if (r.out.entropy) r.out.entropy[row] = none ? 0.0f : logl - p.t / p.l;
     if (r.targets) {
         const bool given = (uint32_t)r.targets[row] < vocab;
-        r.out.target[row] = !given ? __builtin_nanf("") : none ? -kInf : xt - lse;
+        r.out.target[row] = !given ? __builtin_nanf("") : none ? -kInf : (xt - base) - logl;
         r.out.rank[row] = given ? (int32_t)p.before : -1;
     }
 }
 __device__ __forceinline__ void top_result(const Results& r, size_t row, uint32_t place, uint64_t key, float m, float l) {
     const float base = fabsf(m) == kInf ? 0.0f : m;
     r.out.top_ids[row * r.top + place] = (int32_t)~(uint32_t)key;
-    r.out.top[row * r.top + place] = l == 0.0f ? -kInf : value_of((uint32_t)(key >> 32)) - (base + logf(l));
+    r.out.top[row * r.top + place] = l == 0.0f ? -kInf : (value_of((uint32_t)(key >> 32)) - base) - logf(l);
 }
 
 // Workgroup (segment, row); CPT: chunks of a thread.  A row is read in chunks of 16 bytes that are aligned whatever the row's address: chunk c holds
