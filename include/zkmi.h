@@ -550,7 +550,8 @@ typedef struct {
  * which are the rows cu[b] .. cu[b+1]-1 of the call's tensors (cu[0] = 0, not
  * decreasing, cu[seqs] <= rows) and the sequence's last: row i of them is the token
  * at position lens[b] - (cu[b+1]-cu[b]) + i.  A row whose position is negative is no
- * token: nothing is stored for it, and as a query it sees no key.  Token t lies in
+ * token: nothing is stored for it, and as a query it sees no key.  Rows behind
+ * cu[seqs] are nobody's: neither read nor written.  Token t lies in
  * page table[b * table_stride + t / page_tokens]; entries that no token needs are
  * not used.  cu, lens and table are device arrays.  max_new: the most rows any
  * sequence has (host; at least 1).  max_len: about the longest lens[b] (host; it
