@@ -523,7 +523,7 @@ int zkattn_link_verify(const uint8_t seed[32], const uint8_t* proof, size_t len,
  * Floating tensors are of one of these types; the innermost dimension is
  * contiguous, the other strides are given in elements.  Every pointer is aligned
  * to its element type, and what a comment says beyond that. */
-enum { ZK_F32 = 0, ZK_F16 = 1, ZK_BF16 = 2, ZK_I16 = 3 };
+enum { ZK_F32 = 0, ZK_F16 = 1, ZK_BF16 = 2, ZK_I16 = 3, ZK_I32 = 4 };
 
 /* A paged cache of keys and values.  A page holds page_tokens tokens (16, 32, 64,
  * 128 or 256) of all kv_heads heads; head_dim is a multiple of 16, at most 256.
@@ -660,6 +660,69 @@ typedef struct {
 size_t logprobs_workspace_bytes(size_t rows, size_t vocab, uint32_t top);
 int logprobs(const void* logits, size_t row_stride, int dtype, size_t rows, size_t vocab, const int32_t* targets, uint32_t top,
              const logprobs_out* out, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- a decoder layer in 8 bits: activations as codes ---------------------------
+ *
+ * Rows of activations as signed codes with one scale each: a code c of row m stands
+ * for c * scales[m].  Codes are defined bit for bit, so that the integers a proof is
+ * made of are the same whoever computes them:
+ *   amax = the row's largest magnitude, scale = amax / 127, code = rint(x * (127 / amax)),
+ * every quotient and product rounded to 32 bits, rint: ties to even.  A row whose amax is below 2^-100 is
+ * zeros with scale 0; one with a value that is not finite is zeros with scale NaN, which a product hands on to
+ * its outputs.  x: rows x k of a float type, codes: rows x k, scales: rows.  Any row strides of at least k;
+ * rows < 2^31, 1 <= k <= I8_MAX_K. */
+#define I8_MAX_K 131056
+int i8_quantise(int8_t* codes, size_t codes_row_stride, float* scales, const void* x, size_t x_row_stride, int dtype, size_t rows,
+                size_t k, void* stream);
+
+/* y[m][i] = (sum_j x[m][j] w[i][j]) * x_scales[m] * w_scales[i]: rows vectors x of k signed
+ * 8-bit integers (-128 among them) by the weights w of n outputs, [n][k], with a scale for each token
+ * and each output.  The sum is exact in 32 bits; then a float of 32 bits, and each product
+ * is rounded to 32 bits, the last to y's type (ZK_F32, ZK_F16, ZK_BF16).
+ * ZK_I32: y are the sums themselves, int32_t, and the scales are not read (may be NULL): the Y that matmul_sumcheck_prove_i16
+ * proves for the same integers in 16 bits.  k is a multiple of 16, 16 <= k <= I8_MAX_K; n, rows <= 2^24; x and
+ * w 16-byte aligned, x_row_stride a multiple of 16 and at most 2^23; y rows x n, any row stride of at least n.
+ * ws: device, i8_matmul_workspace_bytes(rows, n, k) (0 where there are outputs enough: ws may be NULL then). */
+size_t i8_matmul_workspace_bytes(size_t rows, size_t n, size_t k);
+int i8_matmul(void* y, size_t y_row_stride, int y_dtype, const int8_t* x, size_t x_row_stride, const float* x_scales, size_t rows,
+              const int8_t* w, const float* w_scales, size_t n, size_t k, void* ws, size_t ws_bytes, void* stream);
+
+/* What stands between two blocks of a layer, row by row (a token each):
+ *   t = norm(z) * post_gain + post_bias    what the block before gave, behind it perhaps a norm (post_norm)
+ *   r = alpha * x + gate * t               the residual stream
+ *   h = norm(r) * gain + bias              what the block behind is given (norm)
+ * ZK_NORM_RMS: norm(v) = v / sqrt(mean(v^2) + eps); ZK_NORM_LAYER: (v - mean) / sqrt(mean((v - mean)^2) + eps);
+ * ZK_NORM_NONE: v.  All tensors are of one float type; x, z, r, h rows x dim with their row strides, gains and
+ * biases dim, gate rows x dim, or one row for all with gate_row_stride 0.  NULL: z no block (then neither
+ * post_*, nor gate), gains and gate are ones, biases zeros, r is not stored.  h goes to h, or as codes and scales (as i8_quantise of h
+ * in 32 bits) to codes and scales, or nowhere.  r and h may be the tensors x and z themselves, with
+ * their strides, either way round; no other output overlaps another tensor.
+ * Means are taken in 64 bits; the mean itself and 1 / sqrt(...) are rounded to 32 bits, and every operation after them, in the
+ * order written, once.  h is that of r as it is stored (rounded to the type).  1 <= dim <= 32768,
+ * rows < 2^31, eps > 0 (if there is a norm), alpha finite. */
+enum { ZK_NORM_NONE = 0, ZK_NORM_RMS = 1, ZK_NORM_LAYER = 2 };
+typedef struct {
+    const void* x;
+    size_t x_row_stride;
+    const void* z;
+    size_t z_row_stride;
+    const void* gate;
+    size_t gate_row_stride;
+    const void* post_gain;
+    const void* post_bias;
+    const void* gain;
+    const void* bias;
+    void* r;
+    size_t r_row_stride;
+    void* h;
+    size_t h_row_stride;
+    int8_t* codes;
+    size_t codes_row_stride;
+    float* scales;
+    int post_norm, norm;
+    float alpha, eps;
+} block_norm_args; /* device pointers */
+int block_norm(const block_norm_args* args, int dtype, size_t rows, size_t dim, void* stream);
 
 /* The calling host thread's pinned state (see Ownership), for callers that want no
  * allocation inside their first proof: zkmi_thread_init allocates it now, with

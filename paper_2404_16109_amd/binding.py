@@ -78,6 +78,14 @@ class logprobs_out(ctypes.Structure):
                 ("entropy", ctypes.c_void_p), ("top_ids", ctypes.c_void_p), ("top", ctypes.c_void_p)]
 
 
+class block_norm_args(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_row_stride", ctypes.c_size_t), ("z", ctypes.c_void_p), ("z_row_stride", ctypes.c_size_t),
+                ("gate", ctypes.c_void_p), ("gate_row_stride", ctypes.c_size_t), ("post_gain", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("r", ctypes.c_void_p), ("r_row_stride", ctypes.c_size_t),
+                ("h", ctypes.c_void_p), ("h_row_stride", ctypes.c_size_t), ("codes", ctypes.c_void_p), ("codes_row_stride", ctypes.c_size_t),
+                ("scales", ctypes.c_void_p), ("post_norm", ctypes.c_int), ("norm", ctypes.c_int), ("alpha", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -172,6 +180,10 @@ def _load():
         "w4_expand_i16": (i32, [vp, vp, vp, sz, sz, ctypes.c_uint32, vp]),
         "logprobs_workspace_bytes": (sz, [sz, sz, ctypes.c_uint32]),
         "logprobs": (i32, [vp, sz, i32, sz, sz, vp, ctypes.c_uint32, P(logprobs_out), vp, sz, vp]),
+        "i8_quantise": (i32, [vp, sz, vp, vp, sz, i32, sz, sz, vp]),
+        "i8_matmul_workspace_bytes": (sz, [sz, sz, sz]),
+        "i8_matmul": (i32, [vp, sz, i32, vp, sz, vp, sz, vp, vp, sz, sz, vp, sz, vp]),
+        "block_norm": (i32, [P(block_norm_args), i32, sz, sz, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -196,7 +208,7 @@ EXPORTS = ["zkmi_version", "zkmi_thread_init", "zkmi_thread_release", "zkmi_self
            "zkattn_link_workspace_bytes", "zkattn_link_prove", "zkattn_link_prove_small",
            "zkattn_link_verify_workspace_bytes",
            "zkattn_link_verify", "kvcache_append", "kvcache_attention_workspace_bytes", "kvcache_attention", "kvcache_read",
-           "w4_matvec_workspace_bytes", "w4_matvec", "w4_expand_i16", "logprobs_workspace_bytes", "logprobs"]
+           "w4_matvec_workspace_bytes", "w4_matvec", "w4_expand_i16", "logprobs_workspace_bytes", "logprobs", "i8_quantise", "i8_matmul_workspace_bytes", "i8_matmul", "block_norm"]
 
 
 def raw():
@@ -825,7 +837,9 @@ def zkattn_link_verify(seed, proof, rows, cols, bases, Zp=None, X=None, Y=None, 
 
 # ---- quantised inference ------------------------------------------------------------------------
 
-ZK_F32, ZK_F16, ZK_BF16, ZK_I16 = 0, 1, 2, 3
+ZK_F32, ZK_F16, ZK_BF16, ZK_I16, ZK_I32 = 0, 1, 2, 3, 4
+ZK_NORM_NONE, ZK_NORM_RMS, ZK_NORM_LAYER = 0, 1, 2
+I8_MAX_K = 131056
 ZK_FAULT_LENGTH, ZK_FAULT_PAGE = 1, 2
 ZK_EXP_MIN, ZK_EXP_MAX, ZK_EXP_NAN = -40, 40, -128
 LOGPROBS_MAX_TOP = 32
@@ -977,3 +991,95 @@ def logprobs(logits, targets=None, top=0, ws=None):
     rc = _lib.logprobs(logits.data_ptr(), logits.stride(0), _DTYPES[logits.dtype], rows, vocab,
                        targets.data_ptr() if given else None, top, ctypes.byref(o), *_workspace(ws), _stream())
     return rc, r
+
+
+# ---- a decoder layer in 8 bits --------------------------------------------------------------------
+
+_FLOATS = {torch.float32: ZK_F32, torch.float16: ZK_F16, torch.bfloat16: ZK_BF16}
+_PRODUCTS = {**_FLOATS, torch.int32: ZK_I32}
+
+
+def _matrix(t, rows, cols, dtype, name):
+    """The address of a rows x cols tensor whose rows are contiguous."""
+    assert t.dtype == dtype and t.shape == (rows, cols) and t.is_cuda and (t.stride(1) == 1 or cols == 1), name
+    return t.data_ptr()
+
+
+def _vector(t, n, dtype, name):
+    """The address of a vector of n elements, or None."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.shape == (n,) and t.is_cuda and t.is_contiguous(), name
+    return t.data_ptr()
+
+
+def i8_quantise(x, codes=None, scales=None):
+    """x: (rows, k).  Returns (rc, codes, scales): int8 (rows, k) and float32 (rows), made where they are not given."""
+    rows, k = x.shape
+    if codes is None:
+        codes = torch.empty(rows, k, dtype=torch.int8, device=x.device)
+    if scales is None:
+        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    at = _matrix(x, rows, k, x.dtype, "x")
+    rc = _lib.i8_quantise(_matrix(codes, rows, k, torch.int8, "codes"), codes.stride(0), _vector(scales, rows, torch.float32, "scales"), at,
+                          x.stride(0), _FLOATS[x.dtype], rows, k, _stream())
+    return rc, codes, scales
+
+
+def i8_matmul_workspace_bytes(rows, n, k):
+    return _lib.i8_matmul_workspace_bytes(rows, n, k)
+
+
+def i8_matmul(x, w, x_scales=None, w_scales=None, out=None, dtype=torch.bfloat16, ws=None):
+    """x: int8 (rows, k), any row stride that is a multiple of 16; w: int8 (n, k), contiguous; scales: float32 (rows) and (n).  Returns
+    (rc, y): (rows, n) of `dtype`, or of out's; torch.int32: the sums themselves, without scales."""
+    rows, k = x.shape
+    n = w.shape[0]
+    if out is None:
+        out = torch.empty(rows, n, dtype=dtype, device=x.device)
+    y = _matrix(out, rows, n, out.dtype, "out")
+    assert w.is_contiguous(), "w: contiguous"
+    need = _lib.i8_matmul_workspace_bytes(rows, n, k)
+    if ws is None and need:
+        ws = _ws(need)
+    rc = _lib.i8_matmul(y, out.stride(0), _PRODUCTS[out.dtype], _matrix(x, rows, k, torch.int8, "x"), x.stride(0),
+                        _vector(x_scales, rows, torch.float32, "x_scales"), rows, _matrix(w, n, k, torch.int8, "w"),
+                        _vector(w_scales, n, torch.float32, "w_scales"), n, k, *_workspace(ws), _stream())
+    return rc, out
+
+
+def block_norm(x, z=None, *, norm=ZK_NORM_RMS, gain=None, bias=None, eps=1e-5, post_norm=ZK_NORM_NONE, post_gain=None, post_bias=None, gate=None,
+               alpha=1.0, quantise=False, r=None, h=None, scales=None):
+    """x, z: (rows, dim); gains and biases: (dim); gate: (dim) or (rows, dim), all of one type.  Returns (rc, r, h, scales): r the
+    residual stream (x where the call leaves it as it is), h what the next block is given, of x's type, or int8 codes (quantise=True, or
+    an int8 tensor as h) with scales: float32 (rows), else None.  r and h are made where they are not given."""
+    rows, dim = x.shape
+    kind = x.dtype
+    if r is None and (z is not None or alpha != 1.0):
+        r = torch.empty(rows, dim, dtype=kind, device=x.device)
+    if h is None:
+        h = torch.empty(rows, dim, dtype=torch.int8 if quantise else kind, device=x.device)
+    coded = h.dtype == torch.int8
+    if coded and scales is None:
+        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    a = block_norm_args()
+    a.x, a.x_row_stride = _matrix(x, rows, dim, kind, "x"), x.stride(0)
+    if z is not None:
+        a.z, a.z_row_stride = _matrix(z, rows, dim, kind, "z"), z.stride(0)
+    if gate is not None:
+        if gate.dim() == 1:
+            a.gate, a.gate_row_stride = _vector(gate, dim, kind, "gate"), 0
+        else:
+            a.gate, a.gate_row_stride = _matrix(gate, rows, dim, kind, "gate"), gate.stride(0)
+    a.post_gain, a.post_bias = _vector(post_gain, dim, kind, "post_gain"), _vector(post_bias, dim, kind, "post_bias")
+    a.gain, a.bias = _vector(gain, dim, kind, "gain"), _vector(bias, dim, kind, "bias")
+    if r is not None:
+        a.r, a.r_row_stride = _matrix(r, rows, dim, kind, "r"), r.stride(0)
+    if coded:
+        a.codes, a.codes_row_stride = _matrix(h, rows, dim, torch.int8, "h"), h.stride(0)
+        a.scales = _vector(scales, rows, torch.float32, "scales")
+    else:
+        a.h, a.h_row_stride = _matrix(h, rows, dim, kind, "h"), h.stride(0)
+    a.post_norm, a.norm, a.alpha, a.eps = post_norm, norm, alpha, eps
+    rc = _lib.block_norm(ctypes.byref(a), _FLOATS[kind], rows, dim, _stream())
+    return rc, x if r is None else r, h, scales if coded else None

@@ -1,0 +1,378 @@
+// Products of 8-bit integers: y[m][i] = (sum_j x[m][j] w[i][j]) * x_scales[m] * w_scales[i], or the sums themselves.
+//
+// Sums are exact in 32 bits (|x w| <= 2^14, k < 2^17), in whatever order: parts of k may be added up anywhere.
+//
+// Few rows (k_few: up to 64): the weights are read once, straight into registers, and bound the call.  A workgroup has 16 or 32
+// outputs, its eight wavefronts share k in steps of 128, so that every row of weights is read in whole lines.
+// Many rows (k_tiles): tiles of x and w come through LDS, put there by loads that pass no register, a step of 128 ahead; 16-byte
+// pieces lie in LDS at piece ^ (row & 7), so that eight neighbouring rows answer from different banks.  Where there are fewer tiles
+// than the chip holds, workgroups share k and k_join adds up.
+#include "serve_dev.h"
+
+#pragma clang fp contract(off)
+
+namespace zkmi {
+namespace {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
+
+struct Args {
+    void* y;
+    size_t yrow;
+    const int8_t* x;
+    size_t xrow;
+    const float* xs;
+    const int8_t* w;
+    const float* ws;
+    uint32_t rows, n, k;
+    uint32_t splits, each;  // of k: steps of kStep to a part
+    int32_t* parts;         // [split][row][n_pad]
+    uint32_t n_pad;
+    bool quads;             // y takes four outputs at once
+};
+static const uint32_t kStep = 128;  // of k
+
+// Four outputs of a row, from n0 on: those below n are stored.
+template <int Y>
+__device__ __forceinline__ void put_quad(const Args& a, uint32_t row, uint32_t n0, v4i s) {
+    if (n0 >= a.n) return;
+    const size_t at = (size_t)row * a.yrow + n0;
+    if constexpr (Y == ZK_I32) {
+        int32_t* y = (int32_t*)a.y + at;
+        if (a.quads && n0 + 4 <= a.n) *(v4i*)y = s;
+        else
+            for (uint32_t e = 0; e < 4 && n0 + e < a.n; ++e) y[e] = s[e];
+    } else {
+        const float xs = a.xs[row];
+        float f[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) f[e] = (float)s[e] * xs * (n0 + e < a.n ? a.ws[n0 + e] : 0.0f);
+        if (a.quads && n0 + 4 <= a.n) {
+            if constexpr (Y == ZK_F32) *(v4f*)((float*)a.y + at) = v4f{f[0], f[1], f[2], f[3]};
+            else
+                *(uint2*)((uint16_t*)a.y + at) = make_uint2((uint32_t)half_bits<Y>(f[0]) | ((uint32_t)half_bits<Y>(f[1]) << 16),
+                                                            (uint32_t)half_bits<Y>(f[2]) | ((uint32_t)half_bits<Y>(f[3]) << 16));
+        } else {
+            for (uint32_t e = 0; e < 4 && n0 + e < a.n; ++e) store_one<Y>(a.y, at + e, f[e]);
+        }
+    }
+}
+template <int Y>
+__device__ __forceinline__ void finish_quad(const Args& a, uint32_t split, uint32_t row, uint32_t n0, v4i s) {
+    if (a.splits == 1) return put_quad<Y>(a, row, n0, s);
+    if (n0 < a.n) *(v4i*)(a.parts + ((size_t)split * a.rows + row) * a.n_pad + n0) = s;
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------
+
+// RT: tiles of 16 rows; NT: of 16 outputs.  Lane 16 g + i: row (output) i of a tile, bytes 16 g .. 16 g + 15 of 64.
+static const int kWaves = 8, kAhead = 3;
+template <int RT, int NT, int Y>
+__global__ __launch_bounds__(64 * kWaves) void k_few(Args a) {
+    __shared__ v4i red[kWaves][RT * NT][64];
+    const uint32_t tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, i16 = lane & 15;
+    const uint32_t n0 = blockIdx.x * 16 * NT, split = blockIdx.y;
+    const uint32_t steps = (a.k + kStep - 1) / kStep, first = split * a.each, last = first + a.each < steps ? first + a.each : steps;
+    const int8_t* w[NT];
+    const int8_t* x[RT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const uint32_t o = n0 + 16 * t + i16;
+        w[t] = a.w + (size_t)(o < a.n ? o : a.n - 1) * a.k;
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const uint32_t r = 16 * t + i16;
+        x[t] = a.x + (size_t)(r < a.rows ? r : a.rows - 1) * a.xrow;
+    }
+    v4i acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[r][t] = v4i{0, 0, 0, 0};
+    v4i wr[kAhead][NT][2], xr[kAhead][RT][2];
+    // Every load is made: bytes behind k are the row's first, and zeros of x.
+    auto load = [&](uint32_t s, v4i(&wp)[NT][2], v4i(&xp)[RT][2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t j = s * kStep + 64 * u + 16 * g;
+            const uint32_t at = j < a.k ? j : 0;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) wp[t][u] = *(const v4i*)(w[t] + at);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) xp[t][u] = *(const v4i*)(x[t] + at);
+        }
+    };
+    auto multiply = [&](uint32_t s, const v4i(&wp)[NT][2], const v4i(&xp)[RT][2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bool in = s * kStep + 64 * u + 16 * g < a.k;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const v4i q = in ? xp[r][u] : v4i{0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wp[t][u], q, acc[r][t], 0, 0, 0);
+            }
+        }
+    };
+#pragma unroll
+    for (int p = 0; p < kAhead; ++p)
+        if (first + wave + p * kWaves < last) load(first + wave + p * kWaves, wr[p], xr[p]);
+    for (uint32_t s = first + wave; s < last; s += kAhead * kWaves) {
+#pragma unroll
+        for (int p = 0; p < kAhead; ++p) {
+            if (s + p * kWaves < last) {
+                multiply(s + p * kWaves, wr[p], xr[p]);
+                if (s + (p + kAhead) * kWaves < last) load(s + (p + kAhead) * kWaves, wr[p], xr[p]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) red[wave][r * NT + t][lane] = acc[r][t];
+    __syncthreads();
+    for (uint32_t i = tid; i < RT * NT * 64; i += 64 * kWaves) {
+        const uint32_t q = i >> 6, l = i & 63, row = 16 * (q / NT) + (l & 15);
+        if (row >= a.rows) continue;
+        v4i sum = red[0][q][l];
+#pragma unroll
+        for (int v = 1; v < kWaves; ++v) sum += red[v][q][l];
+        finish_quad<Y>(a, split, row, n0 + 16 * (q % NT) + 4 * (l >> 4), sum);
+    }
+}
+
+// ---- many rows -------------------------------------------------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) void lds_void;
+#define kOutside 0xfffffff0u  // an offset that no tile reaches: loads from there give zeros
+
+// MO, NR: tiles of 32 outputs and of 32 rows that a wavefront has; WO x WR wavefronts.
+template <int MO, int NR, int WO, int WR, int Y>
+__global__ __launch_bounds__(64 * WO * WR) void k_tiles(Args a, uint32_t row_tiles, uint32_t out_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host has no type for a buffer's descriptor
+    constexpr uint32_t waves = WO * WR, outs = 32 * MO * WO, rows = 32 * NR * WR;
+    constexpr int loads_w = outs / 8 / waves, loads_x = rows / 8 / waves;  // of a wavefront in a step: eight rows each
+    __shared__ __attribute__((aligned(16))) int8_t s0[(outs + rows) * kStep];
+    __shared__ __attribute__((aligned(16))) int8_t s1[(outs + rows) * kStep];
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
+    const uint32_t wo = wave % WO, wr = wave / WO, split = blockIdx.y;
+
+    // Workgroups go to the eight XCDs in turn; each gets tiles that lie together, eight row tiles by as many of outputs as come.
+    uint32_t id = blockIdx.x;
+    {
+        const uint32_t total = row_tiles * out_tiles, q = total >> 3, rest = total & 7, xcd = id & 7, in = id >> 3;
+        id = xcd * q + (xcd < rest ? xcd : rest) + in;
+    }
+    const uint32_t band = id / (8 * out_tiles), in_band = id - band * 8 * out_tiles;
+    const uint32_t band_rows = row_tiles - band * 8 < 8 ? row_tiles - band * 8 : 8;
+    const uint32_t r0 = (band * 8 + in_band % band_rows) * rows, o0 = in_band / band_rows * outs;
+
+    const uint32_t steps = (a.k + kStep - 1) / kStep, first = split * a.each, last = first + a.each < steps ? first + a.each : steps;
+    const uint32_t w_rows = a.n - o0 < outs ? a.n - o0 : outs, x_rows = a.rows - r0 < rows ? a.rows - r0 : rows;
+    __amdgpu_buffer_rsrc_t wb = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (size_t)o0 * a.k), 0, (w_rows - 1) * a.k + a.k, 0x00020000);
+    __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (size_t)r0 * a.xrow), 0, (x_rows - 1) * (uint32_t)a.xrow + a.k, 0x00020000);
+    // A lane brings piece (lane & 7) ^ (row & 7) of row lane / 8 of each eight.
+    const uint32_t sub = lane >> 3, piece = ((lane & 7) ^ sub) * 16;
+    uint32_t w_at[loads_w], x_at[loads_x];
+#pragma unroll
+    for (int i = 0; i < loads_w; ++i) {
+        const uint32_t r = (i * waves + wave) * 8 + sub;
+        w_at[i] = r < w_rows ? r * a.k + piece : kOutside;
+    }
+#pragma unroll
+    for (int i = 0; i < loads_x; ++i) {
+        const uint32_t r = (i * waves + wave) * 8 + sub;
+        x_at[i] = r < x_rows ? r * (uint32_t)a.xrow + piece : kOutside;
+    }
+    const uint32_t k_end = last * kStep < a.k ? last * kStep : a.k;
+    auto fetch = [&](uint32_t s, int8_t* to) {
+        const uint32_t j = s * kStep;
+        const bool in = j + piece < k_end;  // pieces behind the part are zeros
+#pragma unroll
+        for (int i = 0; i < loads_w; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wb, (lds_void*)(to + (i * waves + wave) * 1024), 16, in && w_at[i] != kOutside ? w_at[i] + j : kOutside, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < loads_x; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xb, (lds_void*)(to + outs * kStep + (i * waves + wave) * 1024), 16, in && x_at[i] != kOutside ? x_at[i] + j : kOutside, 0,
+                                                     0, 0);
+        __builtin_amdgcn_sched_barrier(0);  // all of them before the products of the step that is there
+    };
+    v16i acc[MO][NR];
+#pragma unroll
+    for (int o = 0; o < MO; ++o)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) acc[o][r] = v16i{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    const uint32_t w_row = (wo * MO * 32 + i32) * kStep, x_row = outs * kStep + (wr * NR * 32 + i32) * kStep;
+    // Operands are read a quarter of a step ahead of the products that take them.
+    auto multiply = [&](const int8_t* from) {
+        v4i w[2][MO], x[2][NR];
+        auto read = [&](int q) {
+            const uint32_t at = ((2 * q + half) ^ (i32 & 7)) * 16;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) x[q & 1][r] = *(const v4i*)(from + x_row + r * 32 * kStep + at);
+#pragma unroll
+            for (int o = 0; o < MO; ++o) w[q & 1][o] = *(const v4i*)(from + w_row + o * 32 * kStep + at);
+        };
+        read(0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (q < 3) read(q + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int o = 0; o < MO; ++o)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) acc[o][r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q & 1][o], x[q & 1][r], acc[o][r], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // What is on its way to LDS has come, and everybody is done with what it replaces next.
+    auto turn = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    fetch(first, s0);
+    turn();
+#pragma unroll 1
+    for (uint32_t s = first; s < last; s += 2) {
+        fetch(s + 1, s1);
+        multiply(s0);
+        turn();
+        fetch(s + 2, s0);
+        multiply(s1);
+        turn();
+    }
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const uint32_t row = r0 + (wr * NR + r) * 32 + i32;
+        if (row >= a.rows) continue;
+#pragma unroll
+        for (int o = 0; o < MO; ++o)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                finish_quad<Y>(a, split, row, o0 + (wo * MO + o) * 32 + 2 * e + 4 * half,
+                               v4i{acc[o][r][e], acc[o][r][e + 1], acc[o][r][e + 2], acc[o][r][e + 3]});
+    }
+#endif
+}
+
+template <int Y>
+__global__ __launch_bounds__(kBlock) void k_join(Args a) {
+    const uint32_t quads = a.n_pad >> 2;
+    const size_t i = (size_t)blockIdx.x * kBlock + threadIdx.x;
+    const size_t row = i / quads;
+    if (row >= a.rows) return;
+    const uint32_t n0 = (uint32_t)(i - row * quads) * 4;
+    v4i s = {0, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t p = 0; p < a.splits; ++p) s += *(const v4i*)(a.parts + ((size_t)p * a.rows + row) * a.n_pad + n0);
+    put_quad<Y>(a, (uint32_t)row, n0, s);
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+enum Tile { kFew16, kFew32, kFew64, kMid, kLarge };
+struct Plan {
+    Tile tile;
+    uint32_t nt, groups, splits, each;
+};
+Plan plan_of(size_t rows, size_t n, size_t k) {
+    Plan p = {};
+    const uint32_t steps = (uint32_t)div_up(k, kStep);
+    uint64_t want;
+    uint32_t least;  // steps worth a part
+    if (rows <= 64) {
+        p.tile = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
+        p.nt = div_up(n, 32) >= 256 ? 2 : 1;
+        p.groups = (uint32_t)div_up(n, 16 * p.nt);
+        want = 256;
+        least = 2 * kWaves;
+    } else {
+        const uint64_t large = div_up(rows, 256) * div_up(n, 256);
+        p.tile = large >= 192 ? kLarge : kMid;
+        p.groups = (uint32_t)(p.tile == kLarge ? large : div_up(rows, 128) * div_up(n, 128));
+        want = p.tile == kLarge ? 256 : 512;
+        least = 8;
+    }
+    uint64_t splits = p.groups >= want / 2 + 1 ? 1 : want / p.groups;
+    if (splits > steps / least) splits = steps / least;
+    if (splits < 1) splits = 1;
+    p.each = (uint32_t)align_up(div_up(steps, splits), 2);  // k_tiles takes two at a time
+    p.splits = (uint32_t)div_up(steps, p.each);
+    return p;
+}
+
+template <int Y>
+int launch(const Args& a, const Plan& p, hipStream_t s) {
+    const dim3 grid(p.groups, p.splits), few(64 * kWaves);
+    const uint32_t rt = (uint32_t)div_up(a.rows, p.tile == kLarge ? 256 : 128), nt = (uint32_t)div_up(a.n, p.tile == kLarge ? 256 : 128);
+    if (p.tile == kFew16 && p.nt == 1) hipLaunchKernelGGL((k_few<1, 1, Y>), grid, few, 0, s, a);
+    else if (p.tile == kFew16) hipLaunchKernelGGL((k_few<1, 2, Y>), grid, few, 0, s, a);
+    else if (p.tile == kFew32 && p.nt == 1) hipLaunchKernelGGL((k_few<2, 1, Y>), grid, few, 0, s, a);
+    else if (p.tile == kFew32) hipLaunchKernelGGL((k_few<2, 2, Y>), grid, few, 0, s, a);
+    else if (p.tile == kFew64 && p.nt == 1) hipLaunchKernelGGL((k_few<4, 1, Y>), grid, few, 0, s, a);
+    else if (p.tile == kFew64) hipLaunchKernelGGL((k_few<4, 2, Y>), grid, few, 0, s, a);
+    else if (p.tile == kMid) hipLaunchKernelGGL((k_tiles<2, 2, 2, 2, Y>), grid, dim3(256), 0, s, a, rt, nt);
+    else hipLaunchKernelGGL((k_tiles<4, 2, 2, 4, Y>), grid, dim3(512), 0, s, a, rt, nt);
+    if (p.splits > 1) hipLaunchKernelGGL((k_join<Y>), dim3((unsigned)div_up((size_t)a.rows * (a.n_pad >> 2), kBlock)), dim3(kBlock), 0, s, a);
+    ZK_HIP_TRY(hipGetLastError());
+    return ZK_OK;
+}
+
+bool sizes_ok(size_t rows, size_t n, size_t k) {
+    return rows <= (size_t)1 << 24 && n >= 1 && n <= (size_t)1 << 24 && k >= 16 && k % 16 == 0 && k <= I8_MAX_K;
+}
+
+}  // namespace
+}  // namespace zkmi
+
+using namespace zkmi;
+
+extern "C" size_t i8_matmul_workspace_bytes(size_t rows, size_t n, size_t k) {
+    if (rows == 0 || !sizes_ok(rows, n, k)) return 0;
+    const Plan p = plan_of(rows, n, k);
+    if (p.splits == 1) return 0;
+    Carver cv(nullptr, 0);
+    cv.take((size_t)p.splits * rows * align_up(n, 4) * sizeof(int32_t));
+    return cv.used();
+}
+
+extern "C" int i8_matmul(void* y, size_t y_row_stride, int y_dtype, const int8_t* x, size_t x_row_stride, const float* x_scales, size_t rows,
+                         const int8_t* w, const float* w_scales, size_t n, size_t k, void* ws, size_t ws_bytes, void* stream) {
+    const size_t bytes = y_dtype == ZK_I32 ? 4 : y_dtype == ZK_I16 ? 0 : dtype_bytes(y_dtype);
+    if (!bytes || !sizes_ok(rows, n, k)) return ZK_E_BADARG;
+    if (rows == 0) return ZK_OK;
+    if (!y || !x || !w || !aligned(y, bytes) || !aligned(x, 16) || !aligned(w, 16)) return ZK_E_BADARG;
+    if (rows > 1 && (x_row_stride < k || x_row_stride % 16 || x_row_stride > (size_t)1 << 23 || y_row_stride < n)) return ZK_E_BADARG;
+    if (y_dtype != ZK_I32 && (!x_scales || !w_scales || !aligned(x_scales, 4) || !aligned(w_scales, 4))) return ZK_E_BADARG;
+    const Plan p = plan_of(rows, n, k);
+    Args a = {};
+    a.y = y;
+    a.yrow = y_row_stride;
+    a.x = x;
+    a.xrow = rows > 1 ? x_row_stride : k;
+    a.xs = x_scales;
+    a.w = w;
+    a.ws = w_scales;
+    a.rows = (uint32_t)rows;
+    a.n = (uint32_t)n;
+    a.k = (uint32_t)k;
+    a.splits = p.splits;
+    a.each = p.each;
+    a.n_pad = (uint32_t)align_up(n, 4);
+    a.quads = aligned(y, 4 * bytes) && (rows == 1 || y_row_stride % 4 == 0);
+    if (p.splits > 1) {
+        if (!ws) return ZK_E_BUFSZ;
+        Carver cv(ws, ws_bytes);
+        a.parts = (int32_t*)cv.take((size_t)p.splits * rows * a.n_pad * sizeof(int32_t));
+        if (cv.overflow() || !a.parts) return ZK_E_BUFSZ;
+    }
+    hipStream_t s = as_stream(stream);
+    switch (y_dtype) {
+        case ZK_I32: return launch<ZK_I32>(a, p, s);
+        case ZK_F32: return launch<ZK_F32>(a, p, s);
+        case ZK_F16: return launch<ZK_F16>(a, p, s);
+        default: return launch<ZK_BF16>(a, p, s);
+    }
+}

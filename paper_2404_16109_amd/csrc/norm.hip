@@ -1,0 +1,422 @@
+// What stands between two blocks of a layer, and activations as 8-bit codes.
+//
+//   t = norm(z) * post_gain + post_bias, r = alpha x + gate t, h = norm(r) * gain + bias; h as it is or as codes with a scale.
+//
+// One workgroup has a row and keeps it in registers: every tensor is read once and written once, which is what bounds the
+// call.  Statistics are sums in 64 bits (at the rate of 32 here) and are rounded to 32 bits once; from there on every step is one
+// operation of 32 bits with its own rounding, so nothing is contracted below: the codes are the integers of a proof, and whoever
+// computes the definition gets the same ones, but for a statistic that lies within some 2^-53 of the middle between two numbers.
+#include "serve_dev.h"
+
+#pragma clang fp contract(off)
+
+namespace zkmi {
+namespace {
+
+static const uint32_t kMostDim = 32768;   // of a row in registers: 1024 threads of 32 elements
+static const uint32_t kMostThreads = 1024;
+static const float kLeast = 0x1p-100f;    // rows whose largest magnitude is below it are zeros: 127 / amax has to be a number
+
+struct NormArgs {
+    block_norm_args a;
+    int dtype;
+    uint32_t dim;
+};
+
+// An element of 16 or 32 bits, as it lies in memory.
+template <int DT>
+struct Element {
+    using type = uint16_t;
+    static constexpr int wide = 8;  // elements to 16 bytes
+};
+template <>
+struct Element<ZK_F32> {
+    using type = uint32_t;
+    static constexpr int wide = 4;
+};
+
+// Which elements of a row a thread has.  WIDE: runs of 16 bytes, so that every load is one; else single ones, side by side
+// across the threads, which takes any alignment and length.
+template <int DT, int E, bool WIDE>
+struct Place {
+    static constexpr int W = Element<DT>::wide;
+    uint32_t tid, threads, dim;
+    __device__ __forceinline__ uint32_t at(int i) const {
+        return WIDE ? (tid + (uint32_t)(i / W) * threads) * W + (uint32_t)(i % W) : tid + (uint32_t)i * threads;
+    }
+    __device__ __forceinline__ bool in(int i) const { return at(WIDE ? i / W * W : i) < dim; }
+};
+
+// A thread's elements of a row, as they lie in memory: asked for long before they are used.  Zeros behind the row's end.
+template <int DT, int E, bool WIDE>
+struct Raw {
+    static constexpr int W = Element<DT>::wide;
+    uint32_t word[WIDE ? E / W * 4 : E];
+    __device__ __forceinline__ void load(const void* p, size_t row, const Place<DT, E, WIDE>& at) {
+        const typename Element<DT>::type* x = (const typename Element<DT>::type*)p + row;
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int v = 0; v < E / W; ++v) {
+                v4u q = {0, 0, 0, 0};
+                if (at.in(v * W)) q = *(const v4u*)(x + at.at(v * W));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) word[4 * v + k] = q[k];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) word[i] = at.in(i) ? (uint32_t)x[at.at(i)] : 0u;
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (DT == ZK_F32) return bits_float(word[i]);
+        else if constexpr (WIDE) return half_of<DT>(word[i >> 1], i & 1);
+        else return half_of<DT>(word[i], 0);
+    }
+};
+
+template <int DT>
+__device__ __forceinline__ float rounded(float f) {
+    if constexpr (DT == ZK_F32) return f;
+    return half_of<DT>(half_bits<DT>(f), 0);
+}
+
+// Stores a thread's elements; f is rounded to the type.
+template <int DT, int E, bool WIDE>
+__device__ __forceinline__ void store_row(void* p, size_t row, const Place<DT, E, WIDE>& at, const float (&f)[E]) {
+    constexpr int W = Element<DT>::wide;
+    typename Element<DT>::type* y = (typename Element<DT>::type*)p + row;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int v = 0; v < E / W; ++v) {
+            v4u q;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (DT == ZK_F32) q[k] = float_bits(f[v * W + k]);
+                else q[k] = (uint32_t)half_bits<DT>(f[v * W + 2 * k]) | ((uint32_t)half_bits<DT>(f[v * W + 2 * k + 1]) << 16);
+            }
+            if (at.in(v * W)) *(v4u*)(y + at.at(v * W)) = q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (at.in(i)) store_one<DT>((void*)y, at.at(i), f[i]);
+    }
+}
+
+// Over a workgroup, in every thread.  LDS slots are used in turn, so that one barrier is enough between two sums.
+struct Scratch {
+    double sums[2][kMostThreads / 64];
+    uint32_t most[kMostThreads / 64];
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_from(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = from_lane<CTRL, ROWS>(0u, (uint32_t)b), hi = from_lane<CTRL, ROWS>(0u, (uint32_t)(b >> 32));
+    return x + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ double wave_add64(double x) {  // the same moves as over_wave; in lane 63
+    x = add_from<0x111, 0xf>(x);
+    x = add_from<0x112, 0xf>(x);
+    x = add_from<0x114, 0xf>(x);
+    x = add_from<0x118, 0xf>(x);
+    x = add_from<0x142, 0xa>(x);
+    return add_from<0x143, 0xc>(x);
+}
+__device__ __forceinline__ double all_add(double x, Scratch& s, int turn, uint32_t waves) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    x = wave_add64(x);
+    if (lane == 63) s.sums[turn & 1][wave] = x;
+    __syncthreads();
+    double sum = 0.0;
+    for (uint32_t w = 0; w < waves; ++w) sum += s.sums[turn & 1][w];
+    return sum;
+}
+
+// v = (v - mean) * rstd * gain + bias, statistics over the workgroup's row.  `turn` counts the sums.
+template <int DT, int E, bool WIDE>
+__device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, const Raw<DT, E, WIDE>& gain, bool has_gain,
+                                          const Raw<DT, E, WIDE>& bias, bool has_bias, const Place<DT, E, WIDE>& at, Scratch& s, int& turn,
+                                          uint32_t waves) {
+    if (kind != ZK_NORM_NONE) {
+        const double n = (double)at.dim;
+        double mean = 0.0, sum = 0.0;
+        if (kind == ZK_NORM_LAYER) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) sum += (double)v[i];  // zeros behind the row's end
+            mean = all_add(sum, s, turn++, waves) / n;
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const double d = at.in(i) ? (double)v[i] - mean : 0.0;
+                sum = __builtin_fma(d, d, sum);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) sum = __builtin_fma((double)v[i], (double)v[i], sum);
+        }
+        const float rstd = (float)(1.0 / sqrt(all_add(sum, s, turn++, waves) / n + (double)eps));
+        if (kind == ZK_NORM_LAYER) {
+            const float m = (float)mean;
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = v[i] - m;
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = v[i] * rstd;
+    }
+    if (has_gain) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = v[i] * gain.get(i);
+    }
+    if (has_bias) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = v[i] + bias.get(i);
+    }
+}
+
+// scale = amax / 127, codes rint(h * (127 / amax)); the sum with 1.5 * 2^23 has the rounded integer in its lowest bits.
+__device__ __forceinline__ bool code_scale(uint32_t most, float& scale, float& inv) {
+    const float amax = bits_float(most);
+    const bool fine = most < 0x7f800000u, some = fine && amax >= kLeast;
+    scale = some ? amax / 127.0f : fine ? 0.0f : __builtin_nanf("");
+    inv = some ? 127.0f / amax : 0.0f;
+    return some;
+}
+__device__ __forceinline__ uint32_t code_of(float h, float inv) { return float_bits(h * inv + 12582912.0f) & 0xffu; }
+
+template <int DT, int E, bool WIDE>
+__device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* scale_at, const Place<DT, E, WIDE>& at, const float (&h)[E], Scratch& s,
+                                            uint32_t waves) {
+    constexpr int W = Element<DT>::wide;
+    uint32_t most = 0;  // the bits of |h|: infinities and NaN are above every number
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const uint32_t bits = at.in(i) ? float_bits(h[i]) & 0x7fffffffu : 0u;
+        most = bits > most ? bits : most;
+    }
+    most = wave_max(most);
+    if (waves > 1) {
+        if ((threadIdx.x & 63) == 0) s.most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        for (uint32_t w = 0; w < waves; ++w) most = s.most[w] > most ? s.most[w] : most;
+    }
+    float scale, inv;
+    const bool some = code_scale(most, scale, inv);
+    if (threadIdx.x == 0) *scale_at = scale;
+    int8_t* y = codes + row;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int v = 0; v < E / W; ++v) {
+            uint32_t q[W / 4];
+#pragma unroll
+            for (int k = 0; k < W / 4; ++k) {
+                const float* f = h + v * W + 4 * k;
+                const uint32_t c = code_of(f[0], inv) | (code_of(f[1], inv) << 8) | (code_of(f[2], inv) << 16) | (code_of(f[3], inv) << 24);
+                q[k] = some ? c : 0u;
+            }
+            if (at.in(v * W)) {
+                if constexpr (W == 8) *(uint2*)(y + at.at(v * W)) = make_uint2(q[0], q[1]);
+                else *(uint32_t*)(y + at.at(v * W)) = q[0];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (at.in(i)) y[at.at(i)] = some ? (int8_t)code_of(h[i], inv) : (int8_t)0;
+    }
+}
+
+template <int DT, int E, bool WIDE>
+__global__ __launch_bounds__(kMostThreads) void k_block_norm(NormArgs n) {
+    __shared__ Scratch s;
+    const block_norm_args& a = n.a;
+    const size_t row = blockIdx.x;
+    const uint32_t waves = blockDim.x >> 6;
+    const Place<DT, E, WIDE> at = {threadIdx.x, blockDim.x, n.dim};
+    Raw<DT, E, WIDE> z, x, gate, gain, bias, post_gain, post_bias;
+    if (a.z) z.load(a.z, row * a.z_row_stride, at);
+    x.load(a.x, row * a.x_row_stride, at);
+    if (a.gate) gate.load(a.gate, row * a.gate_row_stride, at);
+    int turn = 0;
+    float v[E];
+    if (a.z) {
+        if (a.post_gain) post_gain.load(a.post_gain, 0, at);
+        if (a.post_bias) post_bias.load(a.post_bias, 0, at);
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = z.get(i);
+        normalise(v, a.post_norm, a.eps, post_gain, a.post_gain != nullptr, post_bias, a.post_bias != nullptr, at, s, turn, waves);
+        if (a.gate) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = gate.get(i) * v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = a.alpha * x.get(i) + v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = a.alpha * x.get(i);
+    }
+    if (a.gain) gain.load(a.gain, 0, at);
+    if (a.bias) bias.load(a.bias, 0, at);
+    if (a.r) store_row<DT, E, WIDE>(a.r, row * a.r_row_stride, at, v);
+    if (!a.h && !a.codes) return;
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = at.in(i) ? rounded<DT>(v[i]) : 0.0f;  // what the next block sees is what is stored
+    normalise(v, a.norm, a.eps, gain, a.gain != nullptr, bias, a.bias != nullptr, at, s, turn, waves);
+    if (a.h) store_row<DT, E, WIDE>(a.h, row * a.h_row_stride, at, v);
+    else store_codes<DT, E, WIDE>(a.codes, row * a.codes_row_stride, a.scales + row, at, v, s, waves);
+}
+
+template <int DT, int E, bool WIDE>
+__global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
+    __shared__ Scratch s;
+    const size_t row = blockIdx.x;
+    const Place<DT, E, WIDE> at = {threadIdx.x, blockDim.x, dim};
+    Raw<DT, E, WIDE> raw;
+    raw.load(x, row * x_row, at);
+    float v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = raw.get(i);
+    store_codes<DT, E, WIDE>(codes, row * codes_row, scales + row, at, v, s, blockDim.x >> 6);
+}
+
+// Rows longer than the registers of a workgroup: read twice, the second time from a cache that holds them.
+template <int DT>
+__global__ __launch_bounds__(kMostThreads) void k_quantise_long(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
+    __shared__ uint32_t largest[kMostThreads / 64];
+    const size_t row = blockIdx.x, from = row * x_row;
+    uint32_t most = 0;
+    for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
+        const uint32_t bits = float_bits(load_one<DT>(x, from + i)) & 0x7fffffffu;
+        most = bits > most ? bits : most;
+    }
+    most = wave_max(most);
+    if ((threadIdx.x & 63) == 0) largest[threadIdx.x >> 6] = most;
+    __syncthreads();
+    for (uint32_t w = 0; w < kMostThreads / 64; ++w) most = largest[w] > most ? largest[w] : most;
+    float scale, inv;
+    const bool some = code_scale(most, scale, inv);
+    if (threadIdx.x == 0) scales[row] = scale;
+    for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads)
+        codes[row * codes_row + i] = some ? (int8_t)code_of(load_one<DT>(x, from + i), inv) : (int8_t)0;
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+bool float_type(int dtype) { return dtype == ZK_F32 || dtype == ZK_F16 || dtype == ZK_BF16; }
+bool norm_kind(int kind) { return kind == ZK_NORM_NONE || kind == ZK_NORM_RMS || kind == ZK_NORM_LAYER; }
+
+// How a row is spread: elements of a thread, and threads.
+struct Spread {
+    int each;
+    uint32_t threads;
+};
+Spread spread_of(int dtype, uint32_t dim, size_t rows) {
+    const int least = dtype == ZK_F32 ? 4 : 8;
+    int each = least;
+    while (each < 32 && div_up(dim, each) > kMostThreads) each *= 2;
+    (void)rows;
+    return {each, (uint32_t)align_up(div_up(dim, each), 64)};
+}
+
+template <int DT, int E, bool WIDE>
+void launch_norm(const NormArgs& n, unsigned rows, uint32_t threads, hipStream_t s) {
+    hipLaunchKernelGGL((k_block_norm<DT, E, WIDE>), dim3(rows), dim3(threads), 0, s, n);
+}
+template <int DT, bool WIDE>
+void spread_norm(const NormArgs& n, unsigned rows, hipStream_t s) {
+    const Spread p = spread_of(DT, n.dim, rows);
+    if constexpr (DT == ZK_F32)
+        if (p.each == 4) return launch_norm<DT, 4, WIDE>(n, rows, p.threads, s);
+    if (p.each == 8) return launch_norm<DT, 8, WIDE>(n, rows, p.threads, s);
+    if (p.each == 16) return launch_norm<DT, 16, WIDE>(n, rows, p.threads, s);
+    launch_norm<DT, 32, WIDE>(n, rows, p.threads, s);
+}
+
+struct QuantiseArgs {
+    int8_t* codes;
+    size_t codes_row;
+    float* scales;
+    const void* x;
+    size_t x_row;
+    uint32_t dim;
+};
+template <int DT, int E, bool WIDE>
+void launch_quantise(const QuantiseArgs& q, unsigned rows, uint32_t threads, hipStream_t s) {
+    hipLaunchKernelGGL((k_quantise<DT, E, WIDE>), dim3(rows), dim3(threads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim);
+}
+template <int DT, bool WIDE>
+void spread_quantise(const QuantiseArgs& q, unsigned rows, hipStream_t s) {
+    const Spread p = spread_of(DT, q.dim, rows);
+    if constexpr (DT == ZK_F32)
+        if (p.each == 4) return launch_quantise<DT, 4, WIDE>(q, rows, p.threads, s);
+    if (p.each == 8) return launch_quantise<DT, 8, WIDE>(q, rows, p.threads, s);
+    if (p.each == 16) return launch_quantise<DT, 16, WIDE>(q, rows, p.threads, s);
+    launch_quantise<DT, 32, WIDE>(q, rows, p.threads, s);
+}
+template <int DT>
+void quantise_of(const QuantiseArgs& q, bool wide, unsigned rows, hipStream_t s) {
+    if (q.dim > kMostDim) hipLaunchKernelGGL((k_quantise_long<DT>), dim3(rows), dim3(kMostThreads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim);
+    else if (wide) spread_quantise<DT, true>(q, rows, s);
+    else spread_quantise<DT, false>(q, rows, s);
+}
+
+// A matrix of the call: rows far enough apart, aligned to its elements.  With one row the stride says nothing.
+bool rows_ok(const void* p, size_t stride, size_t bytes, size_t rows, size_t dim) {
+    return aligned(p, bytes) && (rows <= 1 || stride >= dim) && stride <= (size_t)1 << 40;
+}
+
+}  // namespace
+}  // namespace zkmi
+
+using namespace zkmi;
+
+extern "C" int block_norm(const block_norm_args* args, int dtype, size_t rows, size_t dim, void* stream) {
+    if (!args || !float_type(dtype) || dim == 0 || dim > kMostDim || rows >= 0x80000000u) return ZK_E_BADARG;
+    block_norm_args a = *args;
+    const size_t bytes = dtype_bytes(dtype);
+    if (!norm_kind(a.norm) || !norm_kind(a.post_norm) || !(a.alpha - a.alpha == 0.0f)) return ZK_E_BADARG;
+    if ((a.norm != ZK_NORM_NONE || a.post_norm != ZK_NORM_NONE) && !(a.eps > 0.0f && a.eps - a.eps == 0.0f)) return ZK_E_BADARG;
+    if (rows == 0) return ZK_OK;
+    if (!a.z && (a.gate || a.post_gain || a.post_bias || a.post_norm != ZK_NORM_NONE)) return ZK_E_BADARG;
+    if ((a.h && a.codes) || (!a.codes != !a.scales)) return ZK_E_BADARG;
+    if (!a.x || (!a.r && !a.h && !a.codes)) return ZK_E_BADARG;
+    if (!rows_ok(a.x, a.x_row_stride, bytes, rows, dim) || (a.z && !rows_ok(a.z, a.z_row_stride, bytes, rows, dim)) ||
+        (a.gate && a.gate_row_stride && !rows_ok(a.gate, a.gate_row_stride, bytes, rows, dim)) || (a.r && !rows_ok(a.r, a.r_row_stride, bytes, rows, dim)) ||
+        (a.h && !rows_ok(a.h, a.h_row_stride, bytes, rows, dim)) || (a.codes && !rows_ok(a.codes, a.codes_row_stride, 1, rows, dim)))
+        return ZK_E_BADARG;
+    for (const void* p : {a.gate, a.gain, a.bias, a.post_gain, a.post_bias, (const void*)a.scales})
+        if (p && !aligned(p, p == a.scales ? 4 : bytes)) return ZK_E_BADARG;
+    const size_t run = 16 / bytes;
+    bool wide = dim % run == 0;
+    const struct {
+        const void* p;
+        size_t stride;
+    } tensors[] = {{a.x, a.x_row_stride}, {a.z, a.z_row_stride}, {a.gate, a.gate_row_stride}, {a.r, a.r_row_stride}, {a.h, a.h_row_stride},
+                   {a.gain, 0}, {a.bias, 0}, {a.post_gain, 0}, {a.post_bias, 0}};
+    for (const auto& t : tensors) wide = wide && (!t.p || (aligned(t.p, 16) && (rows == 1 || t.stride % run == 0)));
+    wide = wide && (!a.codes || (aligned(a.codes, run) && (rows == 1 || a.codes_row_stride % run == 0)));
+    const NormArgs n = {a, dtype, (uint32_t)dim};
+    hipStream_t s = as_stream(stream);
+    const unsigned r = (unsigned)rows;
+    if (dtype == ZK_F32) wide ? spread_norm<ZK_F32, true>(n, r, s) : spread_norm<ZK_F32, false>(n, r, s);
+    else if (dtype == ZK_F16) wide ? spread_norm<ZK_F16, true>(n, r, s) : spread_norm<ZK_F16, false>(n, r, s);
+    else wide ? spread_norm<ZK_BF16, true>(n, r, s) : spread_norm<ZK_BF16, false>(n, r, s);
+    ZK_HIP_TRY(hipGetLastError());
+    return ZK_OK;
+}
+
+extern "C" int i8_quantise(int8_t* codes, size_t codes_row_stride, float* scales, const void* x, size_t x_row_stride, int dtype, size_t rows,
+                           size_t k, void* stream) {
+    if (!float_type(dtype) || k == 0 || k > I8_MAX_K || rows >= 0x80000000u) return ZK_E_BADARG;
+    if (rows == 0) return ZK_OK;
+    const size_t bytes = dtype_bytes(dtype), run = 16 / bytes;
+    if (!codes || !scales || !x || !aligned(scales, 4) || !rows_ok(x, x_row_stride, bytes, rows, k) || !rows_ok(codes, codes_row_stride, 1, rows, k))
+        return ZK_E_BADARG;
+    const bool wide = k % run == 0 && aligned(x, 16) && aligned(codes, run) && (rows == 1 || (x_row_stride % run == 0 && codes_row_stride % run == 0));
+    const QuantiseArgs q = {codes, codes_row_stride, scales, x, x_row_stride, (uint32_t)k};
+    hipStream_t s = as_stream(stream);
+    if (dtype == ZK_F32) quantise_of<ZK_F32>(q, wide, (unsigned)rows, s);
+    else if (dtype == ZK_F16) quantise_of<ZK_F16>(q, wide, (unsigned)rows, s);
+    else quantise_of<ZK_BF16>(q, wide, (unsigned)rows, s);
+    ZK_HIP_TRY(hipGetLastError());
+    return ZK_OK;
+}
