@@ -606,6 +606,19 @@ int kvcache_attention(const kvcache_i8* cache, const void* q, size_t q_row_strid
                       uint32_t q_heads, const kv_seqs* seqs, float scale, uint32_t window, void* out, size_t out_row_stride,
                       size_t out_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* The same for a batch whose sequences all begin with the same tokens: keys at positions below prefix_pages * page_tokens
+ * lie in the pages prefix[0 .. prefix_pages) (device) for every sequence, those behind in the sequence's own, by position, as
+ * ever (lens[b] counts both; the table's entries for the prefix are not used; rows may lie inside the prefix).  Without a window.  The result is that of
+ * kvcache_attention with those pages in every row of the table, but for roundings: the prefix is read once for all
+ * rows, not once for each sequence.  A page of the prefix outside the cache makes NaN of the rows that see a key in it
+ * (ZK_FAULT_PAGE).  prefix_pages may be 0.  rows * (q_heads / kv_heads) < 2^31 - 256.  ws: device (always needed),
+ * kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_pages * page_tokens, max_len). */
+size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
+                                                uint32_t head_dim, uint32_t prefix_tokens, uint32_t max_len);
+int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
+                             uint32_t q_heads, const kv_seqs* seqs, const int32_t* prefix, uint32_t prefix_pages, float scale, void* out,
+                             size_t out_row_stride, size_t out_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* The codes of one sequence's first `tokens` tokens in order, as the 32-bit integers that
  * tlookup_prove_small takes: k_codes, v_codes (device): tokens x kv_heads x head_dim each.
  * pages: device, the sequence's row of the table.  Exponents lie in the cache by page.

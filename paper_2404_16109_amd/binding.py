@@ -174,6 +174,9 @@ def _load():
         "kvcache_attention_workspace_bytes": (sz, [ctypes.c_uint32] * 7),
         "kvcache_attention": (i32, [P(kvcache_i8), vp, sz, sz, i32, ctypes.c_uint32, P(kv_seqs), ctypes.c_float,
                                     ctypes.c_uint32, vp, sz, sz, vp, vp, sz, vp]),
+        "kvcache_attention_prefix_workspace_bytes": (sz, [ctypes.c_uint32] * 8),
+        "kvcache_attention_prefix": (i32, [P(kvcache_i8), vp, sz, sz, i32, ctypes.c_uint32, P(kv_seqs), vp, ctypes.c_uint32, ctypes.c_float,
+                                           vp, sz, sz, vp, vp, sz, vp]),
         "kvcache_read": (i32, [P(kvcache_i8), vp, sz, vp, vp, vp, vp]),
         "w4_matvec_workspace_bytes": (sz, [i32, sz, sz]),
         "w4_matvec": (i32, [vp, sz, vp, sz, i32, sz, vp, vp, sz, sz, ctypes.c_uint32, ctypes.c_float, vp, sz, vp]),
@@ -208,7 +211,8 @@ EXPORTS = ["zkmi_version", "zkmi_thread_init", "zkmi_thread_release", "zkmi_self
            "zkattn_link_workspace_bytes", "zkattn_link_prove", "zkattn_link_prove_small",
            "zkattn_link_verify_workspace_bytes",
            "zkattn_link_verify", "kvcache_append", "kvcache_attention_workspace_bytes", "kvcache_attention", "kvcache_read",
-           "w4_matvec_workspace_bytes", "w4_matvec", "w4_expand_i16", "logprobs_workspace_bytes", "logprobs", "i8_quantise", "i8_matmul_workspace_bytes", "i8_matmul", "block_norm"]
+           "w4_matvec_workspace_bytes", "w4_matvec", "w4_expand_i16", "logprobs_workspace_bytes", "logprobs", "kvcache_attention_prefix_workspace_bytes", "kvcache_attention_prefix",
+           "i8_quantise", "i8_matmul_workspace_bytes", "i8_matmul", "block_norm"]
 
 
 def raw():
@@ -919,6 +923,32 @@ def kvcache_attention(cache, q, cu, lens, table, max_new, max_len, scale, window
     rc = _lib.kvcache_attention(ctypes.byref(cache.c), q.data_ptr(), q.stride(0), q.stride(1), _DTYPES[q.dtype], heads,
                                 ctypes.byref(s), scale, window, out.data_ptr(), out.stride(0), out.stride(1),
                                 lse.data_ptr(), *_workspace(ws), _stream())
+    return rc, out, lse
+
+
+def kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_tokens, max_len):
+    return _lib.kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_tokens, max_len)
+
+
+def kvcache_attention_prefix(cache, q, cu, lens, table, prefix, max_new, max_len, scale, out=None, lse=None, ws=None, fault=None):
+    """As kvcache_attention, for a batch that begins with the same tokens: prefix: int32, the pages that hold them.  Returns
+    (rc, out, lse)."""
+    rows, heads, dim = q.shape
+    assert dim == cache.c.head_dim and q.is_cuda and q.stride(2) == 1
+    assert prefix.dtype == torch.int32 and prefix.dim() == 1 and prefix.is_cuda and prefix.is_contiguous(), "prefix: int32 on the GPU"
+    if out is None:
+        out = torch.empty(rows, heads, dim, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.stride(2) == 1
+    assert lse.shape == (rows, heads) and lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous()
+    s = _kv_seqs(cu, lens, table, rows, max_new, max_len, fault)
+    if ws is None:
+        ws = _ws(_lib.kvcache_attention_prefix_workspace_bytes(s.seqs, rows, max_new, heads, cache.c.kv_heads, dim,
+                                                               prefix.numel() * cache.c.page_tokens, max_len))
+    rc = _lib.kvcache_attention_prefix(ctypes.byref(cache.c), q.data_ptr(), q.stride(0), q.stride(1), _DTYPES[q.dtype], heads,
+                                       ctypes.byref(s), prefix.data_ptr(), prefix.numel(), scale, out.data_ptr(), out.stride(0),
+                                       out.stride(1), lse.data_ptr(), *_workspace(ws), _stream())
     return rc, out, lse
 
 

@@ -1,0 +1,268 @@
+// kvcache_attention_prefix: attention for a batch whose sequences all begin with the same tokens.
+//
+// The keys of a row are those of the prefix and its sequence's own.  With (M, l, o) the maximum, the sum of weights and
+// the weighted values over a part of the keys, parts join by e^(M - max M): so the prefix is one part, or several, for ALL rows
+// of the batch at once, and its codes are read once for 128 rows where they would be read once for each sequence.
+// k_front: rows of the whole batch, 128 to a workgroup, over tiles of the prefix (the products that bound it are those of
+// k_attend_many); k_attend_few / k_attend_many: each sequence's own keys; k_front_join: adds up.
+#include "attend_dev.h"
+
+namespace zkmi {
+namespace {
+
+static const uint32_t kMostParts = 32;  // of the prefix, and of a sequence's own keys
+
+struct PrefixArgs : Args {
+    static constexpr bool joined = true;
+    const int32_t* front;      // the prefix's pages
+    uint32_t front_tokens;     // a multiple of the page
+    uint32_t front_tiles;      // whole tiles of it; what is left is read with each sequence's own
+    uint32_t front_splits, front_each;
+    float* front_parts;        // [head][split][row of the batch]
+    float2* front_ml;
+};
+
+// As for a sequence alone, but that its first tokens lie in the prefix's pages, and its first tiles are not its own.
+__device__ __forceinline__ uint32_t page_of(const PrefixArgs& a, uint32_t b, uint32_t token) {
+    const uint32_t at = token >> a.page_log, last = a.s.table_pages - 1;
+    const int32_t* p = token < a.front_tokens ? a.front + at : a.s.table + (size_t)b * a.s.table_stride + (at < last ? at : last);
+    return (uint32_t)*p;
+}
+__device__ __forceinline__ uint32_t first_seen(const PrefixArgs& a, const SeqView&, int32_t) { return a.front_tiles * kTile; }
+__device__ __forceinline__ uint32_t first_guess(const PrefixArgs& a) { return a.front_tiles; }
+__device__ __forceinline__ Tiles tiles_of(const PrefixArgs& a, const SeqView& v, int32_t, int32_t i1) {
+    const int64_t last = (int64_t)v.len - v.rows + i1;
+    const uint32_t end = last < 0 ? 0 : (uint32_t)(last / kTile) + 1;
+    return Tiles{a.front_tiles, end > a.front_tiles ? end : a.front_tiles};
+}
+
+// The prefix's whole tiles for 128 rows of the batch.
+template <int DT>
+__global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_front(PrefixArgs a) {
+    extern __shared__ char lds[];
+    __shared__ ManyShared sh;
+    __shared__ int32_t place[kRows], least, most;  // positions of the tokens that the rows belong to, -1: nobody's
+    const uint32_t H = a.cache.kv_heads, h = blockIdx.x % H, r0 = blockIdx.x / H * kRows, split = blockIdx.y, tid = threadIdx.x;
+    const uint32_t R = a.s.rows * a.group, r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
+    const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
+    if (tid < kRows) place[tid] = -1;
+    if (tid == 0) {
+        least = 0x7fffffff;
+        most = -1;
+    }
+    __syncthreads();
+    for (uint32_t b = tid; b < a.s.seqs; b += kBlock) {
+        const SeqView v = seq_view(a.s, b, a.page_log);
+        if (!v.ok || v.rows == 0) continue;
+        const int32_t from = v.row0 > tok0 ? v.row0 : tok0, to = v.row0 + v.rows - 1 < tok1 ? v.row0 + v.rows - 1 : tok1;
+        for (int32_t t = from; t <= to; ++t) place[t - tok0] = v.len - v.rows + (t - v.row0);
+    }
+    __syncthreads();
+    if ((int32_t)tid <= tok1 - tok0) {
+        atomicMin(&least, place[tid]);
+        atomicMax(&most, place[tid]);
+    }
+    __syncthreads();
+    if (most < 0) return;  // no row of theirs sees a key, and k_front_join does not ask
+    Tiles tiles = {split * a.front_each, (split + 1) * a.front_each};
+    if (tiles.end > a.front_tiles) tiles.end = a.front_tiles;
+    const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
+    const int32_t pos = r < R ? place[r / a.group - (uint32_t)tok0] : -1;
+    const SeqView all = {0, (int32_t)a.s.rows, 0, true};
+    attend_rows<DT>(a, lds, sh, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+}
+
+// A wavefront: one row of one sequence and head.  Lanes hold four dimensions each; the lanes left of 64 take parts in turn.
+__global__ __launch_bounds__(kBlock) void k_front_join(PrefixArgs a) {
+    const uint32_t H = a.cache.kv_heads, d = a.cache.head_dim, b = blockIdx.y, lane = threadIdx.x & 63;
+    const uint32_t item = uniform(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)), h = item / a.rows_most, r = item - h * a.rows_most;
+    const SeqView v = seq_view(a.s, b, a.page_log);
+    if (!v.ok) {  // the workgroup's first wavefront is at row 0 of a head where one begins there
+        if (blockIdx.x == 0)
+            for (uint32_t head = 0; head < H; ++head) not_a_number(a, b, head);
+        return;
+    }
+    if (h >= H || r >= (uint32_t)v.rows * a.group) return;
+    const int32_t pos = v.len - v.rows + (int32_t)(r / a.group);
+    const uint32_t R = a.s.rows * a.group, row = (uint32_t)v.row0 * a.group + r;
+    // parts of the prefix come first; a row that sees no key has none
+    const uint32_t front = pos >= 0 ? a.front_splits : 0;
+    const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / kRows * kRows);
+    const uint32_t each = part_of(a, tiles), n = tiles.end - tiles.first, own = pos >= 0 && n ? (n + each - 1) / each : 0;
+    const size_t front0 = (size_t)h * a.front_splits * R + row, own0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
+    float m = -kInf, l = 0.0f;
+    if (lane < front + own) {
+        const float2 ml = lane < front ? a.front_ml[front0 + (size_t)lane * R] : a.parts_ml[own0 + (size_t)(lane - front) * a.rows_most];
+        m = ml.x;
+        l = ml.y;
+    }
+    const float top = wave_max(m), ref = top == -kInf ? 0.0f : top, weight = exp2_of(m - ref);
+    l = wave_add(l * weight);
+    const uint32_t quads = d >> 2, ways = 64 / quads, way = lane / quads, c = lane - way * quads;
+    v4f sum = {0, 0, 0, 0};
+    for (uint32_t p0 = 0; p0 < front + own; p0 += ways) {
+        const uint32_t p = p0 + way;
+        const float w = bits_float((uint32_t)__shfl((int)float_bits(weight), (int)(p & 63)));
+        if (way < ways && p < front + own) {
+            const size_t at = p < front ? front0 + (size_t)p * R : own0 + (size_t)(p - front) * a.rows_most;
+            sum += ((const v4f*)(p < front ? a.front_parts : a.parts))[at * quads + c] * w;
+        }
+    }
+    for (uint32_t w = 1; w < ways; ++w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float other = bits_float((uint32_t)__shfl((int)float_bits(sum[e]), (int)((lane + w * quads) & 63)));
+            if (way == 0) sum[e] += other;
+        }
+    }
+    if (way == 0) {
+        const size_t at = row_at(a, v, h, r, a.orow, a.ohead) + 4 * c;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) put_at(a.out, at + e, l == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
+    }
+    if (a.lse && lane == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l);
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+bool few_rows(uint64_t rows) { return rows <= 32; }
+
+// How a call is spread.  rows: of the batch and a head; most: of a sequence and a head.
+struct Plan {
+    uint32_t front_tiles, front_splits, front_each, splits, each;
+};
+Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uint32_t prefix, uint32_t max_len) {
+    Plan p = {};
+    p.front_tiles = prefix / kTile;
+    const auto share = [](uint64_t groups, uint32_t tiles, uint32_t& splits, uint32_t& each) {
+        uint64_t n = groups >= kWorkgroups / 2 ? 1 : div_up(kWorkgroups, groups);
+        if (n > div_up(tiles, 4)) n = div_up(tiles, 4);
+        if (n > kMostParts) n = kMostParts;
+        each = (uint32_t)div_up(tiles, n);
+        splits = (uint32_t)div_up(tiles, each);
+    };
+    if (p.front_tiles) share(kv_heads * div_up(rows, kRows), p.front_tiles, p.front_splits, p.front_each);
+    const uint32_t own = max_len > p.front_tiles * kTile ? (uint32_t)div_up(max_len - p.front_tiles * kTile, kTile) : 1;
+    share((uint64_t)seqs * kv_heads * (few_rows(most) ? 1 : div_up(most, kRows)), own, p.splits, p.each);
+    if ((uint64_t)p.splits * seqs > 65535) {
+        p.splits = 65535 / seqs;
+        p.each = (uint32_t)div_up(own, p.splits);
+    }
+    return p;
+}
+
+// What lies in the workspace; with a null base the bytes alone.
+size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint64_t most, uint32_t seqs, uint32_t kv_heads, uint32_t head_dim, PrefixArgs* a) {
+    const size_t own = (size_t)seqs * kv_heads * p.splits * most, front = (size_t)kv_heads * p.front_splits * rows;
+    void* at[4] = {cv.take(own * head_dim * sizeof(float)), cv.take(own * sizeof(float2)), cv.take(front * head_dim * sizeof(float)),
+                   cv.take(front * sizeof(float2))};
+    if (a) {
+        a->parts = (float*)at[0];
+        a->parts_ml = (float2*)at[1];
+        a->front_parts = (float*)at[2];
+        a->front_ml = (float2*)at[3];
+    }
+    return cv.used();
+}
+
+template <int DT>
+int launch_front(const PrefixArgs& a, uint64_t rows, hipStream_t s) {
+    const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_front<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_front<DT>), dim3((unsigned)(a.cache.kv_heads * div_up(rows, kRows)), a.front_splits), dim3(kBlock), lds, s, a);
+    return ZK_OK;
+}
+template <int DT>
+int launch_many(const PrefixArgs& a, hipStream_t s) {
+    const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT, PrefixArgs>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_attend_many<DT, PrefixArgs>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs * a.splits), dim3(kBlock), lds, s, a);
+    return ZK_OK;
+}
+template <int NJ, int RT>
+int launch_few(const PrefixArgs& a, hipStream_t s) {
+    const size_t lds = FewLds<NJ, RT, 4>::bytes(a.rows_most);
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, 4, PrefixArgs>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_attend_few<NJ, RT, 4, PrefixArgs>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, s, a);
+    return ZK_OK;
+}
+template <int NJ>
+int launch(const PrefixArgs& a, uint64_t rows, hipStream_t s) {
+    const bool full = a.cache.head_dim > 64 * NJ - 32;
+    if (a.front_tiles) ZK_TRY(full ? launch_front<2 * NJ>(a, rows, s) : launch_front<2 * NJ - 1>(a, rows, s));
+    if (a.rows_most <= 16) ZK_TRY((launch_few<NJ, 1>(a, s)));
+    else if (a.few) ZK_TRY((launch_few<NJ, 2>(a, s)));
+    else ZK_TRY(full ? launch_many<2 * NJ>(a, s) : launch_many<2 * NJ - 1>(a, s));
+    hipLaunchKernelGGL(k_front_join, dim3((unsigned)div_up((size_t)a.rows_most * a.cache.kv_heads, kBlock / 64), a.s.seqs), dim3(kBlock), 0, s, a);
+    ZK_HIP_TRY(hipGetLastError());
+    return ZK_OK;
+}
+
+// Rows of a sequence and head at most.
+uint64_t rows_most(uint32_t rows, uint32_t max_new, uint32_t group) { return (uint64_t)(max_new < rows ? max_new : rows) * group; }
+
+}  // namespace
+}  // namespace zkmi
+
+using namespace zkmi;
+
+extern "C" size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
+                                                           uint32_t head_dim, uint32_t prefix_tokens, uint32_t max_len) {
+    if (!kv_heads || q_heads == 0 || q_heads % kv_heads || !seqs || seqs > 65535 || !rows || !max_new) return 0;
+    const uint32_t group = q_heads / kv_heads;
+    const uint64_t all = (uint64_t)rows * group, most = rows_most(rows, max_new, group);
+    Carver cv(nullptr, 0);
+    return carve(cv, plan_of(seqs, all, most, kv_heads, prefix_tokens, max_len), all, most, seqs, kv_heads, head_dim, nullptr);
+}
+
+extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
+                                        uint32_t q_heads, const kv_seqs* seqs, const int32_t* prefix, uint32_t prefix_pages, float scale, void* out,
+                                        size_t out_row_stride, size_t out_head_stride, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    if ((dtype != ZK_F16 && dtype != ZK_BF16) || !cache_ok(cache) || !seqs_ok(seqs)) return ZK_E_BADARG;
+    if (q_heads == 0 || q_heads % cache->kv_heads || q_heads > 65536 || !(scale - scale == 0.0f)) return ZK_E_BADARG;
+    if ((uint64_t)prefix_pages * cache->page_tokens >= 0x80000000u || (prefix_pages && (!prefix || !aligned(prefix, 4)))) return ZK_E_BADARG;
+    if (seqs->rows == 0 || seqs->seqs == 0) return ZK_OK;
+    if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
+    const uint32_t group = q_heads / cache->kv_heads;
+    const uint64_t rows = (uint64_t)seqs->rows * group, most = rows_most(seqs->rows, seqs->max_new, group);
+    if (rows >= 0x7fffff00u || div_up(most, kRows) > 65535 || div_up(rows, kRows) * cache->kv_heads >= 0x80000000u ||
+        div_up(most * cache->kv_heads, kBlock / 64) >= 0x80000000u)
+        return ZK_E_BADARG;
+    PrefixArgs a = {};
+    a.cache = *cache;
+    a.s = *seqs;
+    a.q = q;
+    a.qrow = q_row_stride;
+    a.qhead = q_head_stride;
+    a.out = out;
+    a.orow = out_row_stride;
+    a.ohead = out_head_stride;
+    a.lse = lse;
+    a.scale = scale;
+    a.group = group;
+    a.page_log = (uint32_t)log2_floor(cache->page_tokens);
+    a.dtype = dtype;
+    a.few = few_rows(most);
+    a.wide = aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0;
+    a.rows_most = (uint32_t)most;
+    a.front = prefix;
+    a.front_tokens = prefix_pages * cache->page_tokens;
+    const Plan p = plan_of(seqs->seqs, rows, most, cache->kv_heads, a.front_tokens, seqs->max_len);
+    a.front_tiles = p.front_tiles;
+    a.front_splits = p.front_splits;
+    a.front_each = p.front_each;
+    a.splits = p.splits;
+    a.each = p.each;
+    if (!ws) return ZK_E_BUFSZ;
+    Carver cv(ws, ws_bytes);
+    carve(cv, p, rows, most, seqs->seqs, cache->kv_heads, cache->head_dim, &a);
+    if (cv.overflow()) return ZK_E_BUFSZ;
+    hipStream_t s = as_stream(stream);
+    switch ((cache->head_dim + 63) / 64) {
+        case 1: return launch<1>(a, rows, s);
+        case 2: return launch<2>(a, rows, s);
+        case 3: return launch<3>(a, rows, s);
+        default: return launch<4>(a, rows, s);
+    }
+}

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests.test_serve_binding import OnGpu, stand_in  # noqa: F401
+from tests.test_serve_refusals import BAD_CACHES, BAD_SEQS, cache, seqs
 
 P = 1 << 20   # an address that is never read: every call below is refused, or has nothing to do
 
@@ -101,3 +102,48 @@ def test_python_takes_the_gpus_tensors_only(stand_in):  # noqa: F811
         with pytest.raises(AssertionError):
             zk.i8_matmul(**dict(dict(x=codes, w=w, x_scales=scales, w_scales=ws, out=y, ws=space), **kw))
     assert set(lib.calls) == {"block_norm", "i8_quantise", "i8_matmul"}
+
+
+def prefix(zk, c=None, s=None, q=P, out=P, dtype=2, heads=8, scale=0.1, front=P, pages=2, lse=None, ws=None, ws_bytes=0):
+    c, s = c or cache(zk), s or seqs(zk)
+    return zk.raw().kvcache_attention_prefix(ctypes.byref(c), q, 1024, 128, dtype, heads, ctypes.byref(s), front, pages, scale, out, 1024, 128, lse, ws,
+                                             ws_bytes, None)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_prefix_caches(zk, bad):
+    assert prefix(zk, c=cache(zk, **bad)) == zk.ZK_E_BADARG
+
+
+@pytest.mark.parametrize("bad", BAD_SEQS)
+def test_prefix_sequences(zk, bad):
+    assert prefix(zk, s=seqs(zk, **bad)) == zk.ZK_E_BADARG
+
+
+def test_prefix_arguments(zk):
+    for kw in (dict(q=None), dict(out=None), dict(dtype=0), dict(dtype=3), dict(dtype=4), dict(heads=0), dict(heads=7), dict(heads=131072),
+               dict(scale=float("inf")), dict(scale=float("nan")), dict(q=P + 1), dict(out=P + 1), dict(lse=P + 2), dict(front=None), dict(front=P + 2),
+               dict(pages=1 << 25), dict(s=seqs(zk, rows=(1 << 31) - 1, max_new=1))):
+        assert prefix(zk, **kw) == zk.ZK_E_BADARG, kw
+    assert prefix(zk, s=seqs(zk, rows=0), q=None) == zk.ZK_OK and prefix(zk, s=seqs(zk, seqs=0), q=None) == zk.ZK_OK
+    need = zk.kvcache_attention_prefix_workspace_bytes(2, 5, 3, 8, 2, 128, 128, 100)
+    assert need > 0 and prefix(zk) == zk.ZK_E_BUFSZ and prefix(zk, ws=P, ws_bytes=need // 2) == zk.ZK_E_BUFSZ
+    assert prefix(zk, front=None, pages=0) == zk.ZK_E_BUFSZ   # no prefix: right arguments
+    for a in ((0, 5, 3, 8, 2, 128, 128, 100), (2, 0, 3, 8, 2, 128, 128, 100), (2, 5, 0, 8, 2, 128, 128, 100), (2, 5, 3, 7, 2, 128, 128, 100),
+              (2, 5, 3, 8, 0, 128, 128, 100), (65536, 5, 3, 8, 2, 128, 128, 100)):
+        assert zk.kvcache_attention_prefix_workspace_bytes(*a) == 0
+
+
+def test_prefix_from_python(stand_in):  # noqa: F811
+    zk, lib = stand_in
+    i8, bf16 = torch.int8, torch.bfloat16
+    c = zk.KvCache(OnGpu(4, 2, 16, 32, dtype=i8), OnGpu(4, 2, 32, 16, dtype=i8), OnGpu(4, 2, dtype=i8), OnGpu(4, 2, dtype=i8))
+    kw = dict(cache=c, q=OnGpu(3, 2, 32, dtype=bf16), cu=OnGpu(2), lens=OnGpu(1), table=OnGpu(1, 4), prefix=OnGpu(2), max_new=3, max_len=60, scale=0.1,
+              out=OnGpu(3, 2, 32, dtype=bf16), lse=OnGpu(3, 2, dtype=torch.float32), ws=OnGpu(4096, dtype=torch.uint8))
+    assert zk.kvcache_attention_prefix(**kw)[0] == 0
+    for bad in (dict(prefix=torch.zeros(2, dtype=torch.int32)), dict(prefix=OnGpu(2, dtype=torch.int64)), dict(prefix=OnGpu(1, 2)),
+                dict(q=torch.zeros(3, 2, 32, dtype=bf16)), dict(out=torch.zeros(3, 2, 32, dtype=bf16)), dict(lse=torch.zeros(3, 2)),
+                dict(ws=torch.zeros(4096, dtype=torch.uint8)), dict(fault=torch.zeros(1, dtype=torch.int32)), dict(table=torch.zeros(1, 4, dtype=torch.int32))):
+        with pytest.raises(AssertionError):
+            zk.kvcache_attention_prefix(**dict(kw, **bad))
+    assert lib.calls == ["kvcache_attention_prefix"]
