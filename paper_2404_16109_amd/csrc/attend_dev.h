@@ -461,10 +461,10 @@ __device__ __forceinline__ void attend_part(const A& a, float* sh, const SeqView
     }
 }
 
+// A workgroup's part of a sequence and head.
 template <int NJ, int RT, int W, typename A>
-__global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(A a) {
-    extern __shared__ float sh[];
-    const uint32_t split = blockIdx.x, h = blockIdx.y, b = blockIdx.z, wave = uniform(threadIdx.x >> 6);
+__device__ __forceinline__ void attend_few(const A& a, float* sh, uint32_t split, uint32_t h, uint32_t b) {
+    const uint32_t wave = uniform(threadIdx.x >> 6);
     // The part begins where the caller's lengths put it, but for windows: its pages are asked for beside the lengths.
     const uint32_t guess = first_guess(a) + split * a.each + wave;
     Asked pages = ask_pages(a, b, guess, W);
@@ -481,6 +481,11 @@ __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_atte
     if (t_first + wave != guess) pages = ask_pages(a, b, t_first + wave, W);
     attend_part<NJ, RT, W>(a, sh, v, b, h, t_first, t_end, pages, a.splits == 1 && !A::joined,
                            (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most);
+}
+template <int NJ, int RT, int W>
+__global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
+    extern __shared__ __attribute__((aligned(16))) float sh[];
+    attend_few<NJ, RT, W>(a, sh, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------------------------
@@ -537,7 +542,10 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         v_at[i] = (p.dim < d ? p.dim : 0) << a.page_log;
     }
     v4u kr[PIECES], vr[PIECES];
-    float my_exp = 0.0f;  // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens
+    // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens.  As they are loaded: a float made of one at once waits for
+    // all of the tile, which cost 2 us a tile where the codes come from HBM.
+    int my_exp = 0;
+    bool my_none = false;
     auto fetch = [&](uint32_t t, const uint32_t(&page)[4]) {
         const uint32_t head = T * d;
 #pragma unroll
@@ -553,7 +561,8 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
             const uint32_t key = t * kTile + 16 * (tid & 3);
             if (none && (int32_t)key <= pos_last && key + 16 > seen_from) report(a.s, ZK_FAULT_PAGE);
             const size_t at = (size_t)page_or_0(a, it) * H + h;
-            my_exp = none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at]);
+            my_exp = tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at];
+            my_none = none;
         }
     };
     auto stage = [&](uint32_t buf) {
@@ -573,7 +582,7 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
             v16[0] = widen(vr[i][0], vr[i][1]);
             v16[1] = widen(vr[i][2], vr[i][3]);
         }
-        if (tid < 8) exps[buf][tid >> 2][tid & 3] = my_exp;
+        if (tid < 8) exps[buf][tid >> 2][tid & 3] = my_none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(my_exp);
     };
 
     v16f o[DT];
@@ -684,19 +693,17 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
     if (a.lse && half == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(m == -kInf ? 0.0f : m, l);
 }
 
+// A workgroup's rows of a sequence and head, `tile` 128s before its last.
 template <int DT, typename A>
-__global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(A a) {
-    extern __shared__ char lds[];
-    __shared__ ManyShared sh;
-    const uint32_t h = blockIdx.x, b = blockIdx.z / a.splits, split = blockIdx.z - b * a.splits;
+__device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& sh, uint32_t tile, uint32_t split, uint32_t h, uint32_t b) {
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (blockIdx.y == 0 && a.splits == 1 && !A::joined) not_a_number(a, b, h);
+        if (tile == 0 && a.splits == 1 && !A::joined) not_a_number(a, b, h);
         return;
     }
     const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + kRows - 1) / kRows;
-    if (blockIdx.y >= row_tiles) return;
-    const uint32_t r0 = (row_tiles - 1 - blockIdx.y) * kRows;  // the rows that see most first, of all heads
+    if (tile >= row_tiles) return;
+    const uint32_t r0 = (row_tiles - 1 - tile) * kRows;  // the rows that see most first, of all heads
     const uint32_t r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
     Tiles tiles = tiles_of_rows(a, v, r0);
@@ -710,6 +717,13 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(A a) {
     const int32_t pos = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
     attend_rows<DT>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
                     (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most, a.parts, a.parts_ml);
+}
+template <int DT>
+__global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ ManyShared sh;
+    const uint32_t b = blockIdx.z / a.splits;
+    attend_many<DT>(a, lds, sh, blockIdx.y, blockIdx.z - b * a.splits, blockIdx.x, b);
 }
 
 }  // namespace

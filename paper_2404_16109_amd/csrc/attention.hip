@@ -56,7 +56,7 @@ __device__ __forceinline__ Share share_out(const Args& a, Row& row) {
 
 template <int NJ, int RT>
 __global__ __launch_bounds__(kBlock, NJ * RT <= 2 ? 2 : 1) void k_attend_shared(Args a) {
-    extern __shared__ float sh[];
+    extern __shared__ __attribute__((aligned(16))) float sh[];
     __shared__ Row row;
     __shared__ uint32_t found;
     const uint32_t tid = threadIdx.x, wave = uniform(tid >> 6), H = a.cache.kv_heads;
@@ -194,8 +194,8 @@ int launch_few(const Args& a, hipStream_t stream) {
         }
     }
     if (!a.shared) {
-        if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, W, Args>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL((k_attend_few<NJ, RT, W, Args>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(64 * W), lds, stream, a);
+        if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, W>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        hipLaunchKernelGGL((k_attend_few<NJ, RT, W>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(64 * W), lds, stream, a);
     }
     if (a.splits > 1 || a.shared) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
     ZK_HIP_TRY(hipGetLastError());
@@ -205,8 +205,8 @@ int launch_few(const Args& a, hipStream_t stream) {
 template <int DT>
 int launch_many(const Args& a, hipStream_t stream) {
     const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
-    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT, Args>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_many<DT, Args>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs * a.splits), dim3(kBlock), lds, stream, a);
+    if (lds > 65536) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_attend_many<DT>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs * a.splits), dim3(kBlock), lds, stream, a);
     if (a.splits > 1) hipLaunchKernelGGL(k_attend_join, dim3(a.rows_most, a.cache.kv_heads, a.s.seqs), dim3(kBlock), 0, stream, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;

@@ -3,8 +3,8 @@
 // The keys of a row are those of the prefix and its sequence's own.  With (M, l, o) the maximum, the sum of weights and
 // the weighted values over a part of the keys, parts join by e^(M - max M): so the prefix is one part, or several, for ALL rows
 // of the batch at once, and its codes are read once for 128 rows where they would be read once for each sequence.
-// k_front: rows of the whole batch, 128 to a workgroup, over tiles of the prefix (the products that bound it are those of
-// k_attend_many); k_attend_few / k_attend_many: each sequence's own keys; k_front_join: adds up.
+// k_prefix: workgroups of two kinds in one launch.  The first have 128 rows of the whole batch over tiles of the prefix, which the
+// vector ALU bounds; those behind have a sequence's own keys, which latency bounds, and run beside them.  k_prefix_join adds up.
 #include "attend_dev.h"
 
 namespace zkmi {
@@ -17,7 +17,7 @@ struct PrefixArgs : Args {
     const int32_t* front;      // the prefix's pages
     uint32_t front_tokens;     // a multiple of the page
     uint32_t front_tiles;      // whole tiles of it; what is left is read with each sequence's own
-    uint32_t front_splits, front_each;
+    uint32_t front_splits, front_each, front_groups;
     float* front_parts;        // [head][split][row of the batch]
     float2* front_ml;
 };
@@ -36,44 +36,68 @@ __device__ __forceinline__ Tiles tiles_of(const PrefixArgs& a, const SeqView& v,
     return Tiles{a.front_tiles, end > a.front_tiles ? end : a.front_tiles};
 }
 
-// The prefix's whole tiles for 128 rows of the batch.
+struct FrontShared {
+    ManyShared many;
+    int32_t place[kRows], least, most;  // positions of the tokens that the rows belong to, -1: nobody's
+};
+// A part of the prefix's whole tiles for 128 rows of the batch.
 template <int DT>
-__global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_front(PrefixArgs a) {
-    extern __shared__ char lds[];
-    __shared__ ManyShared sh;
-    __shared__ int32_t place[kRows], least, most;  // positions of the tokens that the rows belong to, -1: nobody's
-    const uint32_t H = a.cache.kv_heads, h = blockIdx.x % H, r0 = blockIdx.x / H * kRows, split = blockIdx.y, tid = threadIdx.x;
-    const uint32_t R = a.s.rows * a.group, r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
+__device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, FrontShared& sh, uint32_t h, uint32_t tile, uint32_t split) {
+    const uint32_t r0 = tile * kRows, tid = threadIdx.x, R = a.s.rows * a.group, r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
-    if (tid < kRows) place[tid] = -1;
+    if (tid < kRows) sh.place[tid] = -1;
     if (tid == 0) {
-        least = 0x7fffffff;
-        most = -1;
+        sh.least = 0x7fffffff;
+        sh.most = -1;
     }
     __syncthreads();
     for (uint32_t b = tid; b < a.s.seqs; b += kBlock) {
         const SeqView v = seq_view(a.s, b, a.page_log);
         if (!v.ok || v.rows == 0) continue;
         const int32_t from = v.row0 > tok0 ? v.row0 : tok0, to = v.row0 + v.rows - 1 < tok1 ? v.row0 + v.rows - 1 : tok1;
-        for (int32_t t = from; t <= to; ++t) place[t - tok0] = v.len - v.rows + (t - v.row0);
+        for (int32_t t = from; t <= to; ++t) sh.place[t - tok0] = v.len - v.rows + (t - v.row0);
     }
     __syncthreads();
     if ((int32_t)tid <= tok1 - tok0) {
-        atomicMin(&least, place[tid]);
-        atomicMax(&most, place[tid]);
+        atomicMin(&sh.least, sh.place[tid]);
+        atomicMax(&sh.most, sh.place[tid]);
     }
     __syncthreads();
-    if (most < 0) return;  // no row of theirs sees a key, and k_front_join does not ask
+    const int32_t least = sh.least, most = sh.most;
+    if (most < 0) return;  // no row of theirs sees a key, and k_prefix_join does not ask
     Tiles tiles = {split * a.front_each, (split + 1) * a.front_each};
     if (tiles.end > a.front_tiles) tiles.end = a.front_tiles;
     const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
-    const int32_t pos = r < R ? place[r / a.group - (uint32_t)tok0] : -1;
+    const int32_t pos = r < R ? sh.place[r / a.group - (uint32_t)tok0] : -1;
     const SeqView all = {0, (int32_t)a.s.rows, 0, true};
-    attend_rows<DT>(a, lds, sh, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+    attend_rows<DT>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+}
+
+// RT: tiles of 16 rows that a sequence and head has, 0: many rows.  Workgroups of one head lie eight apart where there are eight heads, so
+// that an XCD reads the prefix of its own.
+template <int DT, int RT>
+__global__ __launch_bounds__(kBlock, DT <= 4 && RT < 2 ? 2 : 1) void k_prefix(PrefixArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ FrontShared sh;
+    const uint32_t H = a.cache.kv_heads;
+    if (blockIdx.x < a.front_groups) {
+        const uint32_t id = blockIdx.x, h = id % H, at = id / H, tile = at / a.front_splits;
+        return attend_front<DT>(a, lds, sh, h, tile, at - tile * a.front_splits);
+    }
+    uint32_t id = blockIdx.x - a.front_groups;
+    const uint32_t h = id % H;
+    id /= H;
+    const uint32_t split = id % a.splits;
+    id /= a.splits;
+    if constexpr (RT != 0) attend_few<(DT + 1) / 2, RT, 4>(a, (float*)lds, split, h, id);
+    else {
+        const uint32_t tiles = (a.rows_most + kRows - 1) / kRows, b = id / tiles;
+        attend_many<DT>(a, lds, sh.many, id - b * tiles, split, h, b);
+    }
 }
 
 // A wavefront: one row of one sequence and head.  Lanes hold four dimensions each; the lanes left of 64 take parts in turn.
-__global__ __launch_bounds__(kBlock) void k_front_join(PrefixArgs a) {
+__global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
     const uint32_t H = a.cache.kv_heads, d = a.cache.head_dim, b = blockIdx.y, lane = threadIdx.x & 63;
     const uint32_t item = uniform(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)), h = item / a.rows_most, r = item - h * a.rows_most;
     const SeqView v = seq_view(a.s, b, a.page_log);
@@ -132,7 +156,7 @@ bool few_rows(uint64_t rows) { return rows <= 32; }
 struct Plan {
     uint32_t front_tiles, front_splits, front_each, splits, each;
 };
-Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uint32_t prefix, uint32_t max_len) {
+Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uint32_t head_dim, uint32_t prefix, uint32_t max_len) {
     Plan p = {};
     p.front_tiles = prefix / kTile;
     const auto share = [](uint64_t groups, uint32_t tiles, uint32_t& splits, uint32_t& each) {
@@ -142,13 +166,26 @@ Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uin
         each = (uint32_t)div_up(tiles, n);
         splits = (uint32_t)div_up(tiles, each);
     };
-    if (p.front_tiles) share(kv_heads * div_up(rows, kRows), p.front_tiles, p.front_splits, p.front_each);
+    if (p.front_tiles) {
+        // Time of the prefix by the number of parts, in us: as many rounds of a workgroup to each CU as it takes, 0.41 a tile for each 32
+        // dimensions and 1 to begin with, and the parts' way to memory and back at 4 TB/s.  Measured for 320 rows and 8 heads of 128
+        // behind 8192 tokens, whole call: 4 parts 71 us, 8 46, 10 42, 16 44, 32 56; for 2450 rows behind 32768 1 part 875, 3 446, 10 439, 32 566.
+        const uint64_t groups = kv_heads * div_up(rows, kRows);
+        double best = 0.0;
+        for (uint32_t n = 1; n <= kMostParts && n <= p.front_tiles; ++n) {
+            const uint32_t each = (uint32_t)div_up(p.front_tiles, n);
+            if (div_up(p.front_tiles, each) != n) continue;
+            const double us = (double)div_up(groups * n, kWorkgroups / 2) * (0.41 * each * (double)div_up(head_dim, 32) + 1.0) +
+                              (double)(kv_heads * rows * head_dim) * n * 8.0 / 4e6;
+            if (n == 1 || us < best) {
+                best = us;
+                p.front_splits = n;
+                p.front_each = each;
+            }
+        }
+    }
     const uint32_t own = max_len > p.front_tiles * kTile ? (uint32_t)div_up(max_len - p.front_tiles * kTile, kTile) : 1;
     share((uint64_t)seqs * kv_heads * (few_rows(most) ? 1 : div_up(most, kRows)), own, p.splits, p.each);
-    if ((uint64_t)p.splits * seqs > 65535) {
-        p.splits = 65535 / seqs;
-        p.each = (uint32_t)div_up(own, p.splits);
-    }
     return p;
 }
 
@@ -166,37 +203,23 @@ size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint64_t most, uint32_t s
     return cv.used();
 }
 
-template <int DT>
-int launch_front(const PrefixArgs& a, uint64_t rows, hipStream_t s) {
-    const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
-    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_front<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_front<DT>), dim3((unsigned)(a.cache.kv_heads * div_up(rows, kRows)), a.front_splits), dim3(kBlock), lds, s, a);
-    return ZK_OK;
-}
-template <int DT>
-int launch_many(const PrefixArgs& a, hipStream_t s) {
-    const size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
-    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_many<DT, PrefixArgs>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_many<DT, PrefixArgs>), dim3(a.cache.kv_heads, (unsigned)div_up(a.rows_most, kRows), a.s.seqs * a.splits), dim3(kBlock), lds, s, a);
-    return ZK_OK;
-}
-template <int NJ, int RT>
-int launch_few(const PrefixArgs& a, hipStream_t s) {
-    const size_t lds = FewLds<NJ, RT, 4>::bytes(a.rows_most);
-    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_attend_few<NJ, RT, 4, PrefixArgs>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_attend_few<NJ, RT, 4, PrefixArgs>), dim3(a.splits, a.cache.kv_heads, a.s.seqs), dim3(kBlock), lds, s, a);
-    return ZK_OK;
-}
-template <int NJ>
-int launch(const PrefixArgs& a, uint64_t rows, hipStream_t s) {
-    const bool full = a.cache.head_dim > 64 * NJ - 32;
-    if (a.front_tiles) ZK_TRY(full ? launch_front<2 * NJ>(a, rows, s) : launch_front<2 * NJ - 1>(a, rows, s));
-    if (a.rows_most <= 16) ZK_TRY((launch_few<NJ, 1>(a, s)));
-    else if (a.few) ZK_TRY((launch_few<NJ, 2>(a, s)));
-    else ZK_TRY(full ? launch_many<2 * NJ>(a, s) : launch_many<2 * NJ - 1>(a, s));
-    hipLaunchKernelGGL(k_front_join, dim3((unsigned)div_up((size_t)a.rows_most * a.cache.kv_heads, kBlock / 64), a.s.seqs), dim3(kBlock), 0, s, a);
+template <int DT, int RT>
+int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
+    size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
+    if constexpr (RT != 0) {
+        const size_t few = FewLds<(DT + 1) / 2, RT, 4>::bytes(a.rows_most);
+        if (few > lds) lds = few;
+    }
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_prefix<DT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_prefix<DT, RT>), dim3((unsigned)(a.front_groups + own)), dim3(kBlock), lds, s, a);
+    hipLaunchKernelGGL(k_prefix_join, dim3((unsigned)div_up((size_t)a.rows_most * a.cache.kv_heads, kBlock / 64), a.s.seqs), dim3(kBlock), 0, s, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
+}
+template <int DT>
+int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
+    if (a.rows_most <= 16) return launch<DT, 1>(a, own, s);
+    return a.few ? launch<DT, 2>(a, own, s) : launch<DT, 0>(a, own, s);
 }
 
 // Rows of a sequence and head at most.
@@ -213,7 +236,7 @@ extern "C" size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32
     const uint32_t group = q_heads / kv_heads;
     const uint64_t all = (uint64_t)rows * group, most = rows_most(rows, max_new, group);
     Carver cv(nullptr, 0);
-    return carve(cv, plan_of(seqs, all, most, kv_heads, prefix_tokens, max_len), all, most, seqs, kv_heads, head_dim, nullptr);
+    return carve(cv, plan_of(seqs, all, most, kv_heads, head_dim, prefix_tokens, max_len), all, most, seqs, kv_heads, head_dim, nullptr);
 }
 
 extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
@@ -226,9 +249,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
     const uint64_t rows = (uint64_t)seqs->rows * group, most = rows_most(seqs->rows, seqs->max_new, group);
-    if (rows >= 0x7fffff00u || div_up(most, kRows) > 65535 || div_up(rows, kRows) * cache->kv_heads >= 0x80000000u ||
-        div_up(most * cache->kv_heads, kBlock / 64) >= 0x80000000u)
-        return ZK_E_BADARG;
+    if (rows >= 0x7fffff00u || div_up(most * cache->kv_heads, kBlock / 64) >= 0x80000000u) return ZK_E_BADARG;
     PrefixArgs a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -248,21 +269,29 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     a.rows_most = (uint32_t)most;
     a.front = prefix;
     a.front_tokens = prefix_pages * cache->page_tokens;
-    const Plan p = plan_of(seqs->seqs, rows, most, cache->kv_heads, a.front_tokens, seqs->max_len);
+    const Plan p = plan_of(seqs->seqs, rows, most, cache->kv_heads, cache->head_dim, a.front_tokens, seqs->max_len);
     a.front_tiles = p.front_tiles;
     a.front_splits = p.front_splits;
     a.front_each = p.front_each;
     a.splits = p.splits;
     a.each = p.each;
+    const uint64_t front = (uint64_t)cache->kv_heads * p.front_splits * div_up(rows, kRows);
+    const uint64_t own = (uint64_t)seqs->seqs * cache->kv_heads * p.splits * (a.few ? 1 : div_up(most, kRows));
+    if (front + own >= 0x80000000u) return ZK_E_BADARG;
+    a.front_groups = (uint32_t)front;
     if (!ws) return ZK_E_BUFSZ;
     Carver cv(ws, ws_bytes);
     carve(cv, p, rows, most, seqs->seqs, cache->kv_heads, cache->head_dim, &a);
     if (cv.overflow()) return ZK_E_BUFSZ;
     hipStream_t s = as_stream(stream);
-    switch ((cache->head_dim + 63) / 64) {
-        case 1: return launch<1>(a, rows, s);
-        case 2: return launch<2>(a, rows, s);
-        case 3: return launch<3>(a, rows, s);
-        default: return launch<4>(a, rows, s);
+    switch ((cache->head_dim + 31) / 32) {
+        case 1: return launch<1>(a, own, s);
+        case 2: return launch<2>(a, own, s);
+        case 3: return launch<3>(a, own, s);
+        case 4: return launch<4>(a, own, s);
+        case 5: return launch<5>(a, own, s);
+        case 6: return launch<6>(a, own, s);
+        case 7: return launch<7>(a, own, s);
+        default: return launch<8>(a, own, s);
     }
 }
