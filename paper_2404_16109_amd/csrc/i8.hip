@@ -5,7 +5,8 @@
 // Few rows (k_few: up to 64): the weights are read once, straight into registers, and bound the call.  A workgroup has 16 or 32
 // outputs, its eight wavefronts share k in steps of 128, so that every row of weights is read in whole lines.
 // Many rows (k_tiles): tiles of x and w come through LDS, put there by loads that pass no register, a step of 128 ahead; 16-byte
-// pieces lie in LDS at piece ^ (row & 7), so that eight neighbouring rows answer from different banks.  Where there are fewer tiles
+// pieces lie in LDS at piece ^ ((row / 2) & 7): rows of 128 bytes lie in one half of the banks or the other, so 16 neighbouring rows
+// answer from all of them.  Where there are fewer tiles
 // than the chip holds, workgroups share k and k_join adds up.
 #include "serve_dev.h"
 
@@ -173,8 +174,9 @@ __global__ __launch_bounds__(64 * WO * WR) void k_tiles(Args a, uint32_t row_til
     const uint32_t w_rows = a.n - o0 < outs ? a.n - o0 : outs, x_rows = a.rows - r0 < rows ? a.rows - r0 : rows;
     __amdgpu_buffer_rsrc_t wb = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (size_t)o0 * a.k), 0, (w_rows - 1) * a.k + a.k, 0x00020000);
     __amdgpu_buffer_rsrc_t xb = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (size_t)r0 * a.xrow), 0, (x_rows - 1) * (uint32_t)a.xrow + a.k, 0x00020000);
-    // A lane brings piece (lane & 7) ^ (row & 7) of row lane / 8 of each eight.
-    const uint32_t sub = lane >> 3, piece = ((lane & 7) ^ sub) * 16;
+    // A lane brings one piece of row lane / 8 of each eight; which eight of 16 they are is the same in all of its loads.
+    static_assert(waves % 2 == 0, "");
+    const uint32_t sub = lane >> 3, piece = ((lane & 7) ^ (4 * (wave & 1) + (sub >> 1))) * 16;
     uint32_t w_at[loads_w], x_at[loads_x];
 #pragma unroll
     for (int i = 0; i < loads_w; ++i) {
@@ -187,17 +189,24 @@ __global__ __launch_bounds__(64 * WO * WR) void k_tiles(Args a, uint32_t row_til
         x_at[i] = r < x_rows ? r * (uint32_t)a.xrow + piece : kOutside;
     }
     const uint32_t k_end = last * kStep < a.k ? last * kStep : a.k;
-    auto fetch = [&](uint32_t s, int8_t* to) {
-        const uint32_t j = s * kStep;
-        const bool in = j + piece < k_end;  // pieces behind the part are zeros
+    // Before the loads of a step that reaches behind the part: pieces there are zeros, from then on.
+    auto trim = [&](uint32_t step) {
+        if ((step + 1) * kStep > k_end && step * kStep + piece >= k_end) {
 #pragma unroll
-        for (int i = 0; i < loads_w; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wb, (lds_void*)(to + (i * waves + wave) * 1024), 16, in && w_at[i] != kOutside ? w_at[i] + j : kOutside, 0, 0, 0);
+            for (int i = 0; i < loads_w; ++i) w_at[i] = kOutside;
 #pragma unroll
-        for (int i = 0; i < loads_x; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xb, (lds_void*)(to + outs * kStep + (i * waves + wave) * 1024), 16, in && x_at[i] != kOutside ? x_at[i] + j : kOutside, 0,
-                                                     0, 0);
-        __builtin_amdgcn_sched_barrier(0);  // all of them before the products of the step that is there
+            for (int i = 0; i < loads_x; ++i) x_at[i] = kOutside;
+        }
+    };
+    auto load = [&](uint32_t step, int8_t* to, int i) {
+        const uint32_t j = step * kStep < k_end ? step * kStep : 0;
+        if (i < loads_w) __builtin_amdgcn_raw_ptr_buffer_load_lds(wb, (lds_void*)(to + (i * waves + wave) * 1024), 16, w_at[i < loads_w ? i : 0], j, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(xb, (lds_void*)(to + outs * kStep + ((i - loads_w) * waves + wave) * 1024), 16, x_at[i < loads_w ? 0 : i - loads_w], j, 0, 0);
+    };
+    auto fetch = [&](uint32_t step, int8_t* to) {
+        trim(step);
+#pragma unroll
+        for (int i = 0; i < loads_w + loads_x; ++i) load(step, to, i);
     };
     v16i acc[MO][NR];
 #pragma unroll
@@ -205,43 +214,59 @@ __global__ __launch_bounds__(64 * WO * WR) void k_tiles(Args a, uint32_t row_til
 #pragma unroll
         for (int r = 0; r < NR; ++r) acc[o][r] = v16i{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     const uint32_t w_row = (wo * MO * 32 + i32) * kStep, x_row = outs * kStep + (wr * NR * 32 + i32) * kStep;
-    // Operands are read a quarter of a step ahead of the products that take them.
-    auto multiply = [&](const int8_t* from) {
-        v4i w[2][MO], x[2][NR];
-        auto read = [&](int q) {
-            const uint32_t at = ((2 * q + half) ^ (i32 & 7)) * 16;
+    // Operands are read a quarter of a step ahead of the products that take them, those of the next step's first quarter too: the
+    // wait for that step and for everybody to be done with this one lies before the last quarter's products.
+    v4i w[2][MO], x[2][NR];
+    auto read = [&](const int8_t* from, int q) {
+        const uint32_t at = ((2 * q + half) ^ ((i32 >> 1) & 7)) * 16;
 #pragma unroll
-            for (int r = 0; r < NR; ++r) x[q & 1][r] = *(const v4i*)(from + x_row + r * 32 * kStep + at);
+        for (int r = 0; r < NR; ++r) x[q & 1][r] = *(const v4i*)(from + x_row + r * 32 * kStep + at);
 #pragma unroll
-            for (int o = 0; o < MO; ++o) w[q & 1][o] = *(const v4i*)(from + w_row + o * 32 * kStep + at);
-        };
-        read(0);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (q < 3) read(q + 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int o = 0; o < MO; ++o)
-#pragma unroll
-                for (int r = 0; r < NR; ++r) acc[o][r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q & 1][o], x[q & 1][r], acc[o][r], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int o = 0; o < MO; ++o) w[q & 1][o] = *(const v4i*)(from + w_row + o * 32 * kStep + at);
     };
-    // What is on its way to LDS has come, and everybody is done with what it replaces next.
+    auto multiply = [&](int q, auto between) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int o = 0; o < MO; ++o)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                acc[o][r] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q & 1][o], x[q & 1][r], acc[o][r], 0, 0, 0);
+                between(o * NR + r);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto nothing = [](int) {};
+    // Every operand of a step is in registers, and what is on its way to LDS has come.
     auto turn = [] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
+    };
+    auto step = [&](uint32_t s, int8_t* from, const int8_t* other) {
+        read(from, 1);
+        multiply(0, nothing);
+        read(from, 2);
+        multiply(1, nothing);
+        read(from, 3);
+        multiply(2, nothing);
+        turn();
+        read(other, 0);
+        trim(s + 2);
+        multiply(3, [&](int m) {  // the loads among the products
+            constexpr int each = (loads_w + loads_x + MO * NR - 1) / (MO * NR);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = m * each; i < (m + 1) * each && i < loads_w + loads_x; ++i) load(s + 2, from, i);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
     fetch(first, s0);
     turn();
+    read(s0, 0);
+    fetch(first + 1, s1);
 #pragma unroll 1
     for (uint32_t s = first; s < last; s += 2) {
-        fetch(s + 1, s1);
-        multiply(s0);
-        turn();
-        fetch(s + 2, s0);
-        multiply(s1);
-        turn();
+        step(s, s0, s1);
+        step(s + 1, s1, s0);
     }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
