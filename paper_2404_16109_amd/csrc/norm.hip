@@ -77,7 +77,7 @@ struct Raw {
 template <int DT>
 __device__ __forceinline__ float rounded(float f) {
     if constexpr (DT == ZK_F32) return f;
-    return half_of<DT>(half_bits<DT>(f), 0);
+    return half_of<DT>(half_bits<DT>(as_it_is(f)), 0);
 }
 
 // Stores a thread's elements; f is rounded to the type.
@@ -92,14 +92,14 @@ __device__ __forceinline__ void store_row(void* p, size_t row, const Place<DT, E
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if constexpr (DT == ZK_F32) q[k] = float_bits(f[v * W + k]);
-                else q[k] = (uint32_t)half_bits<DT>(f[v * W + 2 * k]) | ((uint32_t)half_bits<DT>(f[v * W + 2 * k + 1]) << 16);
+                else q[k] = (uint32_t)half_bits<DT>(as_it_is(f[v * W + 2 * k])) | ((uint32_t)half_bits<DT>(as_it_is(f[v * W + 2 * k + 1])) << 16);
             }
             if (at.in(v * W)) *(v4u*)(y + at.at(v * W)) = q;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < E; ++i)
-            if (at.in(i)) store_one<DT>((void*)y, at.at(i), f[i]);
+            if (at.in(i)) store_one<DT>((void*)y, at.at(i), as_it_is(f[i]));
     }
 }
 

@@ -50,6 +50,12 @@ __device__ __forceinline__ uint16_t half_bits(float f) {
     return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
+// f as it is, rounded to 32 bits: a product is not joined with the rounding to 16 that follows (v_fma_mix has one rounding for both).
+__device__ __forceinline__ float as_it_is(float f) {
+    asm("" : "+v"(f));
+    return f;
+}
+
 // Over the 64 lanes of a wavefront, in every lane: moves within rows of 16 lanes, then two broadcasts from row to row, all at
 // the rate of the vector ALU (lanes_sum in reduce_dev.h has the same steps).  Lanes without a partner keep their own.
 template <int CTRL, int ROWS>
