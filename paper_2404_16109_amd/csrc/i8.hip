@@ -2,7 +2,7 @@
 //
 // Sums are exact in 32 bits (|x w| <= 2^14, k < 2^17), in whatever order: parts of k may be added up anywhere.
 //
-// Few rows (k_few: up to 64): the weights are read once, straight into registers, and bound the call.  A workgroup has 16 or 32
+// Few rows (k_few: up to 32): the weights are read once, straight into registers, and bound the call.  A workgroup has 16 to 64
 // outputs, its eight wavefronts share k in steps of 128, so that every row of weights is read in whole lines.
 // Many rows (k_tiles): tiles of x and w come through LDS, put there by loads that pass no register, a step of 128 ahead; 16-byte
 // pieces lie in LDS at piece ^ ((row / 2) & 7): rows of 128 bytes lie in one half of the banks or the other, so 16 neighbouring rows
@@ -353,48 +353,87 @@ __global__ __launch_bounds__(kBlock) void k_join(Args a) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 
-enum Tile { kFew16, kFew32, kFew64, kMid, kLarge };
+enum Tile { kFew, kShort, kMid, kWide, kLarge };
 struct Plan {
     Tile tile;
-    uint32_t nt, groups, splits, each;
+    uint32_t nt, groups, splits, each;  // nt: tiles of 16 outputs to a workgroup of k_few
 };
-Plan plan_of(size_t rows, size_t n, size_t k) {
-    Plan p = {};
-    const uint32_t steps = (uint32_t)div_up(k, kStep);
-    uint64_t want;
-    uint32_t least;  // steps worth a part
-    if (rows <= 64) {
-        p.tile = rows <= 16 ? kFew16 : rows <= 32 ? kFew32 : kFew64;
-        p.nt = div_up(n, 32) >= 256 ? 2 : 1;
-        p.groups = (uint32_t)div_up(n, 16 * p.nt);
-        want = 256;
-        least = 2 * kWaves;
-    } else {
-        const uint64_t large = div_up(rows, 256) * div_up(n, 256);
-        p.tile = large >= 192 ? kLarge : kMid;
-        p.groups = (uint32_t)(p.tile == kLarge ? large : div_up(rows, 128) * div_up(n, 128));
-        want = p.tile == kLarge ? 256 : 512;
-        least = 8;
-    }
-    uint64_t splits = p.groups >= want / 2 + 1 ? 1 : want / p.groups;
-    if (splits > steps / least) splits = steps / least;
-    if (splits < 1) splits = 1;
-    p.each = (uint32_t)align_up(div_up(steps, splits), 2);  // k_tiles takes two at a time
+void share_k(Plan& p, uint32_t steps, uint32_t splits) {
+    p.each = (uint32_t)align_up(div_up(steps, splits), 2);  // k_tiles takes two steps at a time
     p.splits = (uint32_t)div_up(steps, p.each);
+}
+
+// Up to 32 rows.  More outputs to a workgroup read x less often, fewer fill the chip.  Measured, us, weights from HBM, 16 / 32 / 64 outputs
+// to a workgroup: one row by 13824 x 5120 16.8 18.6 19.1, 16 rows 25.2 23.6 20.9, 32 rows 38 29 23.7; 32 rows by 5120 x 13824 46 33 48, and
+// with k shared by three 36 29 24.3; 32 rows by 5120 x 5120 16 11.9 16.4 (shared 15 13 12.3); 16 rows by 2000 x 8192 9.9 13.2.
+Plan plan_few(uint32_t rows, size_t n, uint32_t steps) {
+    Plan p = {};
+    p.tile = kFew;
+    const bool shares = rows > 16 && steps >= 64;  // a part takes eight steps at least, and a launch to join them
+    p.nt = rows <= 4 ? 1 : n >= 64 * 200 || (shares && n >= 64 * 32) ? 4 : n >= 32 * 128 ? 2 : 1;
+    p.groups = (uint32_t)div_up(n, 16 * p.nt);
+    uint32_t splits = p.groups < 128 ? 256 / p.groups : 1;
+    const uint32_t most = p.nt == 4 || p.groups <= 32 ? steps / (2 * kWaves) : steps / (16 * kWaves);
+    if (splits > most) splits = most;
+    share_k(p, steps, splits ? splits : 1);
     return p;
 }
 
+// Tiles of more rows: rows and outputs, workgroups to a CU, and us a step of 128 with one, two or three of them there.  Measured with
+// as many tiles as the chip takes at once, the difference between k 8192 and 2048.
+struct Shape {
+    uint32_t rows, outs, slots;
+    double step[3];
+};
+const Shape kShapes[] = {{}, {64, 128, 3, {0.57, 0.81, 0.90}}, {128, 128, 2, {0.66, 0.95}}, {192, 256, 1, {1.38}}, {256, 256, 1, {1.69}}};
+
+// The tile and the parts of k that take least: rounds of the chip's 256 CUs, each with what a workgroup begins and ends with, and the parts'
+// way to memory and back.  Measured and, in brackets, tiles of 128 x 128 in as many parts as are best: 2048 x 5120 x 5120 56.7 us (76.5), of
+// 600 x 2000 x 27200 58.0 (58.0), of 1000 x 5120 x 5120 38.9 (38.9), of 8192 x 13824 x 5120 523.
+Plan plan_tiles(size_t rows, size_t n, uint32_t steps) {
+    Plan best = {};
+    double least = 0.0;
+    for (int t = kShort; t <= kLarge; ++t) {
+        const Shape& s = kShapes[t];
+        const uint64_t groups = div_up(rows, s.rows) * div_up(n, s.outs);
+        for (uint32_t splits = 1; splits <= 16 && splits * 4 <= (steps < 4 ? 4 : steps); ++splits) {
+            if (splits > 1 && groups * (splits - 1) >= 256 * s.slots) break;
+            Plan p = {};
+            p.tile = (Tile)t;
+            p.groups = (uint32_t)groups;
+            share_k(p, steps, splits);
+            const uint64_t all = groups * p.splits, chip = 256 * s.slots, rest = all % chip;
+            const double rounds = (double)(all / chip) * (p.each * s.step[s.slots - 1] + 3.0) + (rest ? p.each * s.step[(rest - 1) / 256] + 3.0 : 0.0);
+            const double us = rounds + (p.splits > 1 ? 2.0 + 8.0 * (double)rows * (double)n * p.splits / 8e6 : 0.0);
+            if (!best.groups || us < least) {
+                least = us;
+                best = p;
+            }
+        }
+    }
+    return best;
+}
+Plan plan_of(size_t rows, size_t n, size_t k) {
+    const uint32_t steps = (uint32_t)div_up(k, kStep);
+    return rows <= 32 ? plan_few((uint32_t)rows, n, steps) : plan_tiles(rows, n, steps);
+}
+
+template <int RT, int Y>
+void launch_few(const Args& a, const Plan& p, hipStream_t s) {
+    const dim3 grid(p.groups, p.splits), block(64 * kWaves);
+    if (p.nt == 1) hipLaunchKernelGGL((k_few<RT, 1, Y>), grid, block, 0, s, a);
+    else if (p.nt == 2) hipLaunchKernelGGL((k_few<RT, 2, Y>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_few<RT, 4, Y>), grid, block, 0, s, a);
+}
 template <int Y>
 int launch(const Args& a, const Plan& p, hipStream_t s) {
-    const dim3 grid(p.groups, p.splits), few(64 * kWaves);
-    const uint32_t rt = (uint32_t)div_up(a.rows, p.tile == kLarge ? 256 : 128), nt = (uint32_t)div_up(a.n, p.tile == kLarge ? 256 : 128);
-    if (p.tile == kFew16 && p.nt == 1) hipLaunchKernelGGL((k_few<1, 1, Y>), grid, few, 0, s, a);
-    else if (p.tile == kFew16) hipLaunchKernelGGL((k_few<1, 2, Y>), grid, few, 0, s, a);
-    else if (p.tile == kFew32 && p.nt == 1) hipLaunchKernelGGL((k_few<2, 1, Y>), grid, few, 0, s, a);
-    else if (p.tile == kFew32) hipLaunchKernelGGL((k_few<2, 2, Y>), grid, few, 0, s, a);
-    else if (p.tile == kFew64 && p.nt == 1) hipLaunchKernelGGL((k_few<4, 1, Y>), grid, few, 0, s, a);
-    else if (p.tile == kFew64) hipLaunchKernelGGL((k_few<4, 2, Y>), grid, few, 0, s, a);
+    const dim3 grid(p.groups, p.splits);
+    const Shape& t = kShapes[p.tile];
+    const uint32_t rt = p.tile == kFew ? 0 : (uint32_t)div_up(a.rows, t.rows), nt = p.tile == kFew ? 0 : (uint32_t)div_up(a.n, t.outs);
+    if (p.tile == kFew) a.rows <= 16 ? launch_few<1, Y>(a, p, s) : launch_few<2, Y>(a, p, s);
+    else if (p.tile == kShort) hipLaunchKernelGGL((k_tiles<2, 1, 2, 2, Y>), grid, dim3(256), 0, s, a, rt, nt);
     else if (p.tile == kMid) hipLaunchKernelGGL((k_tiles<2, 2, 2, 2, Y>), grid, dim3(256), 0, s, a, rt, nt);
+    else if (p.tile == kWide) hipLaunchKernelGGL((k_tiles<2, 3, 4, 2, Y>), grid, dim3(512), 0, s, a, rt, nt);
     else hipLaunchKernelGGL((k_tiles<4, 2, 2, 4, Y>), grid, dim3(512), 0, s, a, rt, nt);
     if (p.splits > 1) hipLaunchKernelGGL((k_join<Y>), dim3((unsigned)div_up((size_t)a.rows * (a.n_pad >> 2), kBlock)), dim3(kBlock), 0, s, a);
     ZK_HIP_TRY(hipGetLastError());

@@ -54,6 +54,14 @@ def test_large(rows, n, k):
     check(rows, n, k, F16)
 
 
+@pytest.mark.parametrize("rows,n,k", [(16, 12801, 400), (32, 12805, 272), (5, 4100, 272), (31, 4099, 144), (20, 2100, 8208), (2000, 5100, 528), (380, 32000, 144),
+                                      (190, 12900, 1040), (1537, 8193, 272)])
+def test_every_tile(rows, n, k):
+    """16 to 64 outputs to a workgroup of few rows, tiles of 128 x 128, 256 x 192 and 256 x 256, all with odd ends."""
+    for dtype in (I32, F32, BF16):
+        check(rows, n, k, dtype)
+
+
 @pytest.mark.parametrize("rows,n", [(1, 33), (40, 20), (200, 130)])
 def test_largest_sums(rows, n):
     """-128 * -128 over the longest k: 2147221504, just below 2^31; and its negative."""
