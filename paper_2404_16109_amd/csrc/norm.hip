@@ -132,6 +132,16 @@ __device__ __forceinline__ double all_add(double x, Scratch& s, int turn, uint32
     return sum;
 }
 
+// What a norm takes off and multiplies by.
+struct Stats {
+    float mean, rstd;
+};
+__device__ __forceinline__ float rstd_of(double squares, double n, float eps) { return (float)(1.0 / sqrt(squares / n + (double)eps)); }
+__device__ __forceinline__ float normed(float v, int kind, const Stats& st) {
+    if (kind == ZK_NORM_LAYER) v = v - st.mean;
+    return kind == ZK_NORM_NONE ? v : v * st.rstd;
+}
+
 // v = (v - mean) * rstd * gain + bias, statistics over the workgroup's row.  `turn` counts the sums.
 template <int DT, int E, bool WIDE>
 __device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, const Raw<DT, E, WIDE>& gain, bool has_gain,
@@ -154,14 +164,9 @@ __device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, co
 #pragma unroll
             for (int i = 0; i < E; ++i) sum = __builtin_fma((double)v[i], (double)v[i], sum);
         }
-        const float rstd = (float)(1.0 / sqrt(all_add(sum, s, turn++, waves) / n + (double)eps));
-        if (kind == ZK_NORM_LAYER) {
-            const float m = (float)mean;
+        const Stats st = {(float)mean, rstd_of(all_add(sum, s, turn++, waves), n, eps)};
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = v[i] - m;
-        }
-#pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = v[i] * rstd;
+        for (int i = 0; i < E; ++i) v[i] = normed(v[i], kind, st);
     }
     if (has_gain) {
 #pragma unroll
@@ -183,6 +188,16 @@ __device__ __forceinline__ bool code_scale(uint32_t most, float& scale, float& i
 }
 __device__ __forceinline__ uint32_t code_of(float h, float inv) { return float_bits(h * inv + 12582912.0f) & 0xffu; }
 
+__device__ __forceinline__ uint32_t all_most(uint32_t most, Scratch& s, uint32_t waves) {
+    most = wave_max(most);
+    if (waves > 1) {
+        if ((threadIdx.x & 63) == 0) s.most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        for (uint32_t w = 0; w < waves; ++w) most = s.most[w] > most ? s.most[w] : most;
+    }
+    return most;
+}
+
 template <int DT, int E, bool WIDE>
 __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* scale_at, const Place<DT, E, WIDE>& at, const float (&h)[E], Scratch& s,
                                             uint32_t waves) {
@@ -193,14 +208,8 @@ __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* sc
         const uint32_t bits = at.in(i) ? float_bits(h[i]) & 0x7fffffffu : 0u;
         most = bits > most ? bits : most;
     }
-    most = wave_max(most);
-    if (waves > 1) {
-        if ((threadIdx.x & 63) == 0) s.most[threadIdx.x >> 6] = most;
-        __syncthreads();
-        for (uint32_t w = 0; w < waves; ++w) most = s.most[w] > most ? s.most[w] : most;
-    }
     float scale, inv;
-    const bool some = code_scale(most, scale, inv);
+    const bool some = code_scale(all_most(most, s, waves), scale, inv);
     if (threadIdx.x == 0) *scale_at = scale;
     int8_t* y = codes + row;
     if constexpr (WIDE) {
@@ -265,6 +274,71 @@ __global__ __launch_bounds__(kMostThreads) void k_block_norm(NormArgs n) {
     else store_codes<DT, E, WIDE>(a.codes, row * a.codes_row_stride, a.scales + row, at, v, s, waves);
 }
 
+// Rows of more than 16 elements to a thread (or of eight that no 16-byte load takes): the row lies in LDS, in 32 bits, each element
+// read and written by the thread that brought it.  In registers, with the gains beside, they would spill (100 us for one row).
+template <int DT>
+__global__ __launch_bounds__(kMostThreads) void k_block_norm_long(NormArgs n) {
+    extern __shared__ __attribute__((aligned(16))) float line[];
+    __shared__ Scratch s;
+    const block_norm_args& a = n.a;
+    const size_t row = blockIdx.x;
+    const uint32_t waves = kMostThreads / 64, dim = n.dim;
+    int turn = 0;
+    auto statistics = [&](int kind) {
+        Stats st = {0.0f, 1.0f};
+        if (kind == ZK_NORM_NONE) return st;
+        double mean = 0.0, sum = 0.0;
+        if (kind == ZK_NORM_LAYER) {
+            for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) sum += (double)line[i];
+            mean = all_add(sum, s, turn++, waves) / (double)dim;
+            sum = 0.0;
+        }
+        for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
+            const double d = (double)line[i] - mean;
+            sum = __builtin_fma(d, d, sum);
+        }
+        st.rstd = rstd_of(all_add(sum, s, turn++, waves), (double)dim, a.eps);
+        st.mean = (float)mean;
+        return st;
+    };
+    auto finished = [&](float v, int kind, const Stats& st, const void* gain, const void* bias, uint32_t i) {
+        v = normed(v, kind, st);
+        if (gain) v = v * load_one<DT>(gain, i);
+        return bias ? v + load_one<DT>(bias, i) : v;
+    };
+    if (a.z) {
+        for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) line[i] = load_one<DT>(a.z, row * a.z_row_stride + i);
+        const Stats st = statistics(a.post_norm);
+        for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
+            float t = finished(line[i], a.post_norm, st, a.post_gain, a.post_bias, i);
+            if (a.gate) t = load_one<DT>(a.gate, row * a.gate_row_stride + i) * t;
+            line[i] = a.alpha * load_one<DT>(a.x, row * a.x_row_stride + i) + t;
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) line[i] = a.alpha * load_one<DT>(a.x, row * a.x_row_stride + i);
+    }
+    for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
+        const float v = line[i];
+        if (a.r) store_one<DT>(a.r, row * a.r_row_stride + i, as_it_is(v));
+        line[i] = rounded<DT>(v);
+    }
+    if (!a.h && !a.codes) return;
+    const Stats st = statistics(a.norm);
+    uint32_t most = 0;
+    for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
+        const float h = finished(line[i], a.norm, st, a.gain, a.bias, i);
+        if (a.h) store_one<DT>(a.h, row * a.h_row_stride + i, as_it_is(h));
+        line[i] = h;
+        const uint32_t bits = float_bits(h) & 0x7fffffffu;
+        most = bits > most ? bits : most;
+    }
+    if (!a.codes) return;
+    float scale, inv;
+    const bool some = code_scale(all_most(most, s, waves), scale, inv);
+    if (threadIdx.x == 0) a.scales[row] = scale;
+    for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) a.codes[row * a.codes_row_stride + i] = some ? (int8_t)code_of(line[i], inv) : (int8_t)0;
+}
+
 template <int DT, int E, bool WIDE>
 __global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
     __shared__ Scratch s;
@@ -281,19 +355,15 @@ __global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t
 // Rows longer than the registers of a workgroup: read twice, the second time from a cache that holds them.
 template <int DT>
 __global__ __launch_bounds__(kMostThreads) void k_quantise_long(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
-    __shared__ uint32_t largest[kMostThreads / 64];
+    __shared__ Scratch s;
     const size_t row = blockIdx.x, from = row * x_row;
     uint32_t most = 0;
     for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
         const uint32_t bits = float_bits(load_one<DT>(x, from + i)) & 0x7fffffffu;
         most = bits > most ? bits : most;
     }
-    most = wave_max(most);
-    if ((threadIdx.x & 63) == 0) largest[threadIdx.x >> 6] = most;
-    __syncthreads();
-    for (uint32_t w = 0; w < kMostThreads / 64; ++w) most = largest[w] > most ? largest[w] : most;
     float scale, inv;
-    const bool some = code_scale(most, scale, inv);
+    const bool some = code_scale(all_most(most, s, kMostThreads / 64), scale, inv);
     if (threadIdx.x == 0) scales[row] = scale;
     for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads)
         codes[row * codes_row + i] = some ? (int8_t)code_of(load_one<DT>(x, from + i), inv) : (int8_t)0;
@@ -304,31 +374,40 @@ __global__ __launch_bounds__(kMostThreads) void k_quantise_long(int8_t* codes, s
 bool float_type(int dtype) { return dtype == ZK_F32 || dtype == ZK_F16 || dtype == ZK_BF16; }
 bool norm_kind(int kind) { return kind == ZK_NORM_NONE || kind == ZK_NORM_RMS || kind == ZK_NORM_LAYER; }
 
-// How a row is spread: elements of a thread, and threads.
+// How a row is spread: elements of a thread, and threads.  As few elements as 1024 threads allow; of many rows 16, which takes fewer steps
+// to add up a row and to bring gains: 8192 rows of 5120 bf16 104 -> 89 us (one row 3.7 -> 4.1, so not of few).
 struct Spread {
     int each;
     uint32_t threads;
 };
-Spread spread_of(int dtype, uint32_t dim, size_t rows) {
-    const int least = dtype == ZK_F32 ? 4 : 8;
-    int each = least;
+Spread spread_of(int dtype, uint32_t dim, size_t rows, bool wide) {
+    int each = dtype == ZK_F32 ? 4 : 8;
+    if (each == 8 && wide && rows >= 1024 && dim >= 1024) each = 16;
     while (each < 32 && div_up(dim, each) > kMostThreads) each *= 2;
-    (void)rows;
     return {each, (uint32_t)align_up(div_up(dim, each), 64)};
 }
 
 template <int DT, int E, bool WIDE>
-void launch_norm(const NormArgs& n, unsigned rows, uint32_t threads, hipStream_t s) {
+int launch_norm(const NormArgs& n, unsigned rows, uint32_t threads, hipStream_t s) {
     hipLaunchKernelGGL((k_block_norm<DT, E, WIDE>), dim3(rows), dim3(threads), 0, s, n);
+    return ZK_OK;
+}
+template <int DT>
+int launch_long(const NormArgs& n, unsigned rows, hipStream_t s) {
+    const size_t lds = n.dim * sizeof(float);
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_block_norm_long<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_block_norm_long<DT>), dim3(rows), dim3(kMostThreads), lds, s, n);
+    return ZK_OK;
 }
 template <int DT, bool WIDE>
-void spread_norm(const NormArgs& n, unsigned rows, hipStream_t s) {
-    const Spread p = spread_of(DT, n.dim, rows);
+int spread_norm(const NormArgs& n, unsigned rows, hipStream_t s) {
+    const Spread p = spread_of(DT, n.dim, rows, WIDE);
     if constexpr (DT == ZK_F32)
         if (p.each == 4) return launch_norm<DT, 4, WIDE>(n, rows, p.threads, s);
     if (p.each == 8) return launch_norm<DT, 8, WIDE>(n, rows, p.threads, s);
-    if (p.each == 16) return launch_norm<DT, 16, WIDE>(n, rows, p.threads, s);
-    launch_norm<DT, 32, WIDE>(n, rows, p.threads, s);
+    if constexpr (WIDE)
+        if (p.each == 16) return launch_norm<DT, 16, WIDE>(n, rows, p.threads, s);
+    return launch_long<DT>(n, rows, s);
 }
 
 struct QuantiseArgs {
@@ -345,7 +424,7 @@ void launch_quantise(const QuantiseArgs& q, unsigned rows, uint32_t threads, hip
 }
 template <int DT, bool WIDE>
 void spread_quantise(const QuantiseArgs& q, unsigned rows, hipStream_t s) {
-    const Spread p = spread_of(DT, q.dim, rows);
+    const Spread p = spread_of(DT, q.dim, rows, WIDE);
     if constexpr (DT == ZK_F32)
         if (p.each == 4) return launch_quantise<DT, 4, WIDE>(q, rows, p.threads, s);
     if (p.each == 8) return launch_quantise<DT, 8, WIDE>(q, rows, p.threads, s);
@@ -397,9 +476,9 @@ extern "C" int block_norm(const block_norm_args* args, int dtype, size_t rows, s
     const NormArgs n = {a, dtype, (uint32_t)dim};
     hipStream_t s = as_stream(stream);
     const unsigned r = (unsigned)rows;
-    if (dtype == ZK_F32) wide ? spread_norm<ZK_F32, true>(n, r, s) : spread_norm<ZK_F32, false>(n, r, s);
-    else if (dtype == ZK_F16) wide ? spread_norm<ZK_F16, true>(n, r, s) : spread_norm<ZK_F16, false>(n, r, s);
-    else wide ? spread_norm<ZK_BF16, true>(n, r, s) : spread_norm<ZK_BF16, false>(n, r, s);
+    if (dtype == ZK_F32) ZK_TRY((wide ? spread_norm<ZK_F32, true>(n, r, s) : spread_norm<ZK_F32, false>(n, r, s)));
+    else if (dtype == ZK_F16) ZK_TRY((wide ? spread_norm<ZK_F16, true>(n, r, s) : spread_norm<ZK_F16, false>(n, r, s)));
+    else ZK_TRY((wide ? spread_norm<ZK_BF16, true>(n, r, s) : spread_norm<ZK_BF16, false>(n, r, s)));
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }

@@ -77,6 +77,21 @@ def test_widths(dim, dtype):
         check(*case(3, dim, dtype, norm, zk.ZK_NORM_NONE, 1, norm == zk.ZK_NORM_LAYER), quantise)
 
 
+@pytest.mark.parametrize("dim", [1024, 1032, 5120, 8192, 16384])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_many_rows(dim, dtype):
+    for norm, quantise in ((zk.ZK_NORM_RMS, True), (zk.ZK_NORM_LAYER, False)):
+        check(*case(1024, dim, dtype, norm, zk.ZK_NORM_RMS, 1, False), quantise)
+
+
+@pytest.mark.parametrize("dim", [8193, 16385, 20000, 32768])
+def test_long_rows_of_all_kinds(dim):
+    for i, (norm, post, gate, biased) in enumerate(itertools.product((0, 1, 2), (0, 1, 2), (0, 1, 2), (False, True))):
+        if i % 4 == dim % 4:
+            check(*case(2, dim, (F32, F16, BF16)[i % 3], norm, post, gate, biased), bool(i & 2))
+    check(*case(3, dim, BF16, zk.ZK_NORM_RMS, 0, 0, False, block=False), True)
+
+
 @pytest.mark.parametrize("norm", [0, 1, 2])
 @pytest.mark.parametrize("post", [0, 1, 2])
 @pytest.mark.parametrize("gate", [0, 1, 2])
