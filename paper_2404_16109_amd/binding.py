@@ -934,21 +934,24 @@ def kvcache_attention_prefix(cache, q, cu, lens, table, prefix, max_new, max_len
     """As kvcache_attention, for a batch that begins with the same tokens: prefix: int32, the pages that hold them.  Returns
     (rc, out, lse)."""
     rows, heads, dim = q.shape
-    assert dim == cache.c.head_dim and q.is_cuda and q.stride(2) == 1
-    assert prefix.dtype == torch.int32 and prefix.dim() == 1 and prefix.is_cuda and prefix.is_contiguous(), "prefix: int32 on the GPU"
+    device, stream = _current()
+    assert dim == cache.c.head_dim and q.stride(2) == 1
+    assert prefix.dtype == torch.int32 and prefix.dim() == 1 and prefix.is_contiguous(), "prefix: int32"
     if out is None:
         out = torch.empty(rows, heads, dim, dtype=q.dtype, device=q.device)
     if lse is None:
         lse = torch.empty(rows, heads, dtype=torch.float32, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.stride(2) == 1
-    assert lse.shape == (rows, heads) and lse.dtype == torch.float32 and lse.is_cuda and lse.is_contiguous()
+    assert out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1
+    assert lse.shape == (rows, heads) and lse.dtype == torch.float32 and lse.is_contiguous()
     s = _kv_seqs(cu, lens, table, rows, max_new, max_len, fault)
     if ws is None:
         ws = _ws(_lib.kvcache_attention_prefix_workspace_bytes(s.seqs, rows, max_new, heads, cache.c.kv_heads, dim,
                                                                prefix.numel() * cache.c.page_tokens, max_len))
+    for t in (cache.k, q, cu, lens, table, prefix, out, lse, ws):
+        assert t.get_device() == device, "tensors on the current GPU"
     rc = _lib.kvcache_attention_prefix(ctypes.byref(cache.c), q.data_ptr(), q.stride(0), q.stride(1), _DTYPES[q.dtype], heads,
                                        ctypes.byref(s), prefix.data_ptr(), prefix.numel(), scale, out.data_ptr(), out.stride(0),
-                                       out.stride(1), lse.data_ptr(), *_workspace(ws), _stream())
+                                       out.stride(1), lse.data_ptr(), *_workspace(ws), stream)
     return rc, out, lse
 
 
@@ -1029,30 +1032,39 @@ _FLOATS = {torch.float32: ZK_F32, torch.float16: ZK_F16, torch.bfloat16: ZK_BF16
 _PRODUCTS = {**_FLOATS, torch.int32: ZK_I32}
 
 
-def _matrix(t, rows, cols, dtype, name):
-    """The address of a rows x cols tensor whose rows are contiguous."""
-    assert t.dtype == dtype and t.shape == (rows, cols) and t.is_cuda and (t.stride(1) == 1 or cols == 1), name
-    return t.data_ptr()
+def _current():
+    """The current device and its stream: where the tensors of a call have to lie, and what it is enqueued on."""
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
-def _vector(t, n, dtype, name):
-    """The address of a vector of n elements, or None."""
+def _matrix(t, shape, dtype, device, name):
+    """(address, row stride) of a tensor of that shape on the current GPU whose rows are contiguous."""
+    row, one = t.stride()
+    assert t.dtype == dtype and t.shape == shape and t.get_device() == device and (one == 1 or shape[1] == 1), name
+    return t.data_ptr(), row
+
+
+def _vector(t, shape, dtype, device, name):
+    """The address of a vector of that shape, or None."""
     if t is None:
         return None
-    assert t.dtype == dtype and t.shape == (n,) and t.is_cuda and t.is_contiguous(), name
+    assert t.dtype == dtype and t.shape == shape and t.get_device() == device and t.is_contiguous(), name
     return t.data_ptr()
 
 
 def i8_quantise(x, codes=None, scales=None):
     """x: (rows, k).  Returns (rc, codes, scales): int8 (rows, k) and float32 (rows), made where they are not given."""
-    rows, k = x.shape
+    shape = rows, k = x.shape
     if codes is None:
         codes = torch.empty(rows, k, dtype=torch.int8, device=x.device)
     if scales is None:
         scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    at = _matrix(x, rows, k, x.dtype, "x")
-    rc = _lib.i8_quantise(_matrix(codes, rows, k, torch.int8, "codes"), codes.stride(0), _vector(scales, rows, torch.float32, "scales"), at,
-                          x.stride(0), _FLOATS[x.dtype], rows, k, _stream())
+    device, stream = _current()
+    rc = _lib.i8_quantise(*_matrix(codes, shape, torch.int8, device, "codes"), _vector(scales, (rows,), torch.float32, device, "scales"),
+                          *_matrix(x, shape, x.dtype, device, "x"), _FLOATS[x.dtype], rows, k, stream)
     return rc, codes, scales
 
 
@@ -1067,14 +1079,16 @@ def i8_matmul(x, w, x_scales=None, w_scales=None, out=None, dtype=torch.bfloat16
     n = w.shape[0]
     if out is None:
         out = torch.empty(rows, n, dtype=dtype, device=x.device)
-    y = _matrix(out, rows, n, out.dtype, "out")
     assert w.is_contiguous(), "w: contiguous"
-    need = _lib.i8_matmul_workspace_bytes(rows, n, k)
-    if ws is None and need:
-        ws = _ws(need)
-    rc = _lib.i8_matmul(y, out.stride(0), _PRODUCTS[out.dtype], _matrix(x, rows, k, torch.int8, "x"), x.stride(0),
-                        _vector(x_scales, rows, torch.float32, "x_scales"), rows, _matrix(w, n, k, torch.int8, "w"),
-                        _vector(w_scales, n, torch.float32, "w_scales"), n, k, *_workspace(ws), _stream())
+    if ws is None:
+        need = _lib.i8_matmul_workspace_bytes(rows, n, k)
+        ws = _ws(need) if need else None
+    kind = out.dtype
+    device, stream = _current()
+    assert ws is None or ws.get_device() == device, "ws: on the current GPU"
+    rc = _lib.i8_matmul(*_matrix(out, (rows, n), kind, device, "out"), _PRODUCTS[kind], *_matrix(x, (rows, k), torch.int8, device, "x"),
+                        _vector(x_scales, (rows,), torch.float32, device, "x_scales"), rows, _matrix(w, (n, k), torch.int8, device, "w")[0],
+                        _vector(w_scales, (n,), torch.float32, device, "w_scales"), n, k, *_workspace(ws), stream)
     return rc, out
 
 
@@ -1083,33 +1097,29 @@ def block_norm(x, z=None, *, norm=ZK_NORM_RMS, gain=None, bias=None, eps=1e-5, p
     """x, z: (rows, dim); gains and biases: (dim); gate: (dim) or (rows, dim), all of one type.  Returns (rc, r, h, scales): r the
     residual stream (x where the call leaves it as it is), h what the next block is given, of x's type, or int8 codes (quantise=True, or
     an int8 tensor as h) with scales: float32 (rows), else None.  r and h are made where they are not given."""
-    rows, dim = x.shape
+    shape = rows, dim = x.shape
     kind = x.dtype
     if r is None and (z is not None or alpha != 1.0):
         r = torch.empty(rows, dim, dtype=kind, device=x.device)
     if h is None:
         h = torch.empty(rows, dim, dtype=torch.int8 if quantise else kind, device=x.device)
     coded = h.dtype == torch.int8
-    if coded and scales is None:
+    if not coded:
+        scales = None
+    elif scales is None:
         scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    a = block_norm_args()
-    a.x, a.x_row_stride = _matrix(x, rows, dim, kind, "x"), x.stride(0)
-    if z is not None:
-        a.z, a.z_row_stride = _matrix(z, rows, dim, kind, "z"), z.stride(0)
-    if gate is not None:
-        if gate.dim() == 1:
-            a.gate, a.gate_row_stride = _vector(gate, dim, kind, "gate"), 0
-        else:
-            a.gate, a.gate_row_stride = _matrix(gate, rows, dim, kind, "gate"), gate.stride(0)
-    a.post_gain, a.post_bias = _vector(post_gain, dim, kind, "post_gain"), _vector(post_bias, dim, kind, "post_bias")
-    a.gain, a.bias = _vector(gain, dim, kind, "gain"), _vector(bias, dim, kind, "bias")
-    if r is not None:
-        a.r, a.r_row_stride = _matrix(r, rows, dim, kind, "r"), r.stride(0)
-    if coded:
-        a.codes, a.codes_row_stride = _matrix(h, rows, dim, torch.int8, "h"), h.stride(0)
-        a.scales = _vector(scales, rows, torch.float32, "scales")
+    none, width = (None, 0), (dim,)
+    device, stream = _current()
+    if gate is None:
+        at = none
+    elif gate.dim() == 1:
+        at = _vector(gate, width, kind, device, "gate"), 0
     else:
-        a.h, a.h_row_stride = _matrix(h, rows, dim, kind, "h"), h.stride(0)
-    a.post_norm, a.norm, a.alpha, a.eps = post_norm, norm, alpha, eps
-    rc = _lib.block_norm(ctypes.byref(a), _FLOATS[kind], rows, dim, _stream())
-    return rc, x if r is None else r, h, scales if coded else None
+        at = _matrix(gate, shape, kind, device, "gate")
+    out = _matrix(h, shape, torch.int8 if coded else kind, device, "h")
+    a = block_norm_args(*_matrix(x, shape, kind, device, "x"), *(none if z is None else _matrix(z, shape, kind, device, "z")), *at,
+                        _vector(post_gain, width, kind, device, "post_gain"), _vector(post_bias, width, kind, device, "post_bias"), _vector(gain, width, kind, device, "gain"),
+                        _vector(bias, width, kind, device, "bias"), *(none if r is None else _matrix(r, shape, kind, device, "r")), *(none if coded else out),
+                        *(out if coded else none), _vector(scales, (rows,), torch.float32, device, "scales"), post_norm, norm, alpha, eps)
+    rc = _lib.block_norm(ctypes.byref(a), _FLOATS[kind], rows, dim, stream)
+    return rc, x if r is None else r, h, scales

@@ -4,8 +4,30 @@ import ctypes
 import pytest
 import torch
 
-from tests.test_serve_binding import OnGpu, stand_in  # noqa: F401
+from tests.test_serve_binding import Library
+from tests.test_serve_binding import OnGpu as OnAGpu
 from tests.test_serve_refusals import BAD_CACHES, BAD_SEQS, cache, seqs
+
+
+class OnGpu(OnAGpu):
+    """A host tensor that says on which GPU it is."""
+
+    def __init__(self, *shape, dtype=torch.int32, device=0):
+        super().__init__(*shape, dtype=dtype)
+        self.device_index = device
+
+    def get_device(self):
+        return self.device_index
+
+
+@pytest.fixture
+def stand_in(monkeypatch):
+    from paper_2404_16109_amd import binding
+    lib = Library()
+    monkeypatch.setattr(binding, "_lib", lib)
+    monkeypatch.setattr(binding, "_current", lambda: (0, 0))
+    return binding, lib
+
 
 P = 1 << 20   # an address that is never read: every call below is refused, or has nothing to do
 
@@ -76,7 +98,7 @@ def test_sizes_of_the_workspace(zk):
         assert zk.i8_matmul_workspace_bytes(rows, n, k) >= 2 * 4 * rows * n
 
 
-def test_python_takes_the_gpus_tensors_only(stand_in):  # noqa: F811
+def test_python_takes_the_gpus_tensors_only(stand_in):
     zk, lib = stand_in
     i8, f32, bf16 = torch.int8, torch.float32, torch.bfloat16
     x, v = OnGpu(3, 32, dtype=bf16), OnGpu(32, dtype=bf16)
@@ -85,6 +107,7 @@ def test_python_takes_the_gpus_tensors_only(stand_in):  # noqa: F811
     assert zk.block_norm(x, x, gain=v, gate=v, **out)[0] == 0
     for kw in (dict(z=host), dict(gain=torch.zeros(32, dtype=bf16)), dict(gate=host), dict(r=host), dict(h=torch.zeros(3, 32, dtype=i8)),
                dict(scales=torch.zeros(3)), dict(gain=OnGpu(32, dtype=f32)), dict(z=OnGpu(3, 31, dtype=bf16)), dict(bias=OnGpu(31, dtype=bf16)),
+               dict(x=OnGpu(3, 32, dtype=bf16, device=1)), dict(r=OnGpu(3, 32, dtype=bf16, device=1)), dict(gain=OnGpu(32, dtype=bf16, device=1)),
                dict(gate=OnGpu(2, 32, dtype=bf16)), dict(post_gain=OnGpu(33, dtype=bf16)), dict(scales=OnGpu(2, dtype=f32))):
         with pytest.raises(AssertionError):
             zk.block_norm(**dict(dict(x=x, z=x, **out), **kw))
@@ -98,7 +121,7 @@ def test_python_takes_the_gpus_tensors_only(stand_in):  # noqa: F811
     assert zk.i8_matmul(codes, w, scales, ws, out=y, ws=space)[0] == 0
     for kw in (dict(x=torch.zeros(3, 32, dtype=i8)), dict(w=torch.zeros(8, 32, dtype=i8)), dict(x_scales=torch.zeros(3)), dict(w_scales=OnGpu(7, dtype=f32)),
                dict(out=torch.zeros(3, 8, dtype=bf16)), dict(out=OnGpu(3, 9, dtype=bf16)), dict(ws=torch.zeros(4096, dtype=torch.uint8)),
-               dict(w=OnGpu(8, 16, dtype=i8))):
+               dict(w=OnGpu(8, 16, dtype=i8)), dict(w=OnGpu(8, 32, dtype=i8, device=1)), dict(ws=OnGpu(4096, dtype=torch.uint8, device=1))):
         with pytest.raises(AssertionError):
             zk.i8_matmul(**dict(dict(x=codes, w=w, x_scales=scales, w_scales=ws, out=y, ws=space), **kw))
     assert set(lib.calls) == {"block_norm", "i8_quantise", "i8_matmul"}
@@ -134,14 +157,15 @@ def test_prefix_arguments(zk):
         assert zk.kvcache_attention_prefix_workspace_bytes(*a) == 0
 
 
-def test_prefix_from_python(stand_in):  # noqa: F811
+def test_prefix_from_python(stand_in):
     zk, lib = stand_in
     i8, bf16 = torch.int8, torch.bfloat16
     c = zk.KvCache(OnGpu(4, 2, 16, 32, dtype=i8), OnGpu(4, 2, 32, 16, dtype=i8), OnGpu(4, 2, dtype=i8), OnGpu(4, 2, dtype=i8))
     kw = dict(cache=c, q=OnGpu(3, 2, 32, dtype=bf16), cu=OnGpu(2), lens=OnGpu(1), table=OnGpu(1, 4), prefix=OnGpu(2), max_new=3, max_len=60, scale=0.1,
               out=OnGpu(3, 2, 32, dtype=bf16), lse=OnGpu(3, 2, dtype=torch.float32), ws=OnGpu(4096, dtype=torch.uint8))
     assert zk.kvcache_attention_prefix(**kw)[0] == 0
-    for bad in (dict(prefix=torch.zeros(2, dtype=torch.int32)), dict(prefix=OnGpu(2, dtype=torch.int64)), dict(prefix=OnGpu(1, 2)),
+    for bad in (dict(prefix=OnGpu(2, device=1)), dict(q=OnGpu(3, 2, 32, dtype=bf16, device=1)), dict(ws=OnGpu(4096, dtype=torch.uint8, device=1)),
+                dict(prefix=torch.zeros(2, dtype=torch.int32)), dict(prefix=OnGpu(2, dtype=torch.int64)), dict(prefix=OnGpu(1, 2)),
                 dict(q=torch.zeros(3, 2, 32, dtype=bf16)), dict(out=torch.zeros(3, 2, 32, dtype=bf16)), dict(lse=torch.zeros(3, 2)),
                 dict(ws=torch.zeros(4096, dtype=torch.uint8)), dict(fault=torch.zeros(1, dtype=torch.int32)), dict(table=torch.zeros(1, 4, dtype=torch.int32))):
         with pytest.raises(AssertionError):
