@@ -81,7 +81,8 @@ __device__ __forceinline__ v8h widen(uint32_t lo, uint32_t hi) {
     return r.v;
 }
 
-__device__ __forceinline__ v2h round2(float a, float b) { return v2h{(_Float16)a, (_Float16)b}; }
+typedef float v2f __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ v2h round2(float a, float b) { return __builtin_convertvector((v2f{a, b}), v2h); }  // one instruction
 
 // Maximum / sum over the lane rows (16 lanes each) 2i, 2i + 1, and over the halves of a wavefront.
 __device__ __forceinline__ float max_rows(float x) {
@@ -504,7 +505,9 @@ struct ManyShared {
 // Rows r0 .. r0 + 127 of the R of a sequence and head over tiles [first, end); the lane's row sees keys (low, pos], every row of the
 // wavefront those up to pos_first, some row of the workgroup pos_last, none those before seen_from.  What comes out are outputs, or
 // sums, r's at part0 + r.
-template <int DT, typename A>
+// RAW: where all keys of a tile are seen, scores stay products until their exponential is taken, which is one step less for each and rounds
+// elsewhere.
+template <int DT, bool RAW, typename A>
 __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& sh, const SeqView& v, uint32_t b, uint32_t h, uint32_t R, uint32_t r0,
                                             const Tiles& tiles, int32_t pos, int32_t pos_first, int32_t pos_last, uint32_t seen_from, bool parts,
                                             size_t part0, float* sums, float2* sums_ml) {
@@ -611,9 +614,9 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         const char* vb = kb + L::k_bytes;
         const int32_t base = (int32_t)(t * kTile);
         v16f s[2];
-        float vback[2];
+        float vback[2], by[2], plus[2];
         float top = -kInf;
-        const bool whole = base + (int32_t)kTile - 1 <= pos_first && base > (a.window ? pos_last - (int32_t)a.window : -1);
+        const bool whole = (!RAW || a.scale > 0.0f) && base + (int32_t)kTile - 1 <= pos_first && base > (a.window ? pos_last - (int32_t)a.window : -1);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             s[st] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -624,15 +627,23 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
             const float ke = exps[buf][0][2 * st + half], ve = exps[buf][1][2 * st + half];
             const float mul = qmul * exp2_of(ke);
             vback[st] = back_of(ve);
-            s[st] = s[st] * mul + ve;
+            by[st] = mul;  // a score is s * by + plus
+            plus[st] = ve;
+            if (!RAW || !whole) {
+                s[st] = s[st] * mul + ve;
+                by[st] = 1.0f;
+                plus[st] = 0.0f;
+            }
             if (!whole) {
                 const int32_t key0 = base + 32 * st + 16 * (int32_t)half;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (key0 + e > pos || key0 + e <= low) s[st][e] = -kInf;
             }
+            float most = -kInf;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[st][e]);
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[st][e]);
+            top = fmaxf(top, RAW ? __builtin_fmaf(most, by[st], plus[st]) : most);
         }
         top = max_halves(top) - kHead;
         if (__ballot(top > m)) {
@@ -647,9 +658,11 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             float sum = 0.0f;
+            const float less = plus[st] - from;
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const float x0 = exp2_of(s[st][e] - from), x1 = exp2_of(s[st][e + 1] - from);
+                const float x0 = exp2_of(RAW ? __builtin_fmaf(s[st][e], by[st], less) : s[st][e] - from);
+                const float x1 = exp2_of(RAW ? __builtin_fmaf(s[st][e + 1], by[st], less) : s[st][e + 1] - from);
                 sum += x0 + x1;
                 const v2h two = round2(x0, x1);
                 p[st][e >> 3][e & 7] = two[0];
@@ -715,7 +728,7 @@ __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& s
     }
     const uint32_t r = r0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
     const int32_t pos = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
-    attend_rows<DT>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
+    attend_rows<DT, false>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
                     (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most, a.parts, a.parts_ml);
 }
 template <int DT>

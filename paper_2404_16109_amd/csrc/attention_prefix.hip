@@ -58,19 +58,19 @@ __device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, Fro
         for (int32_t t = from; t <= to; ++t) sh.place[t - tok0] = v.len - v.rows + (t - v.row0);
     }
     __syncthreads();
-    if ((int32_t)tid <= tok1 - tok0) {
+    if ((int32_t)tid <= tok1 - tok0 && sh.place[tid] >= 0) {  // rows without a token get no answer: what they come to does not matter
         atomicMin(&sh.least, sh.place[tid]);
         atomicMax(&sh.most, sh.place[tid]);
     }
     __syncthreads();
-    const int32_t least = sh.least, most = sh.most;
+    const int32_t least = (int32_t)uniform((uint32_t)sh.least), most = (int32_t)uniform((uint32_t)sh.most);
     if (most < 0) return;  // no row of theirs sees a key, and k_prefix_join does not ask
     Tiles tiles = {split * a.front_each, (split + 1) * a.front_each};
     if (tiles.end > a.front_tiles) tiles.end = a.front_tiles;
     const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
     const int32_t pos = r < R ? sh.place[r / a.group - (uint32_t)tok0] : -1;
     const SeqView all = {0, (int32_t)a.s.rows, 0, true};
-    attend_rows<DT>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+    attend_rows<DT, true>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
 }
 
 // RT: tiles of 16 rows that a sequence and head has, 0: many rows.  Workgroups of one head lie eight apart where there are eight heads, so
