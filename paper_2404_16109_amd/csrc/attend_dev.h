@@ -518,18 +518,23 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, i32 = lane & 31;
     const uint32_t d = a.cache.head_dim, T = 1u << a.page_log, H = a.cache.kv_heads, r = r0 + wave * 32 + i32;
 
-    v8h qf[2 * DT];
-    float qmul;
+    // The first tile's pages, then q, then the tile: loads come back in order.
+    uint32_t page[4], my_page = 0;  // later tiles' pages are looked up two tiles ahead
+    const bool any = tiles.first < tiles.end;
+    if (any) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = page_of(a, b, tiles.first * kTile + 16 * i);
+        my_page = page_of(a, b, (tiles.first + 1) * kTile + 16 * (tid & 3));
+    }
+    v4u raw[2 * DT];
     {
         const size_t at = row_at(a, v, h, r < R ? r : 0, a.qrow, a.qhead);
-        v4u raw[2 * DT];
 #pragma unroll
         for (int k = 0; k < 2 * DT; ++k) {
             v4u one[1] = {v4u{0, 0, 0, 0}};
             if (16u * k < d) load_raw<8>(a.q, at + 16 * k + 8 * half, a.wide, one);
             raw[k] = one[0];
         }
-        qmul = scale_row<16 * DT>(raw, a.dtype, a.scale, qf, LargestOf2());
     }
     const int32_t low = a.window ? pos - (int32_t)a.window : -1;  // keys in (low, pos] are seen
 
@@ -548,7 +553,7 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
     // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens.  As they are loaded: a float made of one at once waits for
     // all of the tile, which cost 2 us a tile where the codes come from HBM.
     int my_exp = 0;
-    bool my_none = false;
+    bool my_none = false, missing = false;  // whether a page is none, and whether such a one was needed
     auto fetch = [&](uint32_t t, const uint32_t(&page)[4]) {
         const uint32_t head = T * d;
 #pragma unroll
@@ -558,22 +563,18 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
             kr[i] = *(const v4u*)(a.cache.k + ((size_t)kp * H + h) * head + k_slot * d + k_at[i]);
             vr[i] = *(const v4u*)(a.cache.v + ((size_t)vp * H + h) * head + v_at[i] + v_slot);
         }
-        if (tid < 8) {
-            const uint32_t it = page[tid & 3];
-            const bool none = it >= a.cache.pages;
-            const uint32_t key = t * kTile + 16 * (tid & 3);
-            if (none && (int32_t)key <= pos_last && key + 16 > seen_from) report(a.s, ZK_FAULT_PAGE);
-            const size_t at = (size_t)page_or_0(a, it) * H + h;
-            my_exp = tid < 4 ? a.cache.k_exp[at] : a.cache.v_exp[at];
-            my_none = none;
-        }
+        // all threads, like eight of them: a branch here would part the products before it from those behind
+        const uint32_t it = page[tid & 3], key = t * kTile + 16 * (tid & 3);
+        my_none = it >= a.cache.pages;
+        missing |= my_none && t < tiles.end && (int32_t)key <= pos_last && key + 16 > seen_from;
+        my_exp = (tid & 4 ? a.cache.v_exp : a.cache.k_exp)[(size_t)page_or_0(a, it) * H + h];
     };
     auto stage = [&](uint32_t buf) {
         char* kb = lds + buf * L::bytes;
         char* vb = kb + L::k_bytes;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            if (!attend_piece_kept<DT>(tid, kBlock, i)) continue;
+            if (128 * DT % kBlock != 0 && !attend_piece_kept<DT>(tid, kBlock, i)) continue;
             const AttendPiece p = attend_piece<DT>(tid, kBlock, i);
             const uint32_t x = p.slot & 31;
             // the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
@@ -592,22 +593,16 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[c] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     float m = -kInf, l = 0.0f;
-    // pages are looked up two tiles ahead, by threads 0..3
-    uint32_t my_page = 0;
-    if (tiles.first < tiles.end) {
-        uint32_t page[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = page_of(a, b, tiles.first * kTile + 16 * i);
-        if (tid < 4) my_page = page_of(a, b, (tiles.first + 1) * kTile + 16 * tid);
-        fetch(tiles.first, page);
-    }
+    if (any) fetch(tiles.first, page);
+    v8h qf[2 * DT];
+    const float qmul = scale_row<16 * DT>(raw, a.dtype, a.scale, qf, LargestOf2());
     for (uint32_t t = tiles.first; t < tiles.end; ++t) {
         const uint32_t buf = (t - tiles.first) & 1;
         stage(buf);
         if (tid < 4) pages[buf][tid] = my_page;
         __syncthreads();
-        if (t + 1 < tiles.end) {
-            if (tid < 4) my_page = page_of(a, b, (t + 2) * kTile + 16 * tid);
+        if (!RAW && t + 1 < tiles.end) {
+            my_page = page_of(a, b, (t + 2) * kTile + 16 * (tid & 3));
             fetch(t + 1, pages[buf]);
         }
         const char* kb = lds + buf * L::bytes;
@@ -624,6 +619,12 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
 #pragma unroll
             for (int k = 0; k < 2 * DT; ++k)
                 s[st] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h*)(krow + 32 * k), qf[k], s[st], 0, 0, 0);
+            if (RAW && st == 0) {
+                // The next tile is asked for among the products of this one; behind the last one some page is read, and not kept.
+                // (431 -> 417 us for 2450 rows behind 32768 tokens; short row tiles lose by it, 82 -> 88 us for a prompt of 2048.)
+                my_page = page_of(a, b, (t + 2) * kTile + 16 * (tid & 3));
+                fetch(t + 1, pages[buf]);
+            }
             const float ke = exps[buf][0][2 * st + half], ve = exps[buf][1][2 * st + half];
             const float mul = qmul * exp2_of(ke);
             vback[st] = back_of(ve);
@@ -680,6 +681,7 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
                     o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h*)(vrow + 64 * st + 16 * k), p[st][k], o[c], 0, 0, 0);
         }
     }
+    if (missing) report(a.s, ZK_FAULT_PAGE);
     l = add_halves(l);
     if (r >= R) return;
     if (parts) {

@@ -120,16 +120,32 @@ __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
         m = ml.x;
         l = ml.y;
     }
-    const float top = wave_max(m), ref = top == -kInf ? 0.0f : top, weight = exp2_of(m - ref);
-    l = wave_add(l * weight);
-    const uint32_t quads = d >> 2, ways = 64 / quads, way = lane / quads, c = lane - way * quads;
+    const uint32_t quads = d >> 2, ways = 64 / quads, way = lane / quads, c = lane - way * quads, parts = front + own;
     v4f sum = {0, 0, 0, 0};
-    for (uint32_t p0 = 0; p0 < front + own; p0 += ways) {
-        const uint32_t p = p0 + way;
-        const float w = bits_float((uint32_t)__shfl((int)float_bits(weight), (int)(p & 63)));
-        if (way < ways && p < front + own) {
-            const size_t at = p < front ? front0 + (size_t)p * R : own0 + (size_t)(p - front) * a.rows_most;
-            sum += ((const v4f*)(p < front ? a.front_parts : a.parts))[at * quads + c] * w;
+    float weight = 0.0f, ref = 0.0f;
+    // eight parts of a lane are on their way at once, the first beside the maxima
+    for (uint32_t p0 = 0; p0 < parts || p0 == 0; p0 += 8 * ways) {
+        v4f x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t p = p0 + u * ways + way;
+            x[u] = v4f{0, 0, 0, 0};
+            if (way < ways && p < parts) {
+                const size_t at = p < front ? front0 + (size_t)p * R : own0 + (size_t)(p - front) * a.rows_most;
+                x[u] = ((const v4f*)(p < front ? a.front_parts : a.parts))[at * quads + c];
+            }
+        }
+        if (p0 == 0) {
+            const float top = wave_max(m);
+            ref = top == -kInf ? 0.0f : top;
+            weight = exp2_of(m - ref);
+            l = wave_add(l * weight);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t p = p0 + u * ways + way;
+            const float w = bits_float((uint32_t)__shfl((int)float_bits(weight), (int)(p & 63)));
+            if (way < ways && p < parts) sum += x[u] * w;
         }
     }
     for (uint32_t w = 1; w < ways; ++w) {
