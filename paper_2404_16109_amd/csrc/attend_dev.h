@@ -199,8 +199,8 @@ __device__ __forceinline__ Tiles tiles_of(const Args& a, const SeqView& v, int32
 // The same for the 128 rows from r0 on that a workgroup of k_attend_many has.
 static const uint32_t kRows = 128;
 template <typename A>
-__device__ __forceinline__ Tiles tiles_of_rows(const A& a, const SeqView& v, uint32_t r0) {
-    const uint32_t R = (uint32_t)v.rows * a.group, last = r0 + kRows < R ? r0 + kRows - 1 : R - 1;
+__device__ __forceinline__ Tiles tiles_of_rows(const A& a, const SeqView& v, uint32_t r0, uint32_t rows = kRows) {
+    const uint32_t R = (uint32_t)v.rows * a.group, last = r0 + rows < R ? r0 + rows - 1 : R - 1;
     return tiles_of(a, v, (int32_t)(r0 / a.group), (int32_t)(last / a.group));
 }
 
@@ -502,17 +502,18 @@ struct ManyShared {
     float exps[2][2][4];    // [buffer][K, V][16 tokens]
     uint32_t pages[2][4];   // of the next tile
 };
-// Rows r0 .. r0 + 127 of the R of a sequence and head over tiles [first, end); the lane's row sees keys (low, pos], every row of the
+// Rows from r0 on, 32 to each of WV wavefronts, of the R of a sequence and head over tiles [first, end); the lane's row sees keys (low, pos], every row of the
 // wavefront those up to pos_first, some row of the workgroup pos_last, none those before seen_from.  What comes out are outputs, or
 // sums, r's at part0 + r.
 // RAW: where all keys of a tile are seen, scores stay products until their exponential is taken, which is one step less for each and rounds
 // elsewhere.
-template <int DT, bool RAW, typename A>
+template <int DT, bool RAW, int WV, typename A>
 __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& sh, const SeqView& v, uint32_t b, uint32_t h, uint32_t R, uint32_t r0,
                                             const Tiles& tiles, int32_t pos, int32_t pos_first, int32_t pos_last, uint32_t seen_from, bool parts,
                                             size_t part0, float* sums, float2* sums_ml) {
     using L = ManyLds<DT>;
-    constexpr int PIECES = (DT + 1) / 2;  // of 16 codes, for a thread, of a tile's K and of its V
+    constexpr uint32_t threads = 64 * WV;
+    constexpr int PIECES = (128 * DT + threads - 1) / threads;  // of 16 codes, for a thread, of a tile's K and of its V
     float(&exps)[2][2][4] = sh.exps;
     uint32_t(&pages)[2][4] = sh.pages;
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, i32 = lane & 31;
@@ -543,7 +544,7 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
     uint32_t k_run[PIECES], k_at[PIECES], v_run[PIECES], v_at[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const AttendPiece p = attend_piece<DT>(tid, kBlock, i);
+        const AttendPiece p = attend_piece<DT>(tid, threads, i);
         k_run[i] = p.slot >> 4;
         k_at[i] = (p.slot & 15) * d + (16 * p.c < d ? 16 * p.c : 0);
         v_run[i] = p.run;
@@ -574,8 +575,8 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         char* vb = kb + L::k_bytes;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            if (128 * DT % kBlock != 0 && !attend_piece_kept<DT>(tid, kBlock, i)) continue;
-            const AttendPiece p = attend_piece<DT>(tid, kBlock, i);
+            if (128 * DT % threads != 0 && !attend_piece_kept<DT>(tid, threads, i)) continue;
+            const AttendPiece p = attend_piece<DT>(tid, threads, i);
             const uint32_t x = p.slot & 31;
             // the product's rows 8 b + 4 h + j come out in lane half h, as tokens 16 h + 4 b + j
             const uint32_t row = (p.slot & 32) + 8 * ((x >> 2) & 3) + 4 * (x >> 4) + (x & 3);
@@ -589,6 +590,7 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         if (tid < 8) exps[buf][tid >> 2][tid & 3] = my_none ? (tid < 4 ? __builtin_nanf("") : 0.0f) : exponent_value(my_exp);
     };
 
+    const bool idle = r0 + uniform(wave) * 32 >= R;
     v16f o[DT];
 #pragma unroll
     for (int c = 0; c < DT; ++c) o[c] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -601,6 +603,11 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         stage(buf);
         if (tid < 4) pages[buf][tid] = my_page;
         __syncthreads();
+        if (WV > 4 && idle) {  // no rows: it brings its share of the next tile
+            my_page = page_of(a, b, (t + 2) * kTile + 16 * (tid & 3));
+            fetch(t + 1, pages[buf]);
+            continue;
+        }
         if (!RAW && t + 1 < tiles.end) {
             my_page = page_of(a, b, (t + 2) * kTile + 16 * (tid & 3));
             fetch(t + 1, pages[buf]);
@@ -708,20 +715,21 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
     if (a.lse && half == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(m == -kInf ? 0.0f : m, l);
 }
 
-// A workgroup's rows of a sequence and head, `tile` 128s before its last.
-template <int DT, typename A>
+// A workgroup's rows of a sequence and head, `tile` times as many before its last.
+template <int DT, int WV, typename A>
 __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& sh, uint32_t tile, uint32_t split, uint32_t h, uint32_t b) {
+    constexpr uint32_t rows = 32 * WV;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
         if (tile == 0 && a.splits == 1 && !A::joined) not_a_number(a, b, h);
         return;
     }
-    const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + kRows - 1) / kRows;
+    const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + rows - 1) / rows;
     if (tile >= row_tiles) return;
-    const uint32_t r0 = (row_tiles - 1 - tile) * kRows;  // the rows that see most first, of all heads
-    const uint32_t r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
+    const uint32_t r0 = (row_tiles - 1 - tile) * rows;  // the rows that see most first, of all heads
+    const uint32_t r_last = r0 + rows - 1 < R - 1 ? r0 + rows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
-    Tiles tiles = tiles_of_rows(a, v, r0);
+    Tiles tiles = tiles_of_rows(a, v, r0, rows);
     if (a.splits > 1) {
         const uint32_t each = part_of(a, tiles);
         tiles.first += split * each;
@@ -730,7 +738,7 @@ __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& s
     }
     const uint32_t r = r0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
     const int32_t pos = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
-    attend_rows<DT, false>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
+    attend_rows<DT, false, WV>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
                     (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most, a.parts, a.parts_ml);
 }
 template <int DT>
@@ -738,7 +746,7 @@ __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ ManyShared sh;
     const uint32_t b = blockIdx.z / a.splits;
-    attend_many<DT>(a, lds, sh, blockIdx.y, blockIdx.z - b * a.splits, blockIdx.x, b);
+    attend_many<DT, 4>(a, lds, sh, blockIdx.y, blockIdx.z - b * a.splits, blockIdx.x, b);
 }
 
 }  // namespace

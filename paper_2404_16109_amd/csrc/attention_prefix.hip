@@ -2,14 +2,17 @@
 //
 // The keys of a row are those of the prefix and its sequence's own.  With (M, l, o) the maximum, the sum of weights and
 // the weighted values over a part of the keys, parts join by e^(M - max M): so the prefix is one part, or several, for ALL rows
-// of the batch at once, and its codes are read once for 128 rows where they would be read once for each sequence.
-// k_prefix: workgroups of two kinds in one launch.  The first have 128 rows of the whole batch over tiles of the prefix, which the
+// of the batch at once, and its codes are read once for so many rows where they would be read once for each sequence.
+// k_prefix: workgroups of two kinds in one launch.  The first have 128 or 256 rows of the whole batch over tiles of the prefix, which the
 // vector ALU bounds; those behind have a sequence's own keys, which latency bounds, and run beside them.  k_prefix_join adds up.
 #include "attend_dev.h"
 
 namespace zkmi {
 namespace {
 
+// Wavefronts to a workgroup, 32 rows to each: of many rows eight share what a tile costs to bring, where their sums fit the registers; with
+// four there is room on a CU for a workgroup of the other kind beside, which few rows need more.
+bool eight_waves(uint64_t rows, uint32_t head_dim) { return rows >= 1024 && head_dim <= 128; }
 static const uint32_t kMostParts = 32;  // of the prefix, and of a sequence's own keys
 
 struct PrefixArgs : Args {
@@ -17,7 +20,7 @@ struct PrefixArgs : Args {
     const int32_t* front;      // the prefix's pages
     uint32_t front_tokens;     // a multiple of the page
     uint32_t front_tiles;      // whole tiles of it; what is left is read with each sequence's own
-    uint32_t front_splits, front_each, front_groups;
+    uint32_t front_splits, front_each, front_groups, row_tile;
     float* front_parts;        // [head][split][row of the batch]
     float2* front_ml;
 };
@@ -36,22 +39,24 @@ __device__ __forceinline__ Tiles tiles_of(const PrefixArgs& a, const SeqView& v,
     return Tiles{a.front_tiles, end > a.front_tiles ? end : a.front_tiles};
 }
 
+template <int WV>
 struct FrontShared {
     ManyShared many;
-    int32_t place[kRows], least, most;  // positions of the tokens that the rows belong to, -1: nobody's
+    int32_t place[32 * WV], least, most;  // positions of the tokens that the rows belong to, -1: nobody's
 };
-// A part of the prefix's whole tiles for 128 rows of the batch.
-template <int DT>
-__device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, FrontShared& sh, uint32_t h, uint32_t tile, uint32_t split) {
-    const uint32_t r0 = tile * kRows, tid = threadIdx.x, R = a.s.rows * a.group, r_last = r0 + kRows - 1 < R - 1 ? r0 + kRows - 1 : R - 1;
+// A part of the prefix's whole tiles for a workgroup's rows of the batch.
+template <int DT, int WV>
+__device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, FrontShared<WV>& sh, uint32_t h, uint32_t tile, uint32_t split) {
+    constexpr uint32_t rows = 32 * WV, threads = 64 * WV;
+    const uint32_t r0 = tile * rows, tid = threadIdx.x, R = a.s.rows * a.group, r_last = r0 + rows - 1 < R - 1 ? r0 + rows - 1 : R - 1;
     const int32_t tok0 = (int32_t)(r0 / a.group), tok1 = (int32_t)(r_last / a.group);
-    if (tid < kRows) sh.place[tid] = -1;
+    if (tid < rows) sh.place[tid] = -1;
     if (tid == 0) {
         sh.least = 0x7fffffff;
         sh.most = -1;
     }
     __syncthreads();
-    for (uint32_t b = tid; b < a.s.seqs; b += kBlock) {
+    for (uint32_t b = tid; b < a.s.seqs; b += threads) {
         const SeqView v = seq_view(a.s, b, a.page_log);
         if (!v.ok || v.rows == 0) continue;
         const int32_t from = v.row0 > tok0 ? v.row0 : tok0, to = v.row0 + v.rows - 1 < tok1 ? v.row0 + v.rows - 1 : tok1;
@@ -70,29 +75,29 @@ __device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, Fro
     const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
     const int32_t pos = r < R ? sh.place[r / a.group - (uint32_t)tok0] : -1;
     const SeqView all = {0, (int32_t)a.s.rows, 0, true};
-    attend_rows<DT, true>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+    attend_rows<DT, true, WV>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
 }
 
 // RT: tiles of 16 rows that a sequence and head has, 0: many rows.  Workgroups of one head lie eight apart where there are eight heads, so
 // that an XCD reads the prefix of its own.
-template <int DT, int RT>
-__global__ __launch_bounds__(kBlock, DT <= 4 && RT < 2 ? 2 : 1) void k_prefix(PrefixArgs a) {
+template <int DT, int RT, int WV>
+__global__ __launch_bounds__(64 * WV, WV == 8 || (DT <= 4 && RT < 2) ? 2 : 1) void k_prefix(PrefixArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ FrontShared sh;
+    __shared__ FrontShared<WV> sh;
     const uint32_t H = a.cache.kv_heads;
     if (blockIdx.x < a.front_groups) {
         const uint32_t id = blockIdx.x, h = id % H, at = id / H, tile = at / a.front_splits;
-        return attend_front<DT>(a, lds, sh, h, tile, at - tile * a.front_splits);
+        return attend_front<DT, WV>(a, lds, sh, h, tile, at - tile * a.front_splits);
     }
     uint32_t id = blockIdx.x - a.front_groups;
     const uint32_t h = id % H;
     id /= H;
     const uint32_t split = id % a.splits;
     id /= a.splits;
-    if constexpr (RT != 0) attend_few<(DT + 1) / 2, RT, 4>(a, (float*)lds, split, h, id);
+    if constexpr (RT != 0) attend_few<(DT + 1) / 2, RT, WV>(a, (float*)lds, split, h, id);
     else {
-        const uint32_t tiles = (a.rows_most + kRows - 1) / kRows, b = id / tiles;
-        attend_many<DT>(a, lds, sh.many, id - b * tiles, split, h, b);
+        const uint32_t tiles = (a.rows_most + a.row_tile - 1) / a.row_tile, b = id / tiles;
+        attend_many<DT, WV>(a, lds, sh.many, id - b * tiles, split, h, b);
     }
 }
 
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
     const uint32_t R = a.s.rows * a.group, row = (uint32_t)v.row0 * a.group + r;
     // parts of the prefix come first; a row that sees no key has none
     const uint32_t front = pos >= 0 ? a.front_splits : 0;
-    const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / kRows * kRows);
+    const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / a.row_tile * a.row_tile, a.row_tile);
     const uint32_t each = part_of(a, tiles), n = tiles.end - tiles.first, own = pos >= 0 && n ? (n + each - 1) / each : 0;
     const size_t front0 = (size_t)h * a.front_splits * R + row, own0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
     float m = -kInf, l = 0.0f;
@@ -170,11 +175,12 @@ bool few_rows(uint64_t rows) { return rows <= 32; }
 
 // How a call is spread.  rows: of the batch and a head; most: of a sequence and a head.
 struct Plan {
-    uint32_t front_tiles, front_splits, front_each, splits, each;
+    uint32_t row_tile, front_tiles, front_splits, front_each, splits, each;
 };
 Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uint32_t head_dim, uint32_t prefix, uint32_t max_len) {
     Plan p = {};
     p.front_tiles = prefix / kTile;
+    p.row_tile = eight_waves(rows, head_dim) ? 256 : 128;
     const auto share = [](uint64_t groups, uint32_t tiles, uint32_t& splits, uint32_t& each) {
         uint64_t n = groups >= kWorkgroups / 2 ? 1 : div_up(kWorkgroups, groups);
         if (n > div_up(tiles, 4)) n = div_up(tiles, 4);
@@ -183,15 +189,15 @@ Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uin
         splits = (uint32_t)div_up(tiles, each);
     };
     if (p.front_tiles) {
-        // Time of the prefix by the number of parts, in us: as many rounds of a workgroup to each CU as it takes, 0.41 a tile for each 32
-        // dimensions and 1 to begin with, and the parts' way to memory and back at 4 TB/s.  Measured for 320 rows and 8 heads of 128
-        // behind 8192 tokens, whole call: 4 parts 71 us, 8 46, 10 42, 16 44, 32 56; for 2450 rows behind 32768 1 part 875, 3 446, 10 439, 32 566.
-        const uint64_t groups = kv_heads * div_up(rows, kRows);
+        // Time of the prefix by the number of parts, in us: as many rounds of a workgroup to each CU as it takes, 0.41 (0.57 with eight
+        // wavefronts) a tile for each 32 dimensions and 1 to begin with, and the parts' way to memory and back at 4 TB/s.  Measured for 320
+        // rows and 8 heads of 128 behind 8192 tokens, whole call: 4 parts 71 us, 8 46, 10 42, 16 44, 32 56.
+        const uint64_t groups = kv_heads * div_up(rows, p.row_tile);
         double best = 0.0;
         for (uint32_t n = 1; n <= kMostParts && n <= p.front_tiles; ++n) {
             const uint32_t each = (uint32_t)div_up(p.front_tiles, n);
             if (div_up(p.front_tiles, each) != n) continue;
-            const double us = (double)div_up(groups * n, kWorkgroups / 2) * (0.41 * each * (double)div_up(head_dim, 32) + 1.0) +
+            const double us = (double)div_up(groups * n, kWorkgroups / 2) * ((p.row_tile == 256 ? 0.57 : 0.41) * each * (double)div_up(head_dim, 32) + 1.0) +
                               (double)(kv_heads * rows * head_dim) * n * 8.0 / 4e6;
             if (n == 1 || us < best) {
                 best = us;
@@ -201,7 +207,7 @@ Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uin
         }
     }
     const uint32_t own = max_len > p.front_tiles * kTile ? (uint32_t)div_up(max_len - p.front_tiles * kTile, kTile) : 1;
-    share((uint64_t)seqs * kv_heads * (few_rows(most) ? 1 : div_up(most, kRows)), own, p.splits, p.each);
+    share((uint64_t)seqs * kv_heads * (few_rows(most) ? 1 : div_up(most, p.row_tile)), own, p.splits, p.each);
     return p;
 }
 
@@ -219,23 +225,29 @@ size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint64_t most, uint32_t s
     return cv.used();
 }
 
-template <int DT, int RT>
+template <int DT, int RT, int WV>
 int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
     size_t lds = 2 * (size_t)ManyLds<DT>::bytes;
     if constexpr (RT != 0) {
-        const size_t few = FewLds<(DT + 1) / 2, RT, 4>::bytes(a.rows_most);
+        const size_t few = FewLds<(DT + 1) / 2, RT, WV>::bytes(a.rows_most);
         if (few > lds) lds = few;
     }
-    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_prefix<DT, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_prefix<DT, RT>), dim3((unsigned)(a.front_groups + own)), dim3(kBlock), lds, s, a);
+    if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_prefix<DT, RT, WV>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((k_prefix<DT, RT, WV>), dim3((unsigned)(a.front_groups + own)), dim3(64 * WV), lds, s, a);
     hipLaunchKernelGGL(k_prefix_join, dim3((unsigned)div_up((size_t)a.rows_most * a.cache.kv_heads, kBlock / 64), a.s.seqs), dim3(kBlock), 0, s, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
+template <int DT, int WV>
+int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
+    if (a.rows_most <= 16) return launch<DT, 1, WV>(a, own, s);
+    return a.few ? launch<DT, 2, WV>(a, own, s) : launch<DT, 0, WV>(a, own, s);
+}
 template <int DT>
 int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
-    if (a.rows_most <= 16) return launch<DT, 1>(a, own, s);
-    return a.few ? launch<DT, 2>(a, own, s) : launch<DT, 0>(a, own, s);
+    if constexpr (DT <= 4)
+        if (a.row_tile == 256) return launch<DT, 8>(a, own, s);
+    return launch<DT, 4>(a, own, s);
 }
 
 // Rows of a sequence and head at most.
@@ -287,12 +299,13 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     a.front_tokens = prefix_pages * cache->page_tokens;
     const Plan p = plan_of(seqs->seqs, rows, most, cache->kv_heads, cache->head_dim, a.front_tokens, seqs->max_len);
     a.front_tiles = p.front_tiles;
+    a.row_tile = p.row_tile;
     a.front_splits = p.front_splits;
     a.front_each = p.front_each;
     a.splits = p.splits;
     a.each = p.each;
-    const uint64_t front = (uint64_t)cache->kv_heads * p.front_splits * div_up(rows, kRows);
-    const uint64_t own = (uint64_t)seqs->seqs * cache->kv_heads * p.splits * (a.few ? 1 : div_up(most, kRows));
+    const uint64_t front = (uint64_t)cache->kv_heads * p.front_splits * div_up(rows, p.row_tile);
+    const uint64_t own = (uint64_t)seqs->seqs * cache->kv_heads * p.splits * (a.few ? 1 : div_up(most, p.row_tile));
     if (front + own >= 0x80000000u) return ZK_E_BADARG;
     a.front_groups = (uint32_t)front;
     if (!ws) return ZK_E_BUFSZ;
