@@ -47,6 +47,15 @@ struct Place {
     __device__ __forceinline__ bool in(int i) const { return at(WIDE ? i / W * W : i) < dim; }
 };
 
+// Two elements of 16 bits, each rounded to nearest.
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ __forceinline__ uint32_t pair_bits(float a, float b) {
+    if constexpr (DT == ZK_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2b));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2h));
+}
+
 // A thread's elements of a row, as they lie in memory: asked for long before they are used.  Zeros behind the row's end.
 template <int DT, int E, bool WIDE>
 struct Raw {
@@ -72,6 +81,26 @@ struct Raw {
         else if constexpr (WIDE) return half_of<DT>(word[i >> 1], i & 1);
         else return half_of<DT>(word[i], 0);
     }
+    // f, rounded to the type
+    __device__ __forceinline__ void set(const float (&f)[E]) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if constexpr (!WIDE) word[i] = half_bits<DT>(as_it_is(f[i]));
+            else if (i & 1) word[i >> 1] = pair_bits<DT>(as_it_is(f[i - 1]), as_it_is(f[i]));
+        }
+    }
+    __device__ __forceinline__ void store(void* p, size_t row, const Place<DT, E, WIDE>& at) const {
+        typename Element<DT>::type* y = (typename Element<DT>::type*)p + row;
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int v = 0; v < E / W; ++v)
+                if (at.in(v * W)) *(v4u*)(y + at.at(v * W)) = v4u{word[4 * v], word[4 * v + 1], word[4 * v + 2], word[4 * v + 3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (at.in(i)) y[at.at(i)] = (typename Element<DT>::type)word[i];
+        }
+    }
 };
 
 template <int DT>
@@ -80,26 +109,18 @@ __device__ __forceinline__ float rounded(float f) {
     return half_of<DT>(half_bits<DT>(as_it_is(f)), 0);
 }
 
-// Stores a thread's elements; f is rounded to the type.
-template <int DT, int E, bool WIDE>
-__device__ __forceinline__ void store_row(void* p, size_t row, const Place<DT, E, WIDE>& at, const float (&f)[E]) {
-    constexpr int W = Element<DT>::wide;
-    typename Element<DT>::type* y = (typename Element<DT>::type*)p + row;
+// A thread's elements of a row of 32 bits.
+template <int E, bool WIDE>
+__device__ __forceinline__ void store_floats(void* p, size_t row, const Place<ZK_F32, E, WIDE>& at, const float (&f)[E]) {
+    float* y = (float*)p + row;
     if constexpr (WIDE) {
 #pragma unroll
-        for (int v = 0; v < E / W; ++v) {
-            v4u q;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if constexpr (DT == ZK_F32) q[k] = float_bits(f[v * W + k]);
-                else q[k] = (uint32_t)half_bits<DT>(as_it_is(f[v * W + 2 * k])) | ((uint32_t)half_bits<DT>(as_it_is(f[v * W + 2 * k + 1])) << 16);
-            }
-            if (at.in(v * W)) *(v4u*)(y + at.at(v * W)) = q;
-        }
+        for (int v = 0; v < E; v += 4)
+            if (at.in(v)) *(v4f*)(y + at.at(v)) = v4f{f[v], f[v + 1], f[v + 2], f[v + 3]};
     } else {
 #pragma unroll
         for (int i = 0; i < E; ++i)
-            if (at.in(i)) store_one<DT>((void*)y, at.at(i), as_it_is(f[i]));
+            if (at.in(i)) y[at.at(i)] = as_it_is(f[i]);
     }
 }
 
@@ -186,7 +207,7 @@ __device__ __forceinline__ bool code_scale(uint32_t most, float& scale, float& i
     inv = some ? 127.0f / amax : 0.0f;
     return some;
 }
-__device__ __forceinline__ uint32_t code_of(float h, float inv) { return float_bits(h * inv + 12582912.0f) & 0xffu; }
+__device__ __forceinline__ uint32_t code_of(float h, float inv) { return float_bits(h * inv + 12582912.0f); }  // the lowest byte
 
 __device__ __forceinline__ uint32_t all_most(uint32_t most, Scratch& s, uint32_t waves) {
     most = wave_max(most);
@@ -198,6 +219,14 @@ __device__ __forceinline__ uint32_t all_most(uint32_t most, Scratch& s, uint32_t
     return most;
 }
 
+// Behind the row's end everything is zero and stays so (gains and biases are zeros there), but for what a mean was taken off.
+template <int DT, int E, bool WIDE>
+__device__ __forceinline__ void zeros_behind(float (&v)[E], int kind, const Place<DT, E, WIDE>& at) {
+    if (kind != ZK_NORM_LAYER) return;
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = at.in(i) ? v[i] : 0.0f;
+}
+
 template <int DT, int E, bool WIDE>
 __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* scale_at, const Place<DT, E, WIDE>& at, const float (&h)[E], Scratch& s,
                                             uint32_t waves) {
@@ -205,7 +234,7 @@ __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* sc
     uint32_t most = 0;  // the bits of |h|: infinities and NaN are above every number
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        const uint32_t bits = at.in(i) ? float_bits(h[i]) & 0x7fffffffu : 0u;
+        const uint32_t bits = float_bits(h[i]) & 0x7fffffffu;  // zeros behind the row's end
         most = bits > most ? bits : most;
     }
     float scale, inv;
@@ -218,9 +247,10 @@ __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* sc
             uint32_t q[W / 4];
 #pragma unroll
             for (int k = 0; k < W / 4; ++k) {
-                const float* f = h + v * W + 4 * k;
-                const uint32_t c = code_of(f[0], inv) | (code_of(f[1], inv) << 8) | (code_of(f[2], inv) << 16) | (code_of(f[3], inv) << 24);
-                q[k] = some ? c : 0u;
+                const float* f = h + v * W + 4 * k;  // the lowest byte of each
+                const uint32_t lo = __builtin_amdgcn_perm(code_of(f[1], inv), code_of(f[0], inv), 0x0c0c0400u);
+                const uint32_t hi = __builtin_amdgcn_perm(code_of(f[3], inv), code_of(f[2], inv), 0x0c0c0400u);
+                q[k] = some ? __builtin_amdgcn_perm(hi, lo, 0x05040100u) : 0u;
             }
             if (at.in(v * W)) {
                 if constexpr (W == 8) *(uint2*)(y + at.at(v * W)) = make_uint2(q[0], q[1]);
@@ -254,6 +284,7 @@ __global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : 4) void k_block_norm(Nor
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = z.get(i);
         normalise(v, a.post_norm, a.eps, post_gain, a.post_gain != nullptr, post_bias, a.post_bias != nullptr, at, s, turn, waves);
+        zeros_behind(v, a.post_norm, at);
         if (a.gate) {
 #pragma unroll
             for (int i = 0; i < E; ++i) v[i] = gate.get(i) * v[i];
@@ -266,13 +297,32 @@ __global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : 4) void k_block_norm(Nor
     }
     if (a.gain) gain.load(a.gain, 0, at);
     if (a.bias) bias.load(a.bias, 0, at);
-    if (a.r) store_row<DT, E, WIDE>(a.r, row * a.r_row_stride, at, v);
-    if (!a.h && !a.codes) return;
+    if constexpr (DT == ZK_F32) {
+        if (a.r) store_floats(a.r, row * a.r_row_stride, at, v);
+        if (!a.h && !a.codes) return;
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = at.in(i) ? rounded<DT>(v[i]) : 0.0f;  // what the next block sees is what is stored
+        for (int i = 0; i < E; ++i) v[i] = WIDE || at.in(i) ? v[i] : 0.0f;
+    } else {
+        Raw<DT, E, WIDE> out;
+        out.set(v);
+        if (a.r) out.store(a.r, row * a.r_row_stride, at);
+        if (!a.h && !a.codes) return;
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = out.get(i);  // what the next block sees is what is stored
+    }
     normalise(v, a.norm, a.eps, gain, a.gain != nullptr, bias, a.bias != nullptr, at, s, turn, waves);
-    if (a.h) store_row<DT, E, WIDE>(a.h, row * a.h_row_stride, at, v);
-    else store_codes<DT, E, WIDE>(a.codes, row * a.codes_row_stride, a.scales + row, at, v, s, waves);
+    if (a.h) {
+        if constexpr (DT == ZK_F32) {
+            store_floats(a.h, row * a.h_row_stride, at, v);
+        } else {
+            Raw<DT, E, WIDE> out;
+            out.set(v);
+            out.store(a.h, row * a.h_row_stride, at);
+        }
+        return;
+    }
+    zeros_behind(v, a.norm, at);
+    store_codes<DT, E, WIDE>(a.codes, row * a.codes_row_stride, a.scales + row, at, v, s, waves);
 }
 
 // Rows of more than 16 elements to a thread (or of eight that no 16-byte load takes): the row lies in LDS, in 32 bits, each element
