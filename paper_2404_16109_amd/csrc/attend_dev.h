@@ -551,8 +551,8 @@ __device__ __forceinline__ void attend_rows(const A& a, char* lds, ManyShared& s
         v_at[i] = (p.dim < d ? p.dim : 0) << a.page_log;
     }
     v4u kr[PIECES], vr[PIECES];
-    // threads 0..7: K's and V's exponents of the tile's runs of 16 tokens.  As they are loaded: a float made of one at once waits for
-    // all of the tile, which cost 2 us a tile where the codes come from HBM.
+    // K's and V's exponents of the tile's runs of 16 tokens, as they are loaded: a float made of one at once would wait for all of
+    // the tile.
     int my_exp = 0;
     bool my_none = false, missing = false;  // whether a page is none, and whether such a one was needed
     auto fetch = [&](uint32_t t, const uint32_t(&page)[4]) {

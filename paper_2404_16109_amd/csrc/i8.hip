@@ -3,11 +3,14 @@
 // Sums are exact in 32 bits (|x w| <= 2^14, k < 2^17), in whatever order: parts of k may be added up anywhere.
 //
 // Few rows (k_few: up to 32): the weights are read once, straight into registers, and bound the call.  A workgroup has 16 to 64
-// outputs, its eight wavefronts share k in steps of 128, so that every row of weights is read in whole lines.
+// outputs, its eight wavefronts share k in steps of 128, so that every row of weights is read in whole lines.  Measured, weights from HBM:
+// one row by 13824 x 5120 16.8 us, 4.2 TB/s; 32 rows 20 us.  One row by 5120 x 5120 8.4 us where the bytes alone take 5.1: latency.
 // Many rows (k_tiles): tiles of x and w come through LDS, put there by loads that pass no register, a step of 128 ahead; 16-byte
 // pieces lie in LDS at piece ^ ((row / 2) & 7): rows of 128 bytes lie in one half of the banks or the other, so 16 neighbouring rows
-// answer from all of them.  Where there are fewer tiles
-// than the chip holds, workgroups share k and k_join adds up.
+// answer from all of them (no conflict is counted).  One barrier a step, before its last quarter, the loads among that quarter's
+// products.  Measured: 8192 x 13824 x 5120 522 us, 2.2 P operations/s, 8192^3 2.4 (a library's product 2.2 and 2.4): the matrix cores are
+// 61% busy at 1.84 GHz, to which the card's power brings the clock.  Stages of 64 of k, four or five ahead, took 645 us where this took 584.
+// Where there are fewer tiles than the chip holds, workgroups share k and k_join adds up (333 rows by 5120 x 13824: 33 us and 6).
 #include "serve_dev.h"
 
 #pragma clang fp contract(off)

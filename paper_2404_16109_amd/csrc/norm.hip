@@ -6,6 +6,10 @@
 // call.  Statistics are sums in 64 bits (at the rate of 32 here) and are rounded to 32 bits once; from there on every step is one
 // operation of 32 bits with its own rounding, so nothing is contracted below: the codes are the integers of a proof, and whoever
 // computes the definition gets the same ones, but for a statistic that lies within some 2^-53 of the middle between two numbers.
+//
+// Measured: 8192 rows of 5120 bf16 through two norms and a gate to codes (378 MB) 84.8 us, 4.45 TB/s where a copy reaches 5.1, the vector
+// ALU 61% busy; 777 rows of 4097 floats, which no 16-byte load takes, 14.7 us, 3.5 TB/s; codes of 8192 x 13824 f16 58 us, 5.8 TB/s (part of it
+// stays in the last cache); one row 3.6 us in a graph, latency, where a launch of nothing is 1.7.
 #include "serve_dev.h"
 
 #pragma clang fp contract(off)
