@@ -611,7 +611,8 @@ int kvcache_attention(const kvcache_i8* cache, const void* q, size_t q_row_strid
  * ever (lens[b] counts both; the table's entries for the prefix are not used; rows may lie inside the prefix).  Without a window.  The result is that of
  * kvcache_attention with those pages in every row of the table, but for roundings: the prefix is read once for all
  * rows, not once for each sequence.  A page of the prefix outside the cache makes NaN of the rows that see a key in it
- * (ZK_FAULT_PAGE).  prefix_pages may be 0.  rows * (q_heads / kv_heads) < 2^31 - 256.  ws: device (always needed),
+ * (ZK_FAULT_PAGE).  prefix_pages may be 0.  rows * (q_heads / kv_heads) < 2^31 - 256;
+ * max_new * q_heads < 2^26; seqs * kv_heads, times the parts that a long context is shared out in (at most 32), below some 2^22.  ws: device (always needed),
  * kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_pages * page_tokens, max_len). */
 size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
                                                 uint32_t head_dim, uint32_t prefix_tokens, uint32_t max_len);
@@ -693,7 +694,7 @@ int i8_quantise(int8_t* codes, size_t codes_row_stride, float* scales, const voi
  * and each output.  The sum is exact in 32 bits; then a float of 32 bits, and each product
  * is rounded to 32 bits, the last to y's type (ZK_F32, ZK_F16, ZK_BF16).
  * ZK_I32: y are the sums themselves, int32_t, and the scales are not read (may be NULL): the Y that matmul_sumcheck_prove_i16
- * proves for the same integers in 16 bits.  k is a multiple of 16, 16 <= k <= I8_MAX_K; n, rows <= 2^24; x and
+ * proves for the same integers in 16 bits.  k is a multiple of 16, 16 <= k <= I8_MAX_K; n, rows <= 2^24, rows * n < 2^38; x and
  * w 16-byte aligned, x_row_stride a multiple of 16 and at most 2^23; y rows x n, any row stride of at least n.
  * ws: device, i8_matmul_workspace_bytes(rows, n, k) (0 where there are outputs enough: ws may be NULL then). */
 size_t i8_matmul_workspace_bytes(size_t rows, size_t n, size_t k);

@@ -281,7 +281,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
     const uint64_t rows = (uint64_t)seqs->rows * group, most = rows_most(seqs->rows, seqs->max_new, group);
-    if (rows >= 0x7fffff00u || div_up(most * cache->kv_heads, kBlock / 64) >= 0x80000000u) return ZK_E_BADARG;
+    if (rows >= 0x7fffff00u || most * cache->kv_heads >= (uint64_t)1 << 26) return ZK_E_BADARG;
     PrefixArgs a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -310,7 +310,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     a.each = p.each;
     const uint64_t front = (uint64_t)cache->kv_heads * p.front_splits * div_up(rows, p.row_tile);
     const uint64_t own = (uint64_t)seqs->seqs * cache->kv_heads * p.splits * (a.few ? 1 : div_up(most, p.row_tile));
-    if (front + own >= 0x80000000u) return ZK_E_BADARG;
+    if (front + own >= (uint64_t)1 << 23) return ZK_E_BADARG;  // a launch holds fewer than 2^32 threads
     a.front_groups = (uint32_t)front;
     if (!ws) return ZK_E_BUFSZ;
     Carver cv(ws, ws_bytes);

@@ -399,6 +399,7 @@ Plan plan_tiles(size_t rows, size_t n, uint32_t steps) {
     for (int t = kShort; t <= kLarge; ++t) {
         const Shape& s = kShapes[t];
         const uint64_t groups = div_up(rows, s.rows) * div_up(n, s.outs);
+        if (t < kLarge && groups >= (uint64_t)1 << 22) continue;  // a launch holds fewer than 2^32 threads
         for (uint32_t splits = 1; splits <= 16 && splits * 4 <= (steps < 4 ? 4 : steps); ++splits) {
             if (splits > 1 && groups * (splits - 1) >= 256 * s.slots) break;
             Plan p = {};
@@ -470,6 +471,7 @@ extern "C" int i8_matmul(void* y, size_t y_row_stride, int y_dtype, const int8_t
     if (rows > 1 && (x_row_stride < k || x_row_stride % 16 || x_row_stride > (size_t)1 << 23 || y_row_stride < n)) return ZK_E_BADARG;
     if (y_dtype != ZK_I32 && (!x_scales || !w_scales || !aligned(x_scales, 4) || !aligned(w_scales, 4))) return ZK_E_BADARG;
     const Plan p = plan_of(rows, n, k);
+    if (p.tile != kFew && (uint64_t)div_up(rows, kShapes[p.tile].rows) * div_up(n, kShapes[p.tile].outs) >= (uint64_t)1 << 23) return ZK_E_BADARG;
     Args a = {};
     a.y = y;
     a.yrow = y_row_stride;

@@ -25,7 +25,12 @@ struct NormArgs {
     block_norm_args a;
     int dtype;
     uint32_t dim;
+    size_t rows;
 };
+// A launch holds fewer than 2^32 threads in a direction: workgroups of many rows lie in two.
+static const size_t kRowsAcross = (size_t)1 << 20;
+dim3 grid_of(size_t rows) { return rows <= kRowsAcross ? dim3((unsigned)rows) : dim3((unsigned)kRowsAcross, (unsigned)div_up(rows, kRowsAcross)); }
+__device__ __forceinline__ size_t row_of_block() { return (size_t)blockIdx.y * kRowsAcross + blockIdx.x; }
 
 // An element of 16 or 32 bits, as it lies in memory.
 template <int DT>
@@ -273,7 +278,8 @@ template <int DT, int E, bool WIDE>
 __global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : 4) void k_block_norm(NormArgs n) {
     __shared__ Scratch s;
     const block_norm_args& a = n.a;
-    const size_t row = blockIdx.x;
+    const size_t row = row_of_block();
+    if (row >= n.rows) return;
     const uint32_t waves = blockDim.x >> 6;
     const Place<DT, E, WIDE> at = {threadIdx.x, blockDim.x, n.dim};
     Raw<DT, E, WIDE> z, x, gate, gain, bias, post_gain, post_bias;
@@ -336,7 +342,8 @@ __global__ __launch_bounds__(kMostThreads) void k_block_norm_long(NormArgs n) {
     extern __shared__ __attribute__((aligned(16))) float line[];
     __shared__ Scratch s;
     const block_norm_args& a = n.a;
-    const size_t row = blockIdx.x;
+    const size_t row = row_of_block();
+    if (row >= n.rows) return;
     const uint32_t waves = kMostThreads / 64, dim = n.dim;
     int turn = 0;
     auto statistics = [&](int kind) {
@@ -395,9 +402,11 @@ __global__ __launch_bounds__(kMostThreads) void k_block_norm_long(NormArgs n) {
 }
 
 template <int DT, int E, bool WIDE>
-__global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
+__global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim,
+                                                         size_t rows) {
     __shared__ Scratch s;
-    const size_t row = blockIdx.x;
+    const size_t row = row_of_block();
+    if (row >= rows) return;
     const Place<DT, E, WIDE> at = {threadIdx.x, blockDim.x, dim};
     Raw<DT, E, WIDE> raw;
     raw.load(x, row * x_row, at);
@@ -409,9 +418,11 @@ __global__ __launch_bounds__(kMostThreads) void k_quantise(int8_t* codes, size_t
 
 // Rows longer than the registers of a workgroup: read twice, the second time from a cache that holds them.
 template <int DT>
-__global__ __launch_bounds__(kMostThreads) void k_quantise_long(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim) {
+__global__ __launch_bounds__(kMostThreads) void k_quantise_long(int8_t* codes, size_t codes_row, float* scales, const void* x, size_t x_row, uint32_t dim,
+                                                              size_t rows) {
     __shared__ Scratch s;
-    const size_t row = blockIdx.x, from = row * x_row;
+    const size_t row = row_of_block(), from = row * x_row;
+    if (row >= rows) return;
     uint32_t most = 0;
     for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) {
         const uint32_t bits = float_bits(load_one<DT>(x, from + i)) & 0x7fffffffu;
@@ -443,26 +454,26 @@ Spread spread_of(int dtype, uint32_t dim, size_t rows, bool wide) {
 }
 
 template <int DT, int E, bool WIDE>
-int launch_norm(const NormArgs& n, unsigned rows, uint32_t threads, hipStream_t s) {
-    hipLaunchKernelGGL((k_block_norm<DT, E, WIDE>), dim3(rows), dim3(threads), 0, s, n);
+int launch_norm(const NormArgs& n, uint32_t threads, hipStream_t s) {
+    hipLaunchKernelGGL((k_block_norm<DT, E, WIDE>), grid_of(n.rows), dim3(threads), 0, s, n);
     return ZK_OK;
 }
 template <int DT>
-int launch_long(const NormArgs& n, unsigned rows, hipStream_t s) {
+int launch_long(const NormArgs& n, hipStream_t s) {
     const size_t lds = n.dim * sizeof(float);
     if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_block_norm_long<DT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((k_block_norm_long<DT>), dim3(rows), dim3(kMostThreads), lds, s, n);
+    hipLaunchKernelGGL((k_block_norm_long<DT>), grid_of(n.rows), dim3(kMostThreads), lds, s, n);
     return ZK_OK;
 }
 template <int DT, bool WIDE>
-int spread_norm(const NormArgs& n, unsigned rows, hipStream_t s) {
-    const Spread p = spread_of(DT, n.dim, rows, WIDE);
+int spread_norm(const NormArgs& n, hipStream_t s) {
+    const Spread p = spread_of(DT, n.dim, n.rows, WIDE);
     if constexpr (DT == ZK_F32)
-        if (p.each == 4) return launch_norm<DT, 4, WIDE>(n, rows, p.threads, s);
-    if (p.each == 8) return launch_norm<DT, 8, WIDE>(n, rows, p.threads, s);
+        if (p.each == 4) return launch_norm<DT, 4, WIDE>(n, p.threads, s);
+    if (p.each == 8) return launch_norm<DT, 8, WIDE>(n, p.threads, s);
     if constexpr (WIDE)
-        if (p.each == 16) return launch_norm<DT, 16, WIDE>(n, rows, p.threads, s);
-    return launch_long<DT>(n, rows, s);
+        if (p.each == 16) return launch_norm<DT, 16, WIDE>(n, p.threads, s);
+    return launch_long<DT>(n, s);
 }
 
 struct QuantiseArgs {
@@ -472,25 +483,26 @@ struct QuantiseArgs {
     const void* x;
     size_t x_row;
     uint32_t dim;
+    size_t rows;
 };
 template <int DT, int E, bool WIDE>
-void launch_quantise(const QuantiseArgs& q, unsigned rows, uint32_t threads, hipStream_t s) {
-    hipLaunchKernelGGL((k_quantise<DT, E, WIDE>), dim3(rows), dim3(threads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim);
+void launch_quantise(const QuantiseArgs& q, uint32_t threads, hipStream_t s) {
+    hipLaunchKernelGGL((k_quantise<DT, E, WIDE>), grid_of(q.rows), dim3(threads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim, q.rows);
 }
 template <int DT, bool WIDE>
-void spread_quantise(const QuantiseArgs& q, unsigned rows, hipStream_t s) {
-    const Spread p = spread_of(DT, q.dim, rows, WIDE);
+void spread_quantise(const QuantiseArgs& q, hipStream_t s) {
+    const Spread p = spread_of(DT, q.dim, q.rows, WIDE);
     if constexpr (DT == ZK_F32)
-        if (p.each == 4) return launch_quantise<DT, 4, WIDE>(q, rows, p.threads, s);
-    if (p.each == 8) return launch_quantise<DT, 8, WIDE>(q, rows, p.threads, s);
-    if (p.each == 16) return launch_quantise<DT, 16, WIDE>(q, rows, p.threads, s);
-    launch_quantise<DT, 32, WIDE>(q, rows, p.threads, s);
+        if (p.each == 4) return launch_quantise<DT, 4, WIDE>(q, p.threads, s);
+    if (p.each == 8) return launch_quantise<DT, 8, WIDE>(q, p.threads, s);
+    if (p.each == 16) return launch_quantise<DT, 16, WIDE>(q, p.threads, s);
+    launch_quantise<DT, 32, WIDE>(q, p.threads, s);
 }
 template <int DT>
-void quantise_of(const QuantiseArgs& q, bool wide, unsigned rows, hipStream_t s) {
-    if (q.dim > kMostDim) hipLaunchKernelGGL((k_quantise_long<DT>), dim3(rows), dim3(kMostThreads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim);
-    else if (wide) spread_quantise<DT, true>(q, rows, s);
-    else spread_quantise<DT, false>(q, rows, s);
+void quantise_of(const QuantiseArgs& q, bool wide, hipStream_t s) {
+    if (q.dim > kMostDim) hipLaunchKernelGGL((k_quantise_long<DT>), grid_of(q.rows), dim3(kMostThreads), 0, s, q.codes, q.codes_row, q.scales, q.x, q.x_row, q.dim, q.rows);
+    else if (wide) spread_quantise<DT, true>(q, s);
+    else spread_quantise<DT, false>(q, s);
 }
 
 // A matrix of the call: rows far enough apart, aligned to its elements.  With one row the stride says nothing.
@@ -528,12 +540,11 @@ extern "C" int block_norm(const block_norm_args* args, int dtype, size_t rows, s
                    {a.gain, 0}, {a.bias, 0}, {a.post_gain, 0}, {a.post_bias, 0}};
     for (const auto& t : tensors) wide = wide && (!t.p || (aligned(t.p, 16) && (rows == 1 || t.stride % run == 0)));
     wide = wide && (!a.codes || (aligned(a.codes, run) && (rows == 1 || a.codes_row_stride % run == 0)));
-    const NormArgs n = {a, dtype, (uint32_t)dim};
+    const NormArgs n = {a, dtype, (uint32_t)dim, rows};
     hipStream_t s = as_stream(stream);
-    const unsigned r = (unsigned)rows;
-    if (dtype == ZK_F32) ZK_TRY((wide ? spread_norm<ZK_F32, true>(n, r, s) : spread_norm<ZK_F32, false>(n, r, s)));
-    else if (dtype == ZK_F16) ZK_TRY((wide ? spread_norm<ZK_F16, true>(n, r, s) : spread_norm<ZK_F16, false>(n, r, s)));
-    else ZK_TRY((wide ? spread_norm<ZK_BF16, true>(n, r, s) : spread_norm<ZK_BF16, false>(n, r, s)));
+    if (dtype == ZK_F32) ZK_TRY((wide ? spread_norm<ZK_F32, true>(n, s) : spread_norm<ZK_F32, false>(n, s)));
+    else if (dtype == ZK_F16) ZK_TRY((wide ? spread_norm<ZK_F16, true>(n, s) : spread_norm<ZK_F16, false>(n, s)));
+    else ZK_TRY((wide ? spread_norm<ZK_BF16, true>(n, s) : spread_norm<ZK_BF16, false>(n, s)));
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -546,11 +557,11 @@ extern "C" int i8_quantise(int8_t* codes, size_t codes_row_stride, float* scales
     if (!codes || !scales || !x || !aligned(scales, 4) || !rows_ok(x, x_row_stride, bytes, rows, k) || !rows_ok(codes, codes_row_stride, 1, rows, k))
         return ZK_E_BADARG;
     const bool wide = k % run == 0 && aligned(x, 16) && aligned(codes, run) && (rows == 1 || (x_row_stride % run == 0 && codes_row_stride % run == 0));
-    const QuantiseArgs q = {codes, codes_row_stride, scales, x, x_row_stride, (uint32_t)k};
+    const QuantiseArgs q = {codes, codes_row_stride, scales, x, x_row_stride, (uint32_t)k, rows};
     hipStream_t s = as_stream(stream);
-    if (dtype == ZK_F32) quantise_of<ZK_F32>(q, wide, (unsigned)rows, s);
-    else if (dtype == ZK_F16) quantise_of<ZK_F16>(q, wide, (unsigned)rows, s);
-    else quantise_of<ZK_BF16>(q, wide, (unsigned)rows, s);
+    if (dtype == ZK_F32) quantise_of<ZK_F32>(q, wide, s);
+    else if (dtype == ZK_F16) quantise_of<ZK_F16>(q, wide, s);
+    else quantise_of<ZK_BF16>(q, wide, s);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }

@@ -242,6 +242,21 @@ def test_many_short_rows():
     check(x, z, kw, True)
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    """Rows times the threads of each are more than 2^32."""
+    rows = (1 << 26) + 1234567
+    x = torch.zeros(rows, 1, dtype=F16, device="cuda")
+    x[::3] = -2.0
+    x[-1] = 5.0
+    rc, codes, scales = zk.i8_quantise(x)
+    assert rc == zk.ZK_OK
+    assert (codes[::3][:-1] == -127).all() and codes[-1] == 127 and not codes[1::3][:-1].any() and not codes[2::3][:-1].any()
+    step = torch.tensor(2.0, dtype=F32) / torch.tensor(127.0, dtype=F32)
+    assert (scales[::3][:-1] == step.item()).all() and scales[-1] == (torch.tensor(5.0) / torch.tensor(127.0)).item()
+    rc, r, h, _ = zk.block_norm(x, x, norm=zk.ZK_NORM_NONE)
+    assert rc == zk.ZK_OK and torch.equal(r, x + x) and torch.equal(h, r)
+
+
 def test_other_stream_and_graph():
     x, z, kw = case(40, 520, BF16, zk.ZK_NORM_RMS, zk.ZK_NORM_LAYER, 2, True)
     xg, zg, kwg = x.cuda(), z.cuda(), on_gpu(kw)

@@ -95,6 +95,30 @@ def test_spread_as_the_caller_says(new, lens):
         check(cache, q, cu, lens, table, 30, 0.125, max_new=max_new, max_len=max_len)
 
 
+@pytest.mark.parametrize("new,lens", [([1, 1], [300, 260]), ([40, 2], [300, 260])])
+@pytest.mark.parametrize("scale", [0.0, -0.1, 0.3, 1e-30])
+def test_scales_of_scores(new, lens, scale):
+    cache, q, cu, table, _ = make(zk, new, lens, 4, 2, 64, 16, BF16, 31)
+    check(cache, q, cu, lens, table, 12, scale)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [300, 300]])
+def test_large_and_small_queries(new):
+    lens, d = [700, 600], 128
+    for size, kexp, scale in ((1e30, -40, 1e-25), (1e-30, 20, 1e20), (300.0, -6, 0.3)):
+        cache, q, cu, table, gen = make(zk, new, lens, 4, 1, d, 32, BF16, 5)
+        cache.k_exp.fill_(kexp)
+        check(cache, (q.float() * size).to(BF16), cu, lens, table, 9, scale)
+
+
+def test_many_rows_of_each_width():
+    """Eight wavefronts to a workgroup up to 128 dimensions, four beyond; some without rows."""
+    for d in (16, 64, 80, 128, 160):
+        new, lens = [150, 3, 120, 1, 40], [500, 400, 330, 329, 400]
+        cache, q, cu, table, _ = make(zk, new, lens, 8, 2, d, 32, F16, d)
+        check(cache, q, cu, lens, table, 9, d ** -0.5)
+
+
 def test_many_sequences():
     """More than a workgroup's threads, ragged, some without rows or tokens of their own."""
     g = torch.Generator().manual_seed(4)

@@ -57,7 +57,7 @@ def test_matmul(zk):
     for kw in (dict(y=None), dict(x=None), dict(w=None), dict(x_scales=None), dict(w_scales=None), dict(dtype=3), dict(dtype=5), dict(dtype=-1), dict(n=0),
                dict(k=0), dict(k=8), dict(k=24), dict(k=131072, xs=131072), dict(n=(1 << 24) + 1, ys=1 << 25), dict(rows=(1 << 24) + 1), dict(x=P + 8),
                dict(w=P + 8), dict(y=P + 1), dict(dtype=0, y=P + 2), dict(dtype=4, y=P + 2), dict(xs=240), dict(xs=264), dict(xs=(1 << 23) + 16), dict(ys=63),
-               dict(x_scales=P + 2), dict(w_scales=P + 1)):
+               dict(x_scales=P + 2), dict(w_scales=P + 1), dict(rows=1 << 24, n=1 << 24, ys=1 << 24)):
         assert matmul(zk, **kw) == zk.ZK_E_BADARG, kw
     assert matmul(zk, rows=0, x=None, y=None, w=None) == zk.ZK_OK
     need = zk.i8_matmul_workspace_bytes(2, 64, 65536)
@@ -146,7 +146,7 @@ def test_prefix_sequences(zk, bad):
 def test_prefix_arguments(zk):
     for kw in (dict(q=None), dict(out=None), dict(dtype=0), dict(dtype=3), dict(dtype=4), dict(heads=0), dict(heads=7), dict(heads=131072),
                dict(scale=float("inf")), dict(scale=float("nan")), dict(q=P + 1), dict(out=P + 1), dict(lse=P + 2), dict(front=None), dict(front=P + 2),
-               dict(pages=1 << 25), dict(s=seqs(zk, rows=(1 << 31) - 1, max_new=1))):
+               dict(pages=1 << 25), dict(s=seqs(zk, rows=1 << 24, max_new=1 << 24)), dict(c=cache(zk, kv_heads=1024), heads=1024, s=seqs(zk, seqs=65535, rows=65535, max_new=1)), dict(s=seqs(zk, rows=(1 << 31) - 1, max_new=1))):
         assert prefix(zk, **kw) == zk.ZK_E_BADARG, kw
     assert prefix(zk, s=seqs(zk, rows=0), q=None) == zk.ZK_OK and prefix(zk, s=seqs(zk, seqs=0), q=None) == zk.ZK_OK
     need = zk.kvcache_attention_prefix_workspace_bytes(2, 5, 3, 8, 2, 128, 128, 100)
