@@ -152,6 +152,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(Args a) {
 typedef __attribute__((address_space(3))) void lds_void;
 #define kOutside 0xfffffff0u  // an offset that no tile reaches: loads from there give zeros
 
+// What lanes of a wavefront have written to LDS is there for its other lanes, and what they have read may be written over.
+__device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A wavefront's outputs, from the accumulators (lane: one row, four outputs side by side) through LDS to memory (16 bytes of a row a lane).
 template <int Y, int MO, int NR>
 __device__ __forceinline__ void store_tile(const Args& a, const v16i (&acc)[MO][NR], int8_t* corner, const float* scales, uint32_t row0, uint32_t n0, void* to,
@@ -187,6 +193,7 @@ __device__ __forceinline__ void store_tile(const Args& a, const v16i (&acc)[MO][
                                                      (uint32_t)half_bits<Y>(f[2]) | ((uint32_t)half_bits<Y>(f[3]) << 16));
                     }
                 }
+            lanes_meet();
 #pragma unroll
             for (uint32_t q = 0; q < 32 * lanes / 64; ++q) {
                 const uint32_t in = q * (64 / lanes) + lane / lanes, row = row0 + 32 * r + in, c = lane % lanes, out = n0 + 32 * g + c * each;
@@ -204,6 +211,7 @@ __device__ __forceinline__ void store_tile(const Args& a, const v16i (&acc)[MO][
                     }
                 }
             }
+            lanes_meet();
         }
     }
 }
