@@ -1104,9 +1104,8 @@ def block_norm(x, z=None, *, norm=ZK_NORM_RMS, gain=None, bias=None, eps=1e-5, p
     if h is None:
         h = torch.empty(rows, dim, dtype=torch.int8 if quantise else kind, device=x.device)
     coded = h.dtype == torch.int8
-    if not coded:
-        scales = None
-    elif scales is None:
+    assert coded or not (quantise or scales is not None), "h: int8 for codes, which alone have scales"
+    if coded and scales is None:
         scales = torch.empty(rows, dtype=torch.float32, device=x.device)
     none, width = (None, 0), (dim,)
     device, stream = _current()
