@@ -376,7 +376,9 @@ void share_k(Plan& p, uint32_t steps, uint32_t splits) {
 
 // Up to 32 rows.  More outputs to a workgroup read x less often, fewer fill the chip.  Measured, us, weights from HBM, 16 / 32 / 64 outputs
 // to a workgroup: one row by 13824 x 5120 16.8 18.6 19.1, 16 rows 25.2 23.6 20.9, 32 rows 38 29 23.7; 32 rows by 5120 x 13824 46 33 48, and
-// with k shared by three 36 29 24.3; 32 rows by 5120 x 5120 16 11.9 16.4 (shared 15 13 12.3); 16 rows by 2000 x 8192 9.9 13.2.
+// with k shared by three 36 29 24.3; 32 rows by 5120 x 5120 16 11.9 16.4 (shared 15 13 12.3); 16 rows by 2000 x 8192 9.9 13.2.  Few outputs
+// share a long k, which costs a launch: one row by 941 x 21856 11.9 us in one part, 7.9 in four, by 339 x 10768 7.2 and 5.7 in a graph, but 7.4
+// and 9.3 called from Python, where launches count; by 500 x 4096 4.7 and 4.8.
 Plan plan_few(uint32_t rows, size_t n, uint32_t steps) {
     Plan p = {};
     p.tile = kFew;
@@ -384,7 +386,7 @@ Plan plan_few(uint32_t rows, size_t n, uint32_t steps) {
     p.nt = rows <= 4 ? 1 : n >= 64 * 200 || (shares && n >= 64 * 32) ? 4 : n >= 32 * 128 ? 2 : 1;
     p.groups = (uint32_t)div_up(n, 16 * p.nt);
     uint32_t splits = p.groups < 128 ? 256 / p.groups : 1;
-    const uint32_t most = p.nt == 4 || p.groups <= 32 ? steps / (2 * kWaves) : steps / (16 * kWaves);
+    const uint32_t most = p.nt == 4 || steps >= 96 ? steps / (2 * kWaves) : 1;
     if (splits > most) splits = most;
     share_k(p, steps, splits ? splits : 1);
     return p;
