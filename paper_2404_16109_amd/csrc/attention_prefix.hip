@@ -281,7 +281,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
     const uint64_t rows = (uint64_t)seqs->rows * group, most = rows_most(seqs->rows, seqs->max_new, group);
-    if (rows >= 0x7fffff00u || most * cache->kv_heads >= (uint64_t)1 << 26) return ZK_E_BADARG;
+    if (rows >= 0x7fffff00u || div_up(most * cache->kv_heads, kBlock / 64) >= (uint64_t)1 << 24) return ZK_E_BADARG;  // k_prefix_join: below 2^32 threads
     PrefixArgs a = {};
     a.cache = *cache;
     a.s = *seqs;

@@ -171,3 +171,13 @@ def test_prefix_from_python(stand_in):
         with pytest.raises(AssertionError):
             zk.kvcache_attention_prefix(**dict(kw, **bad))
     assert lib.calls == ["kvcache_attention_prefix"]
+
+
+def test_prefix_launches_are_below_2_to_the_32_threads(zk):
+    """A wavefront for each row of a sequence and head, four to a workgroup: the largest call that fits wants its workspace, the next is
+    refused before anything is enqueued."""
+    c = cache(zk, kv_heads=1)
+    for rows, want in (((1 << 26) - 4, zk.ZK_E_BUFSZ), ((1 << 26) - 3, zk.ZK_E_BADARG), ((1 << 26) - 2, zk.ZK_E_BADARG), ((1 << 26) - 1, zk.ZK_E_BADARG)):
+        assert prefix(zk, c=c, heads=1, s=seqs(zk, seqs=1, rows=rows, max_new=rows)) == want, rows
+    for rows, want in (((1 << 21) - 1, zk.ZK_E_BUFSZ), (1 << 21, zk.ZK_E_BADARG)):   # 32 heads
+        assert prefix(zk, c=c, heads=32, s=seqs(zk, seqs=1, rows=rows, max_new=rows)) == want, rows
