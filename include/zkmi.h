@@ -711,8 +711,9 @@ int i8_matmul(void* y, size_t y_row_stride, int y_dtype, const int8_t* x, size_t
  * post_*, nor gate), gains and gate are ones, biases zeros, r is not stored.  h goes to h, or as codes and scales (as i8_quantise of h
  * in 32 bits) to codes and scales, or nowhere.  r and h may be the tensors x and z themselves, with
  * their strides, either way round; no other output overlaps another tensor.
- * Means are taken in 64 bits; the mean itself and 1 / sqrt(...) are rounded to 32 bits, and every operation after them, in the
- * order written, once.  h is that of r as it is stored (rounded to the type).  1 <= dim <= 32768,
+ * A mean is the exact sum, rounded to 64 bits once (whatever the order in which it is taken), over dim; that of squares is of exact squares, of what
+ * v is off the mean in 64 bits.  + eps, sqrt and 1 / are steps of 64 bits; the mean itself and 1 / sqrt(...) are rounded to 32 bits, and every operation
+ * after them, in the order written, once.  h is that of r as it is stored (rounded to the type).  1 <= dim <= 32768,
  * rows < 2^31, eps > 0 (if there is a norm), alpha finite. */
 enum { ZK_NORM_NONE = 0, ZK_NORM_RMS = 1, ZK_NORM_LAYER = 2 };
 typedef struct {

@@ -5,7 +5,9 @@
 // One workgroup has a row and keeps it in registers: every tensor is read once and written once, which is what bounds the
 // call.  Statistics are sums in 64 bits (at the rate of 32 here) and are rounded to 32 bits once; from there on every step is one
 // operation of 32 bits with its own rounding, so nothing is contracted below: the codes are the integers of a proof, and whoever
-// computes the definition gets the same ones, but for a statistic that lies within some 2^-53 of the middle between two numbers.
+// computes the definition gets the same ones.  The definition's sums are exact; those here are rounded in an order that the spread of a row
+// over threads decides (its width, how many rows there are, addresses).  So a statistic is looked at before it is used: where roundings might
+// have moved it over the middle between two floats, its row is added up again without any (Ziv's test).
 //
 // Measured: 8192 rows of 5120 bf16 through two norms and a gate to codes (378 MB) 84.8 us, 4.45 TB/s where a copy reaches 5.1, the vector
 // ALU 61% busy; 777 rows of 4097 floats, which no 16-byte load takes, 14.7 us, 3.5 TB/s; codes of 8192 x 13824 f16 58 us, 5.8 TB/s (part of it
@@ -133,16 +135,23 @@ __device__ __forceinline__ void store_floats(void* p, size_t row, const Place<ZK
     }
 }
 
+static const uint32_t kDigits = 10, kCopies = 16;  // of 32 bits, from 2^-149 on: what 2^15 floats add up to; copies, so that few lanes meet
+
 // Over a workgroup, in every thread.  LDS slots are used in turn, so that one barrier is enough between two sums.
 struct Scratch {
-    double sums[2][kMostThreads / 64];
+    double sums[2][kMostThreads / 64], lost[2][kMostThreads / 64];
+    unsigned long long digits[kDigits][kCopies];
     uint32_t most[kMostThreads / 64];
 };
 template <int CTRL, int ROWS>
-__device__ __forceinline__ double add_from(double x) {
+__device__ __forceinline__ double partner(double x) {  // 0 where a lane has none
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
     const uint32_t lo = from_lane<CTRL, ROWS>(0u, (uint32_t)b), hi = from_lane<CTRL, ROWS>(0u, (uint32_t)(b >> 32));
-    return x + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_from(double x) {
+    return x + partner<CTRL, ROWS>(x);
 }
 __device__ __forceinline__ double wave_add64(double x) {  // the same moves as over_wave; in lane 63
     x = add_from<0x111, 0xf>(x);
@@ -162,11 +171,143 @@ __device__ __forceinline__ double all_add(double x, Scratch& s, int turn, uint32
     return sum;
 }
 
+// As uniform.
+__device__ __forceinline__ double one_for_all(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, ((uint64_t)uniform((uint32_t)(b >> 32)) << 32) | uniform((uint32_t)b));
+}
+
 // What a norm takes off and multiplies by.
 struct Stats {
     float mean, rstd;
 };
-__device__ __forceinline__ float rstd_of(double squares, double n, float eps) { return (float)(1.0 / sqrt(squares / n + (double)eps)); }
+__device__ __forceinline__ double rstd_of(double variance, float eps) { return 1.0 / sqrt(variance + (double)eps); }
+
+// A sum of squares and what its additions have lost (Knuth's two-sum): together exact to some 2^-90 of it, since nothing cancels.
+struct Squares {
+    double sum = 0.0, lost = 0.0;
+    __device__ __forceinline__ void add(double x) {
+        const double s = sum + x, b = s - sum;
+        lost += (sum - (s - b)) + (x - b);
+        sum = s;
+    }
+    __device__ __forceinline__ void add_of(double v, double mean) {  // (v - mean)^2: v - mean is d + less, d^2 is square and its own loss
+        const double d = v - mean, b = d - v, less = (v - (d - b)) - (mean + b), square = d * d;
+        add(square);
+        lost += __builtin_fma(d, d, -square) + 2.0 * d * less;
+    }
+    template <int CTRL, int ROWS>
+    __device__ __forceinline__ void add_partner() {
+        const double other = partner<CTRL, ROWS>(sum), also = partner<CTRL, ROWS>(lost);
+        add(other);
+        lost += also;
+    }
+};
+__device__ __forceinline__ double all_add(Squares x, Scratch& s, int turn, uint32_t waves) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    x.add_partner<0x111, 0xf>();
+    x.add_partner<0x112, 0xf>();
+    x.add_partner<0x114, 0xf>();
+    x.add_partner<0x118, 0xf>();
+    x.add_partner<0x142, 0xa>();
+    x.add_partner<0x143, 0xc>();
+    if (lane == 63) {
+        s.sums[turn & 1][wave] = x.sum;
+        s.lost[turn & 1][wave] = x.lost;
+    }
+    __syncthreads();
+    Squares all;
+#pragma unroll 1
+    for (uint32_t w = 0; w < waves; ++w) {
+        all.add(s.sums[turn & 1][w]);
+        all.lost += s.lost[turn & 1][w];
+    }
+    return all.sum + all.lost;
+}
+
+// A sum of floats, which may cancel, in fixed point: a float's 24 bits lie in two digits, which integers add up in any order.
+__device__ __forceinline__ void add_digits(Scratch& s, float v) {
+    const uint32_t bits = float_bits(v), e = (bits >> 23) & 0xff, at = e ? e - 1 : 0;
+    const uint64_t x = (uint64_t)((bits & 0x7fffffu) | (e ? 0x800000u : 0u)) << (at & 31);
+    const uint64_t lo = (uint32_t)x, hi = x >> 32;
+    unsigned long long* digit = &s.digits[at >> 5][threadIdx.x % kCopies];
+    atomicAdd(digit, bits >> 31 ? 0 - lo : lo);
+    atomicAdd(digit + kCopies, bits >> 31 ? 0 - hi : hi);
+}
+// What they come to, rounded once; by one thread, which leaves them in another form.
+__device__ __forceinline__ double digits_value(Scratch& s) {
+    int64_t carry = 0;
+#pragma unroll 1
+    for (uint32_t k = 0; k < kDigits; ++k) {  // each to 32 bits
+        carry += (int64_t)s.digits[k][0];
+        s.digits[k][0] = (uint32_t)carry;
+        carry >>= 32;
+    }
+    const bool negative = carry < 0;
+    if (negative) {
+        carry = 1;
+#pragma unroll 1
+        for (uint32_t k = 0; k < kDigits; ++k) {
+            carry += (uint32_t)~s.digits[k][0];
+            s.digits[k][0] = (uint32_t)carry;
+            carry >>= 32;
+        }
+    }
+    int top = (int)kDigits - 1;
+#pragma unroll 1
+    while (top > 0 && s.digits[top][0] == 0) --top;
+    if (s.digits[top][0] == 0) return 0.0;
+    // the highest 64 bits, in the lowest of them whether anything lies below
+    uint64_t most = (s.digits[top][0] << 32) | (top > 0 ? s.digits[top - 1][0] : 0), rest = top > 1 ? s.digits[top - 2][0] << 32 : 0;
+    const int zeros = __builtin_clzll(most);
+    if (zeros) {
+        most = (most << zeros) | (rest >> (64 - zeros));
+        rest <<= zeros;
+    }
+#pragma unroll 1
+    for (int k = 0; k < top - 2; ++k) rest |= s.digits[k][0];
+    const double value = ldexp((double)(most | (rest ? 1 : 0)), 32 * (top - 1) - zeros - 149);
+    return negative ? -value : value;
+}
+
+// Whether two sums of the same row in other orders might come to statistics that differ in 32 bits.  A summand goes through `each` additions
+// (at most 32) of its thread, 6 of its wavefront and those of the workgroup's, so that a sum is within as many times 2^-53 of its summands' sizes,
+// whose mean is at most |mean| + sqrt(variance) (Cauchy).  Once in some 2^20 rows they might (where a mean is small beside its row, oftener); then
+// the row is added up again, exactly.  What is given is the same in every thread.
+__device__ __forceinline__ bool undecided(int kind, double mean, double variance, double rstd, float eps, uint32_t each, uint32_t waves) {
+    // within 2^-45 of the middle between two floats, or below the normal ones
+    const uint64_t bits = __builtin_bit_cast(uint64_t, rstd);
+    const uint32_t low = ((uint32_t)bits - (0x10000000u - 256u)) & 0x1fffffffu, high = (uint32_t)(bits >> 32);
+    bool open = low < 512u || high - 1u < 0x38100000u - 1u;
+    if (kind == ZK_NORM_LAYER) {
+        const double by = (double)(each + waves + 10) * 0x1.01p-53 * (__builtin_fabs(mean) + __builtin_amdgcn_sqrt(variance));  // the root to some 2^-20
+        // around a mean that is off by as much the squares come to by^2 more
+        open = open || __ballot((float)(mean - by) < (float)(mean + by) || by * by * 0x1p47 > variance + (double)eps);
+    }
+    return open;
+}
+// `over` hands each of the thread's elements on, and whether it is one of the row.
+template <typename Over>
+__device__ __forceinline__ Stats exact_stats(int kind, double n, float eps, Scratch& s, int& turn, uint32_t waves, Over over) {
+    double mean = 0.0;
+    if (kind == ZK_NORM_LAYER) {
+        const int slot = turn++ & 1;
+        for (uint32_t k = threadIdx.x; k < kDigits * kCopies; k += blockDim.x) s.digits[0][k] = 0;
+        __syncthreads();
+        over([&](float v, bool in) { add_digits(s, in ? v : 0.0f); });
+        __syncthreads();
+        if (threadIdx.x < kDigits)
+            for (uint32_t c = 1; c < kCopies; ++c) s.digits[threadIdx.x][0] += s.digits[threadIdx.x][c];
+        __syncthreads();
+        if (threadIdx.x == 0) s.sums[slot][0] = digits_value(s);
+        __syncthreads();
+        mean = s.sums[slot][0] / n;
+    }
+    Squares squares;
+    over([&](float v, bool in) { squares.add_of(in ? (double)v : mean, mean); });
+    const double variance = all_add(squares, s, turn++, waves) / n;
+    return Stats{(float)mean, (float)rstd_of(variance, eps)};
+}
 __device__ __forceinline__ float normed(float v, int kind, const Stats& st) {
     if (kind == ZK_NORM_LAYER) v = v - st.mean;
     return kind == ZK_NORM_NONE ? v : v * st.rstd;
@@ -183,7 +324,7 @@ __device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, co
         if (kind == ZK_NORM_LAYER) {
 #pragma unroll
             for (int i = 0; i < E; ++i) sum += (double)v[i];  // zeros behind the row's end
-            mean = all_add(sum, s, turn++, waves) / n;
+            mean = one_for_all(all_add(sum, s, turn++, waves) / n);
             sum = 0.0;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
@@ -194,7 +335,13 @@ __device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, co
 #pragma unroll
             for (int i = 0; i < E; ++i) sum = __builtin_fma((double)v[i], (double)v[i], sum);
         }
-        const Stats st = {(float)mean, rstd_of(all_add(sum, s, turn++, waves), n, eps)};
+        const double variance = all_add(sum, s, turn++, waves) / n, rstd = one_for_all(rstd_of(variance, eps));
+        Stats st = {(float)mean, (float)rstd};
+        if (__builtin_expect(undecided(kind, mean, variance, rstd, eps, E, waves), 0))
+            st = exact_stats(kind, n, eps, s, turn, waves, [&](auto take) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) take(v[i], at.in(i));
+            });
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = normed(v[i], kind, st);
     }
@@ -273,9 +420,11 @@ __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* sc
     }
 }
 
-// Eight wavefronts to a SIMD where eight elements do: 777 rows of 4097 floats 16.3 -> 14.6 us, though a few registers spill.
+// Eight wavefronts to a SIMD where eight elements do: 777 rows of 4097 floats 16.3 -> 14.6 us, though registers spill (6 to 8 of a thread's
+// where no 16-byte load is taken, 14 of floats in whole runs); five with 16 elements of 16 bits, which would be four with the registers that the
+// second sums ask for (8192 rows of 5120 bf16 90 us, 114 with four).
 template <int DT, int E, bool WIDE>
-__global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : 4) void k_block_norm(NormArgs n) {
+__global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : DT == ZK_F32 ? 4 : 5) void k_block_norm(NormArgs n) {
     __shared__ Scratch s;
     const block_norm_args& a = n.a;
     const size_t row = row_of_block();
@@ -338,7 +487,7 @@ __global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : 4) void k_block_norm(Nor
 // Rows of more than 16 elements to a thread (or of eight that no 16-byte load takes): the row lies in LDS, in 32 bits, each element
 // read and written by the thread that brought it.  In registers, with the gains beside, they would spill (100 us for one row).
 template <int DT>
-__global__ __launch_bounds__(kMostThreads) void k_block_norm_long(NormArgs n) {
+__global__ __launch_bounds__(kMostThreads, 8) void k_block_norm_long(NormArgs n) {
     extern __shared__ __attribute__((aligned(16))) float line[];
     __shared__ Scratch s;
     const block_norm_args& a = n.a;
@@ -359,7 +508,12 @@ __global__ __launch_bounds__(kMostThreads) void k_block_norm_long(NormArgs n) {
             const double d = (double)line[i] - mean;
             sum = __builtin_fma(d, d, sum);
         }
-        st.rstd = rstd_of(all_add(sum, s, turn++, waves), (double)dim, a.eps);
+        const double variance = all_add(sum, s, turn++, waves) / (double)dim, rstd = one_for_all(rstd_of(variance, a.eps));
+        if (__builtin_expect(undecided(kind, mean, variance, rstd, a.eps, 32, waves), 0))
+            return exact_stats(kind, (double)dim, a.eps, s, turn, waves, [&](auto take) {
+                for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) take(line[i], true);
+            });
+        st.rstd = (float)rstd;
         st.mean = (float)mean;
         return st;
     };
