@@ -613,7 +613,8 @@ int kvcache_attention(const kvcache_i8* cache, const void* q, size_t q_row_strid
  * rows, not once for each sequence.  A page of the prefix outside the cache makes NaN of the rows that see a key in it
  * (ZK_FAULT_PAGE).  prefix_pages may be 0.  rows * (q_heads / kv_heads) < 2^31 - 256;
  * max_new * q_heads <= 2^26 - 4; seqs * kv_heads, times the parts that a long context is shared out in (at most 32), below some 2^22.  ws: device (always needed),
- * kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_pages * page_tokens, max_len). */
+ * kvcache_attention_prefix_workspace_bytes(seqs, rows, max_new, q_heads, kv_heads, head_dim, prefix_pages * page_tokens, max_len): for each of the rows and
+ * q_heads 4 * (head_dim + 2) bytes for each part, however unlike the sequences are. */
 size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32_t rows, uint32_t max_new, uint32_t q_heads, uint32_t kv_heads,
                                                 uint32_t head_dim, uint32_t prefix_tokens, uint32_t max_len);
 int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,

@@ -175,10 +175,20 @@ __device__ void not_a_number(const Args& a, uint32_t b, uint32_t h) {
         }
 }
 
+// A sequence that is skipped, where a later launch sees to its outputs.
+__device__ __forceinline__ void fault_once(const Args& a, uint32_t part, uint32_t h) {
+    if (part == 0 && h == 0 && threadIdx.x == 0) report(a.s, ZK_FAULT_LENGTH);
+}
+
 // The first key that row i of a sequence sees, or any of the later rows.
 __device__ __forceinline__ uint32_t first_seen(const Args& a, const SeqView& v, int32_t i) {
     const int64_t low = a.window ? (int64_t)v.len - v.rows + i - (int64_t)a.window + 1 : 0;
     return low > 0 ? (uint32_t)low : 0;
+}
+
+// Where the sums of a sequence and head over a part of its keys lie: those of its first row, the others behind.
+__device__ __forceinline__ size_t own_part(const Args& a, const SeqView&, uint32_t b, uint32_t h, uint32_t split) {
+    return (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most;
 }
 
 // The tile that a sequence's keys begin with, before its lengths are known.
@@ -471,7 +481,8 @@ __device__ __forceinline__ void attend_few(const A& a, float* sh, uint32_t split
     Asked pages = ask_pages(a, b, guess, W);
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (a.splits == 1 && !A::joined) not_a_number(a, b, h);
+        if (A::joined) fault_once(a, split, h);
+        else if (a.splits == 1) not_a_number(a, b, h);
         return;
     }
     if (v.rows == 0) return;
@@ -480,8 +491,7 @@ __device__ __forceinline__ void attend_few(const A& a, float* sh, uint32_t split
     const uint32_t t_first = tiles.first + split * each, t_end = t_first + each < tiles.end ? t_first + each : tiles.end;
     if (a.splits > 1 && t_first >= t_end) return;  // k_attend_join knows
     if (t_first + wave != guess) pages = ask_pages(a, b, t_first + wave, W);
-    attend_part<NJ, RT, W>(a, sh, v, b, h, t_first, t_end, pages, a.splits == 1 && !A::joined,
-                           (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most);
+    attend_part<NJ, RT, W>(a, sh, v, b, h, t_first, t_end, pages, a.splits == 1 && !A::joined, own_part(a, v, b, h, split));
 }
 template <int NJ, int RT, int W>
 __global__ __launch_bounds__(64 * W, W == 4 && NJ * RT <= 2 ? 2 : 1) void k_attend_few(Args a) {
@@ -721,7 +731,8 @@ __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& s
     constexpr uint32_t rows = 32 * WV;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (tile == 0 && a.splits == 1 && !A::joined) not_a_number(a, b, h);
+        if (A::joined) fault_once(a, split + tile, h);
+        else if (tile == 0 && a.splits == 1) not_a_number(a, b, h);
         return;
     }
     const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + rows - 1) / rows;
@@ -739,7 +750,7 @@ __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& s
     const uint32_t r = r0 + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
     const int32_t pos = r < R ? v.len - v.rows + (int32_t)(r / a.group) : -1;
     attend_rows<DT, false, WV>(a, lds, sh, v, b, h, R, r0, tiles, pos, v.len - v.rows + tok0, v.len - v.rows + tok1, first_seen(a, v, tok0), a.splits > 1 || A::joined,
-                    (((size_t)b * a.cache.kv_heads + h) * a.splits + split) * a.rows_most, a.parts, a.parts_ml);
+                    own_part(a, v, b, h, split), a.parts, a.parts_ml);
 }
 template <int DT>
 __global__ __launch_bounds__(kBlock, DT <= 4 ? 2 : 1) void k_attend_many(Args a) {

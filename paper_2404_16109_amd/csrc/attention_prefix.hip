@@ -18,6 +18,7 @@ namespace {
 // four there is room on a CU for a workgroup of the other kind beside, which few rows need more.
 bool eight_waves(uint64_t rows, uint32_t head_dim) { return rows >= 1024 && head_dim <= 128; }
 static const uint32_t kMostParts = 32;  // of the prefix, and of a sequence's own keys
+static const uint32_t kMostJoins = 1 << 20;  // workgroups of k_prefix_join that a head has
 
 struct PrefixArgs : Args {
     static constexpr bool joined = true;
@@ -25,9 +26,15 @@ struct PrefixArgs : Args {
     uint32_t front_tokens;     // a multiple of the page
     uint32_t front_tiles;      // whole tiles of it; what is left is read with each sequence's own
     uint32_t front_splits, front_each, front_groups, row_tile;
-    float* front_parts;        // [head][split][row of the batch]
-    float2* front_ml;
 };
+// Sums lie as [head][part][row of the batch], the parts of the prefix before the own ones: what is kept for a row does not go by how many
+// rows other sequences have.
+__device__ __forceinline__ size_t part_rows(const PrefixArgs& a, uint32_t h, uint32_t part) {
+    return ((size_t)h * (a.front_splits + a.splits) + part) * (a.s.rows * a.group);
+}
+__device__ __forceinline__ size_t own_part(const PrefixArgs& a, const SeqView& v, uint32_t, uint32_t h, uint32_t split) {
+    return part_rows(a, h, a.front_splits + split) + (uint32_t)v.row0 * a.group;
+}
 
 // As for a sequence alone, but that its first tokens lie in the prefix's pages, and its first tiles are not its own.
 __device__ __forceinline__ uint32_t page_of(const PrefixArgs& a, uint32_t b, uint32_t token) {
@@ -79,7 +86,7 @@ __device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, Fro
     const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
     const int32_t pos = r < R ? sh.place[r / a.group - (uint32_t)tok0] : -1;
     const SeqView all = {0, (int32_t)a.s.rows, 0, true};
-    attend_rows<DT, true, WV>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, ((size_t)h * a.front_splits + split) * R, a.front_parts, a.front_ml);
+    attend_rows<DT, true, WV>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, part_rows(a, h, split), a.parts, a.parts_ml);
 }
 
 // RT: tiles of 16 rows that a sequence and head has, 0: many rows.  Workgroups of one head lie eight apart where there are eight heads, so
@@ -105,31 +112,45 @@ __global__ __launch_bounds__(64 * WV, WV == 8 || (DT <= 4 && RT < 2) ? 2 : 1) vo
     }
 }
 
-// A wavefront: one row of one sequence and head.  Lanes hold four dimensions each; the lanes left of 64 take parts in turn.
-__global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
-    const uint32_t H = a.cache.kv_heads, d = a.cache.head_dim, b = blockIdx.y, lane = threadIdx.x & 63;
-    const uint32_t item = uniform(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)), h = item / a.rows_most, r = item - h * a.rows_most;
-    const SeqView v = seq_view(a.s, b, a.page_log);
-    if (!v.ok) {  // the workgroup's first wavefront is at row 0 of a head where one begins there
-        if (blockIdx.x == 0)
-            for (uint32_t head = 0; head < H; ++head) not_a_number(a, b, head);
+// A wavefront: one row of the batch and a head.  Lanes hold four dimensions each; the lanes left of 64 take parts in turn.
+__device__ __forceinline__ void join_row(const PrefixArgs& a, uint32_t h, uint32_t row) {
+    const uint32_t H = a.cache.kv_heads, d = a.cache.head_dim, lane = threadIdx.x & 63, token = row / a.group;
+    // the first sequence that has the row: 64 of them are looked at at once
+    SeqView v;
+    bool found = false;
+    for (uint32_t b0 = 0; b0 < a.s.seqs && !found; b0 += 64) {
+        const uint32_t b = b0 + lane < a.s.seqs ? b0 + lane : a.s.seqs - 1;
+        const int32_t from = a.s.cu[b], end = a.s.cu[b + 1], len = a.s.lens[b];
+        const uint64_t has = __ballot(from <= (int32_t)token && (int32_t)token < end);
+        if (has) {
+            const int at = __ffsll((long long)has) - 1;
+            v = seq_view(a.s, a.page_log, __builtin_amdgcn_readlane(from, at), __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(len, at));
+            found = true;
+        }
+    }
+    if (!found) return;  // nobody's
+    const size_t out0 = (size_t)token * a.orow + (size_t)(h * a.group + (row - token * a.group)) * a.ohead;
+    const size_t lse_at = (size_t)token * H * a.group + h * a.group + (row - token * a.group);
+    if (!v.ok) {
+        for (uint32_t i = lane; i < d; i += 64) put_at(a.out, out0 + i, __builtin_nanf(""), a.dtype);
+        if (a.lse && lane == 0) a.lse[lse_at] = __builtin_nanf("");
         return;
     }
-    if (h >= H || r >= (uint32_t)v.rows * a.group) return;
+    const uint32_t r = row - (uint32_t)v.row0 * a.group;
     const int32_t pos = v.len - v.rows + (int32_t)(r / a.group);
-    const uint32_t R = a.s.rows * a.group, row = (uint32_t)v.row0 * a.group + r;
     // parts of the prefix come first; a row that sees no key has none
     const uint32_t front = pos >= 0 ? a.front_splits : 0;
     const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / a.row_tile * a.row_tile, a.row_tile);
-    const uint32_t each = part_of(a, tiles), n = tiles.end - tiles.first, own = pos >= 0 && n ? (n + each - 1) / each : 0;
-    const size_t front0 = (size_t)h * a.front_splits * R + row, own0 = ((size_t)b * H + h) * a.splits * a.rows_most + r;
+    const uint32_t each = part_of(a, tiles), n = tiles.end - tiles.first, own = pos >= 0 && n ? (n + each - 1) / each : 0, parts = front + own;
+    const size_t first = part_rows(a, h, 0) + row;
+    const uint32_t R = a.s.rows * a.group;  // from a part to the next
     float m = -kInf, l = 0.0f;
-    if (lane < front + own) {
-        const float2 ml = lane < front ? a.front_ml[front0 + (size_t)lane * R] : a.parts_ml[own0 + (size_t)(lane - front) * a.rows_most];
+    if (lane < parts) {
+        const float2 ml = a.parts_ml[first + (size_t)lane * R];
         m = ml.x;
         l = ml.y;
     }
-    const uint32_t quads = d >> 2, ways = 64 / quads, way = lane / quads, c = lane - way * quads, parts = front + own;
+    const uint32_t quads = d >> 2, ways = 64 / quads, way = lane / quads, c = lane - way * quads;
     v4f sum = {0, 0, 0, 0};
     float weight = 0.0f, ref = 0.0f;
     // eight parts of a lane are on their way at once, the first beside the maxima
@@ -139,10 +160,7 @@ __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
         for (int u = 0; u < 8; ++u) {
             const uint32_t p = p0 + u * ways + way;
             x[u] = v4f{0, 0, 0, 0};
-            if (way < ways && p < parts) {
-                const size_t at = p < front ? front0 + (size_t)p * R : own0 + (size_t)(p - front) * a.rows_most;
-                x[u] = ((const v4f*)(p < front ? a.front_parts : a.parts))[at * quads + c];
-            }
+            if (way < ways && p < parts) x[u] = ((const v4f*)a.parts)[(first + (size_t)p * R) * quads + c];
         }
         if (p0 == 0) {
             const float top = wave_max(m);
@@ -165,12 +183,15 @@ __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
         }
     }
     if (way == 0) {
-        const size_t at = row_at(a, v, h, r, a.orow, a.ohead) + 4 * c;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) put_at(a.out, at + e, l == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
+        for (int e = 0; e < 4; ++e) put_at(a.out, out0 + 4 * c + e, l == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
     }
-    if (a.lse && lane == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l);
+    if (a.lse && lane == 0) a.lse[lse_at] = lse_of(ref, l);
+}
+__global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
+    const uint32_t R = a.s.rows * a.group, step = gridDim.x * (kBlock / 64);
+    for (uint32_t row = uniform(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)); row < R; row += step) join_row(a, blockIdx.y, row);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
@@ -216,15 +237,12 @@ Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uin
 }
 
 // What lies in the workspace; with a null base the bytes alone.
-size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint64_t most, uint32_t seqs, uint32_t kv_heads, uint32_t head_dim, PrefixArgs* a) {
-    const size_t own = (size_t)seqs * kv_heads * p.splits * most, front = (size_t)kv_heads * p.front_splits * rows;
-    void* at[4] = {cv.take(own * head_dim * sizeof(float)), cv.take(own * sizeof(float2)), cv.take(front * head_dim * sizeof(float)),
-                   cv.take(front * sizeof(float2))};
+size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint32_t kv_heads, uint32_t head_dim, PrefixArgs* a) {
+    const size_t parts = (size_t)kv_heads * (p.front_splits + p.splits) * rows;
+    void* at[2] = {cv.take(parts * head_dim * sizeof(float)), cv.take(parts * sizeof(float2))};
     if (a) {
         a->parts = (float*)at[0];
         a->parts_ml = (float2*)at[1];
-        a->front_parts = (float*)at[2];
-        a->front_ml = (float2*)at[3];
     }
     return cv.used();
 }
@@ -238,7 +256,8 @@ int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
     }
     if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_prefix<DT, RT, WV>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL((k_prefix<DT, RT, WV>), dim3((unsigned)(a.front_groups + own)), dim3(64 * WV), lds, s, a);
-    hipLaunchKernelGGL(k_prefix_join, dim3((unsigned)div_up((size_t)a.rows_most * a.cache.kv_heads, kBlock / 64), a.s.seqs), dim3(kBlock), 0, s, a);
+    const size_t joins = div_up((size_t)a.s.rows * a.group, kBlock / 64);
+    hipLaunchKernelGGL(k_prefix_join, dim3((unsigned)(joins < kMostJoins ? joins : kMostJoins), a.cache.kv_heads), dim3(kBlock), 0, s, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -268,7 +287,7 @@ extern "C" size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32
     const uint32_t group = q_heads / kv_heads;
     const uint64_t all = (uint64_t)rows * group, most = rows_most(rows, max_new, group);
     Carver cv(nullptr, 0);
-    return carve(cv, plan_of(seqs, all, most, kv_heads, head_dim, prefix_tokens, max_len), all, most, seqs, kv_heads, head_dim, nullptr);
+    return carve(cv, plan_of(seqs, all, most, kv_heads, head_dim, prefix_tokens, max_len), all, kv_heads, head_dim, nullptr);
 }
 
 extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
@@ -281,7 +300,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     if (!q || !out || !aligned(q, 2) || !aligned(out, 2) || (lse && !aligned(lse, 4))) return ZK_E_BADARG;
     const uint32_t group = q_heads / cache->kv_heads;
     const uint64_t rows = (uint64_t)seqs->rows * group, most = rows_most(seqs->rows, seqs->max_new, group);
-    if (rows >= 0x7fffff00u || div_up(most * cache->kv_heads, kBlock / 64) >= (uint64_t)1 << 24) return ZK_E_BADARG;  // k_prefix_join: below 2^32 threads
+    if (rows >= 0x7fffff00u || most * cache->kv_heads > ((uint64_t)1 << 26) - 4) return ZK_E_BADARG;
     PrefixArgs a = {};
     a.cache = *cache;
     a.s = *seqs;
@@ -314,7 +333,7 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     a.front_groups = (uint32_t)front;
     if (!ws) return ZK_E_BUFSZ;
     Carver cv(ws, ws_bytes);
-    carve(cv, p, rows, most, seqs->seqs, cache->kv_heads, cache->head_dim, &a);
+    carve(cv, p, rows, cache->kv_heads, cache->head_dim, &a);
     if (cv.overflow()) return ZK_E_BUFSZ;
     hipStream_t s = as_stream(stream);
     switch ((cache->head_dim + 31) / 32) {

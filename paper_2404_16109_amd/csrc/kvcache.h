@@ -10,15 +10,17 @@ struct SeqView {
     bool ok;
 };
 
-__device__ __forceinline__ SeqView seq_view(const kv_seqs& s, uint32_t b, uint32_t page_log) {
+__device__ __forceinline__ SeqView seq_view(const kv_seqs& s, uint32_t page_log, int32_t from, int32_t end, int32_t len) {
     SeqView v;
-    v.row0 = s.cu[b];
-    const int32_t end = s.cu[b + 1];
+    v.row0 = from;
     v.rows = end - v.row0;
-    v.len = s.lens[b];
+    v.len = len;
     v.ok = v.row0 >= 0 && end >= v.row0 && (uint32_t)end <= s.rows && (uint32_t)v.rows <= s.max_new && v.len >= 0 &&
            ((uint64_t)v.len + (1u << page_log) - 1) >> page_log <= s.table_pages;
     return v;
+}
+__device__ __forceinline__ SeqView seq_view(const kv_seqs& s, uint32_t b, uint32_t page_log) {
+    return seq_view(s, page_log, s.cu[b], s.cu[b + 1], s.lens[b]);
 }
 
 __device__ __forceinline__ void report(const kv_seqs& s, uint32_t what) {

@@ -181,3 +181,20 @@ def test_prefix_launches_are_below_2_to_the_32_threads(zk):
         assert prefix(zk, c=c, heads=1, s=seqs(zk, seqs=1, rows=rows, max_new=rows)) == want, rows
     for rows, want in (((1 << 21) - 1, zk.ZK_E_BUFSZ), (1 << 21, zk.ZK_E_BADARG)):   # 32 heads
         assert prefix(zk, c=c, heads=32, s=seqs(zk, seqs=1, rows=rows, max_new=rows)) == want, rows
+
+
+@pytest.mark.parametrize("seqs_,rows,max_new,prefix_tokens,max_len", [
+    (128, 2048 + 127, 2048, 8192, 10240), (256, 4096 + 255, 4096, 2048, 8000), (64, 64, 1, 8192, 8704), (16, 490, 64, 32768, 33068), (1, 5000, 5000, 4096, 5000),
+    (65535, 65535, 1, 512, 600), (700, 700 + 299, 300, 0, 900)])
+def test_workspace_of_a_prefix_goes_by_rows(zk, seqs_, rows, max_new, prefix_tokens, max_len):
+    """A prompt's next part beside single tokens wants no more than its rows do: 32 parts of the prefix and 32 own ones at most, and some where
+    either has one tile only."""
+    for heads, kv, d in ((40, 8, 128), (16, 16, 64), (8, 1, 256)):
+        need = zk.kvcache_attention_prefix_workspace_bytes(seqs_, rows, max_new, heads, kv, d, prefix_tokens, max_len)
+        part = rows * heads * 4 * (d + 2)
+        own = max(max_len - prefix_tokens, 1)
+        most = min(32, -(-prefix_tokens // 64)) + min(32, -(-own // 256))   # own parts have four tiles at least
+        assert part <= need <= part * most + 4096, (need, part)
+    # beside many sequences nothing of their own is shared out: parts of the prefix and one more
+    if seqs_ == 128:
+        assert zk.kvcache_attention_prefix_workspace_bytes(seqs_, rows, max_new, 40, 8, 128, prefix_tokens, max_len) < 1 << 30
