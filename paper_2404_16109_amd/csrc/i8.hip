@@ -11,6 +11,7 @@
 // products.  Measured: 8192 x 13824 x 5120 522 us, 2.2 P operations/s, 8192^3 2.4 (a library's product 2.2 and 2.4): the matrix cores are
 // 61% busy at 1.84 GHz, to which the card's power brings the clock.  Stages of 64 of k, four or five ahead, took 645 us where this took 584.
 // Where there are fewer tiles than the chip holds, workgroups share k and k_join adds up (333 rows by 5120 x 13824: 33 us and 6).
+#include "i8_plan.h"
 #include "serve_dev.h"
 
 #pragma clang fp contract(off)
@@ -35,7 +36,6 @@ struct Args {
     uint32_t n_pad;
     bool quads, wide;       // y takes four outputs, or 16 bytes, at once
 };
-static const uint32_t kStep = 128;  // of k
 
 // Four outputs of a row, from n0 on: those below n are stored.
 template <int Y>
@@ -71,7 +71,7 @@ __device__ __forceinline__ void finish_quad(const Args& a, uint32_t split, uint3
 // ---- few rows --------------------------------------------------------------------------------------------------------
 
 // RT: tiles of 16 rows; NT: of 16 outputs.  Lane 16 g + i: row (output) i of a tile, bytes 16 g .. 16 g + 15 of 64.
-static const int kWaves = 8, kAhead = 3;
+static const int kAhead = 3;
 template <int RT, int NT, int Y>
 __global__ __launch_bounds__(64 * kWaves) void k_few(Args a) {
     __shared__ v4i red[kWaves][RT * NT][64];
@@ -364,85 +364,17 @@ __global__ __launch_bounds__(kBlock) void k_join(Args a) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 
-enum Tile { kFew, kShort, kMid, kWide, kLarge };
-struct Plan {
-    Tile tile;
-    uint32_t nt, groups, splits, each;  // nt: tiles of 16 outputs to a workgroup of k_few
-};
-void share_k(Plan& p, uint32_t steps, uint32_t splits) {
-    p.each = (uint32_t)align_up(div_up(steps, splits), 2);  // k_tiles takes two steps at a time
-    p.splits = (uint32_t)div_up(steps, p.each);
-}
-
-// Up to 32 rows.  More outputs to a workgroup read x less often, fewer fill the chip.  Measured, us, weights from HBM, 16 / 32 / 64 outputs
-// to a workgroup: one row by 13824 x 5120 16.8 18.6 19.1, 16 rows 25.2 23.6 20.9, 32 rows 38 29 23.7; 32 rows by 5120 x 13824 46 33 48, and
-// with k shared by three 36 29 24.3; 32 rows by 5120 x 5120 16 11.9 16.4 (shared 15 13 12.3); 16 rows by 2000 x 8192 9.9 13.2.  Few outputs
-// share a long k, which costs a launch: one row by 941 x 21856 11.9 us in one part, 7.9 in four, by 339 x 10768 7.2 and 5.7 in a graph, but 7.4
-// and 9.3 called from Python, where launches count; by 500 x 4096 4.7 and 4.8.
-Plan plan_few(uint32_t rows, size_t n, uint32_t steps) {
-    Plan p = {};
-    p.tile = kFew;
-    const bool shares = rows > 16 && steps >= 64;  // a part takes eight steps at least, and a launch to join them
-    p.nt = rows <= 4 ? 1 : n >= 64 * 200 || (shares && n >= 64 * 32) ? 4 : n >= 32 * 128 ? 2 : 1;
-    p.groups = (uint32_t)div_up(n, 16 * p.nt);
-    uint32_t splits = p.groups < 128 ? 256 / p.groups : 1;
-    const uint32_t most = p.nt == 4 || steps >= 96 ? steps / (2 * kWaves) : 1;
-    if (splits > most) splits = most;
-    share_k(p, steps, splits ? splits : 1);
-    return p;
-}
-
-// Tiles of more rows: rows and outputs, workgroups to a CU, and us a step of 128 with one, two or three of them there.  Measured with
-// as many tiles as the chip takes at once, the difference between k 8192 and 2048.
-struct Shape {
-    uint32_t rows, outs, slots;
-    double step[3];
-};
-const Shape kShapes[] = {{}, {64, 128, 3, {0.57, 0.81, 0.90}}, {128, 128, 2, {0.66, 0.95}}, {192, 256, 1, {1.38}}, {256, 256, 1, {1.69}}};
-
-// The tile and the parts of k that take least: rounds of the chip's 256 CUs, each with what a workgroup begins and ends with, and the parts'
-// way to memory and back.  Measured and, in brackets, tiles of 128 x 128 in as many parts as are best: 2048 x 5120 x 5120 56.7 us (76.5), of
-// 600 x 2000 x 27200 58.0 (58.0), of 1000 x 5120 x 5120 38.9 (38.9), of 8192 x 13824 x 5120 523.
-Plan plan_tiles(size_t rows, size_t n, uint32_t steps) {
-    Plan best = {};
-    double least = 0.0;
-    for (int t = kShort; t <= kLarge; ++t) {
-        const Shape& s = kShapes[t];
-        const uint64_t groups = div_up(rows, s.rows) * div_up(n, s.outs);
-        if (t < kLarge && groups >= (uint64_t)1 << 22) continue;  // a launch holds fewer than 2^32 threads
-        for (uint32_t splits = 1; splits <= 16 && splits * 4 <= (steps < 4 ? 4 : steps); ++splits) {
-            if (splits > 1 && groups * (splits - 1) >= 256 * s.slots) break;
-            Plan p = {};
-            p.tile = (Tile)t;
-            p.groups = (uint32_t)groups;
-            share_k(p, steps, splits);
-            const uint64_t all = groups * p.splits, chip = 256 * s.slots, rest = all % chip;
-            const double rounds = (double)(all / chip) * (p.each * s.step[s.slots - 1] + 3.0) + (rest ? p.each * s.step[(rest - 1) / 256] + 3.0 : 0.0);
-            const double us = rounds + (p.splits > 1 ? 2.0 + 8.0 * (double)rows * (double)n * p.splits / 8e6 : 0.0);
-            if (!best.groups || us < least) {
-                least = us;
-                best = p;
-            }
-        }
-    }
-    return best;
-}
-Plan plan_of(size_t rows, size_t n, size_t k) {
-    const uint32_t steps = (uint32_t)div_up(k, kStep);
-    return rows <= 32 ? plan_few((uint32_t)rows, n, steps) : plan_tiles(rows, n, steps);
-}
-
 template <int RT, int Y>
-void launch_few(const Args& a, const Plan& p, hipStream_t s) {
+void launch_few(const Args& a, const I8Plan& p, hipStream_t s) {
     const dim3 grid(p.groups, p.splits), block(64 * kWaves);
     if (p.nt == 1) hipLaunchKernelGGL((k_few<RT, 1, Y>), grid, block, 0, s, a);
     else if (p.nt == 2) hipLaunchKernelGGL((k_few<RT, 2, Y>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_few<RT, 4, Y>), grid, block, 0, s, a);
 }
 template <int Y>
-int launch(const Args& a, const Plan& p, hipStream_t s) {
+int launch(const Args& a, const I8Plan& p, hipStream_t s) {
     const dim3 grid(p.groups, p.splits);
-    const Shape& t = kShapes[p.tile];
+    const I8Shape& t = kShapes[p.tile];
     const uint32_t rt = p.tile == kFew ? 0 : (uint32_t)div_up(a.rows, t.rows), nt = p.tile == kFew ? 0 : (uint32_t)div_up(a.n, t.outs);
     if (p.tile == kFew) a.rows <= 16 ? launch_few<1, Y>(a, p, s) : launch_few<2, Y>(a, p, s);
     else if (p.tile == kShort) hipLaunchKernelGGL((k_tiles<2, 1, 2, 2, Y>), grid, dim3(256), 0, s, a, rt, nt);
@@ -465,7 +397,7 @@ using namespace zkmi;
 
 extern "C" size_t i8_matmul_workspace_bytes(size_t rows, size_t n, size_t k) {
     if (rows == 0 || !sizes_ok(rows, n, k)) return 0;
-    const Plan p = plan_of(rows, n, k);
+    const I8Plan p = i8_plan(rows, n, k);
     if (p.splits == 1) return 0;
     Carver cv(nullptr, 0);
     cv.take((size_t)p.splits * rows * align_up(n, 4) * sizeof(int32_t));
@@ -480,7 +412,7 @@ extern "C" int i8_matmul(void* y, size_t y_row_stride, int y_dtype, const int8_t
     if (!y || !x || !w || !aligned(y, bytes) || !aligned(x, 16) || !aligned(w, 16)) return ZK_E_BADARG;
     if (rows > 1 && (x_row_stride < k || x_row_stride % 16 || x_row_stride > (size_t)1 << 23 || y_row_stride < n)) return ZK_E_BADARG;
     if (y_dtype != ZK_I32 && (!x_scales || !w_scales || !aligned(x_scales, 4) || !aligned(w_scales, 4))) return ZK_E_BADARG;
-    const Plan p = plan_of(rows, n, k);
+    const I8Plan p = i8_plan(rows, n, k);
     if (p.tile != kFew && (uint64_t)div_up(rows, kShapes[p.tile].rows) * div_up(n, kShapes[p.tile].outs) >= (uint64_t)1 << 23) return ZK_E_BADARG;
     Args a = {};
     a.y = y;
