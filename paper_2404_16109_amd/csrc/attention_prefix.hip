@@ -10,14 +10,12 @@
 // it 15 are latency, a prefix of one page takes as long, 15 the tiles, 1.2 each, and the rest parts on their way to memory and back); 16 questions
 // of up to 64 tokens behind 32768 386 us, 824 TFLOP/s: vector ALU 55% and matrix cores 41% busy, together nearly all.
 #include "attend_dev.h"
+#include "prefix_plan.h"
 
 namespace zkmi {
 namespace {
 
-// Wavefronts to a workgroup, 32 rows to each: of many rows eight share what a tile costs to bring, where their sums fit the registers; with
-// four there is room on a CU for a workgroup of the other kind beside, which few rows need more.
-bool eight_waves(uint64_t rows, uint32_t head_dim) { return rows >= 1024 && head_dim <= 128; }
-static const uint32_t kMostParts = 32;  // of the prefix, and of a sequence's own keys
+static_assert(kPrefixTile == kTile && kPrefixWorkgroups == kWorkgroups, "");
 static const uint32_t kMostJoins = 1 << 20;  // workgroups of k_prefix_join that a head has
 
 struct PrefixArgs : Args {
@@ -196,48 +194,8 @@ __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 
-bool few_rows(uint64_t rows) { return rows <= 32; }
-
-// How a call is spread.  rows: of the batch and a head; most: of a sequence and a head.
-struct Plan {
-    uint32_t row_tile, front_tiles, front_splits, front_each, splits, each;
-};
-Plan plan_of(uint32_t seqs, uint64_t rows, uint64_t most, uint32_t kv_heads, uint32_t head_dim, uint32_t prefix, uint32_t max_len) {
-    Plan p = {};
-    p.front_tiles = prefix / kTile;
-    p.row_tile = eight_waves(rows, head_dim) ? 256 : 128;
-    const auto share = [](uint64_t groups, uint32_t tiles, uint32_t& splits, uint32_t& each) {
-        uint64_t n = groups >= kWorkgroups / 2 ? 1 : div_up(kWorkgroups, groups);
-        if (n > div_up(tiles, 4)) n = div_up(tiles, 4);
-        if (n > kMostParts) n = kMostParts;
-        each = (uint32_t)div_up(tiles, n);
-        splits = (uint32_t)div_up(tiles, each);
-    };
-    if (p.front_tiles) {
-        // Time of the prefix by the number of parts, in us: as many rounds of a workgroup to each CU as it takes, 0.41 (0.57 with eight
-        // wavefronts) a tile for each 32 dimensions and 1 to begin with, and the parts' way to memory and back at 4 TB/s.  Measured for 320
-        // rows and 8 heads of 128 behind 8192 tokens, whole call: 4 parts 71 us, 8 46, 10 42, 16 44, 32 56.
-        const uint64_t groups = kv_heads * div_up(rows, p.row_tile);
-        double best = 0.0;
-        for (uint32_t n = 1; n <= kMostParts && n <= p.front_tiles; ++n) {
-            const uint32_t each = (uint32_t)div_up(p.front_tiles, n);
-            if (div_up(p.front_tiles, each) != n) continue;
-            const double us = (double)div_up(groups * n, kWorkgroups / 2) * ((p.row_tile == 256 ? 0.57 : 0.41) * each * (double)div_up(head_dim, 32) + 1.0) +
-                              (double)(kv_heads * rows * head_dim) * n * 8.0 / 4e6;
-            if (n == 1 || us < best) {
-                best = us;
-                p.front_splits = n;
-                p.front_each = each;
-            }
-        }
-    }
-    const uint32_t own = max_len > p.front_tiles * kTile ? (uint32_t)div_up(max_len - p.front_tiles * kTile, kTile) : 1;
-    share((uint64_t)seqs * kv_heads * (few_rows(most) ? 1 : div_up(most, p.row_tile)), own, p.splits, p.each);
-    return p;
-}
-
 // What lies in the workspace; with a null base the bytes alone.
-size_t carve(Carver& cv, const Plan& p, uint64_t rows, uint32_t kv_heads, uint32_t head_dim, PrefixArgs* a) {
+size_t carve(Carver& cv, const PrefixPlan& p, uint64_t rows, uint32_t kv_heads, uint32_t head_dim, PrefixArgs* a) {
     const size_t parts = (size_t)kv_heads * (p.front_splits + p.splits) * rows;
     void* at[2] = {cv.take(parts * head_dim * sizeof(float)), cv.take(parts * sizeof(float2))};
     if (a) {
@@ -263,8 +221,11 @@ int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
 }
 template <int DT, int WV>
 int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
-    if (a.rows_most <= 16) return launch<DT, 1, WV>(a, own, s);
-    return a.few ? launch<DT, 2, WV>(a, own, s) : launch<DT, 0, WV>(a, own, s);
+    switch (prefix_row_tiles(a.rows_most)) {
+        case 1: return launch<DT, 1, WV>(a, own, s);
+        case 2: return launch<DT, 2, WV>(a, own, s);
+        default: return launch<DT, 0, WV>(a, own, s);
+    }
 }
 template <int DT>
 int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
@@ -287,7 +248,7 @@ extern "C" size_t kvcache_attention_prefix_workspace_bytes(uint32_t seqs, uint32
     const uint32_t group = q_heads / kv_heads;
     const uint64_t all = (uint64_t)rows * group, most = rows_most(rows, max_new, group);
     Carver cv(nullptr, 0);
-    return carve(cv, plan_of(seqs, all, most, kv_heads, head_dim, prefix_tokens, max_len), all, kv_heads, head_dim, nullptr);
+    return carve(cv, prefix_plan(seqs, all, most, kv_heads, head_dim, prefix_tokens, max_len), all, kv_heads, head_dim, nullptr);
 }
 
 extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, size_t q_row_stride, size_t q_head_stride, int dtype,
@@ -315,12 +276,12 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     a.group = group;
     a.page_log = (uint32_t)log2_floor(cache->page_tokens);
     a.dtype = dtype;
-    a.few = few_rows(most);
+    a.few = prefix_few(most);
     a.wide = aligned(q, 16) && q_row_stride % 8 == 0 && q_head_stride % 8 == 0;
     a.rows_most = (uint32_t)most;
     a.front = prefix;
     a.front_tokens = prefix_pages * cache->page_tokens;
-    const Plan p = plan_of(seqs->seqs, rows, most, cache->kv_heads, cache->head_dim, a.front_tokens, seqs->max_len);
+    const PrefixPlan p = prefix_plan(seqs->seqs, rows, most, cache->kv_heads, cache->head_dim, a.front_tokens, seqs->max_len);
     a.front_tiles = p.front_tiles;
     a.row_tile = p.row_tile;
     a.front_splits = p.front_splits;
