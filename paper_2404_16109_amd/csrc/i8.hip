@@ -8,7 +8,7 @@
 // Many rows (k_tiles): tiles of x and w come through LDS, put there by loads that pass no register, a step of 128 ahead; 16-byte
 // pieces lie in LDS at piece ^ ((row / 2) & 7): rows of 128 bytes lie in one half of the banks or the other, so 16 neighbouring rows
 // answer from all of them (no conflict is counted).  One barrier a step, before its last quarter, the loads among that quarter's
-// products.  Measured: 8192 x 13824 x 5120 522 us, 2.2 P operations/s, 8192^3 2.4 (a library's product 2.2 and 2.4): the matrix cores are
+// products.  Measured: 8192 x 13824 x 5120 520 us, 2.2 P operations/s, 8192^3 2.4 (a library's product 2.2 and 2.4): the matrix cores are
 // 61% busy at 1.84 GHz, to which the card's power brings the clock.  Stages of 64 of k, four or five ahead, took 645 us where this took 584.
 // Where there are fewer tiles than the chip holds, workgroups share k and k_join adds up (333 rows by 5120 x 13824: 33 us and 6).
 #include "i8_plan.h"
