@@ -175,11 +175,6 @@ __device__ void not_a_number(const Args& a, uint32_t b, uint32_t h) {
         }
 }
 
-// A sequence that is skipped, where a later launch sees to its outputs.
-__device__ __forceinline__ void fault_once(const Args& a, uint32_t part, uint32_t h) {
-    if (part == 0 && h == 0 && threadIdx.x == 0) report(a.s, ZK_FAULT_LENGTH);
-}
-
 // The first key that row i of a sequence sees, or any of the later rows.
 __device__ __forceinline__ uint32_t first_seen(const Args& a, const SeqView& v, int32_t i) {
     const int64_t low = a.window ? (int64_t)v.len - v.rows + i - (int64_t)a.window + 1 : 0;
@@ -481,8 +476,7 @@ __device__ __forceinline__ void attend_few(const A& a, float* sh, uint32_t split
     Asked pages = ask_pages(a, b, guess, W);
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (A::joined) fault_once(a, split, h);
-        else if (a.splits == 1) not_a_number(a, b, h);
+        if (a.splits == 1 && !A::joined) not_a_number(a, b, h);
         return;
     }
     if (v.rows == 0) return;
@@ -731,8 +725,7 @@ __device__ __forceinline__ void attend_many(const A& a, char* lds, ManyShared& s
     constexpr uint32_t rows = 32 * WV;
     const SeqView v = seq_view(a.s, b, a.page_log);
     if (!v.ok) {
-        if (A::joined) fault_once(a, split + tile, h);
-        else if (tile == 0 && a.splits == 1) not_a_number(a, b, h);
+        if (tile == 0 && a.splits == 1 && !A::joined) not_a_number(a, b, h);
         return;
     }
     const uint32_t R = (uint32_t)v.rows * a.group, row_tiles = (R + rows - 1) / rows;

@@ -9,7 +9,7 @@
 // Measured, 8 heads of 128 and 40 of queries, whole calls in a graph: a step of 64 sequences behind 8192 tokens 37 us (11.1 GFLOP, 54 MB: of
 // it 15 are latency, a prefix of one page takes as long, 15 the tiles, 1.2 each, and the rest parts on their way to memory and back); 16 questions
 // of up to 64 tokens behind 32768 377 to 388 us, 820 to 843 TFLOP/s, on one card, 416 on another (vector ALU 56% and matrix cores 41% busy in a run under the
-// profiler, whose kernels took 430 and 17 us); a prompt's next 2048 tokens beside 127 single ones behind 8192 0.86 ms.
+// profiler, whose kernels took 430 and 17 us); a prompt's next 2048 tokens beside 127 single ones behind 8192 0.87 ms.
 // Registers: kernels of two tiles of rows to a sequence spill, 107 of a thread's for heads beyond 192, 16 for those of 65 to 128 with eight
 // wavefronts; no others do.
 #include "attend_dev.h"
@@ -19,7 +19,7 @@ namespace zkmi {
 namespace {
 
 static_assert(kPrefixTile == kTile && kPrefixWorkgroups == kWorkgroups, "");
-static const uint32_t kMostJoins = 1 << 20;  // workgroups of k_prefix_join that a head has
+static const uint32_t kMostJoins = 1 << 20;  // workgroups of k_prefix_join in a direction of the launch
 
 struct PrefixArgs : Args {
     static constexpr bool joined = true;
@@ -27,14 +27,17 @@ struct PrefixArgs : Args {
     uint32_t front_tokens;     // a multiple of the page
     uint32_t front_tiles;      // whole tiles of it; what is left is read with each sequence's own
     uint32_t front_splits, front_each, front_groups, row_tile;
+    uint32_t joins;  // workgroups of k_prefix_join that a head's rows have, in a direction of the launch
+    float seqs_per_row;
 };
-// Sums lie as [head][part][row of the batch], the parts of the prefix before the own ones: what is kept for a row does not go by how many
-// rows other sequences have.
-__device__ __forceinline__ size_t part_rows(const PrefixArgs& a, uint32_t h, uint32_t part) {
-    return ((size_t)h * (a.front_splits + a.splits) + part) * (a.s.rows * a.group);
+// Sums lie by the rows of the batch, so that what is kept does not go by how many rows other sequences have: those of the prefix as
+// [head][part][row], behind them the own ones as [part][sequence][head][row], which workgroups that run side by side write side by side.
+__device__ __forceinline__ size_t front_part(const PrefixArgs& a, uint32_t h, uint32_t part) {
+    return ((size_t)h * a.front_splits + part) * (a.s.rows * a.group);
 }
-__device__ __forceinline__ size_t own_part(const PrefixArgs& a, const SeqView& v, uint32_t, uint32_t h, uint32_t split) {
-    return part_rows(a, h, a.front_splits + split) + (uint32_t)v.row0 * a.group;
+__device__ __forceinline__ size_t own_part(const PrefixArgs& a, const SeqView& v, uint32_t, uint32_t h, uint32_t part) {
+    const size_t H = a.cache.kv_heads, R = a.s.rows * a.group;
+    return (a.front_splits + part) * H * R + ((size_t)v.row0 * H + (size_t)v.rows * h) * a.group;
 }
 
 // As for a sequence alone, but that its first tokens lie in the prefix's pages, and its first tiles are not its own.
@@ -87,7 +90,7 @@ __device__ __forceinline__ void attend_front(const PrefixArgs& a, char* lds, Fro
     const uint32_t r = r0 + (tid >> 6) * 32 + (tid & 31);
     const int32_t pos = r < R ? sh.place[r / a.group - (uint32_t)tok0] : -1;
     const SeqView all = {0, (int32_t)a.s.rows, 0, true};
-    attend_rows<DT, true, WV>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, part_rows(a, h, split), a.parts, a.parts_ml);
+    attend_rows<DT, true, WV>(a, lds, sh.many, all, 0, h, R, r0, tiles, pos, least, most, 0, true, front_part(a, h, split), a.parts, a.parts_ml);
 }
 
 // RT: tiles of 16 rows that a sequence and head has, 0: many rows.  Workgroups of one head lie eight apart where there are eight heads, so
@@ -113,28 +116,45 @@ __global__ __launch_bounds__(64 * WV, WV == 8 || (DT <= 4 && RT < 2) ? 2 : 1) vo
     }
 }
 
+// The sequence that has a row of the batch, for a wavefront; one that is not ok where none has it.  64 are looked at at once: those about where it
+// lies if all have as many rows, then those that a search of cu comes to, then all, if cu says that there is one (and does not rise).
+__device__ __forceinline__ SeqView seq_of(const PrefixArgs& a, int32_t token) {
+    const uint32_t n = a.s.seqs, lane = threadIdx.x & 63, most = n > 64 ? n - 64 : 0;
+    const int32_t about = (int32_t)((float)token * a.seqs_per_row) - 32;
+    uint32_t b0 = about <= 0 ? 0 : (uint32_t)about < most ? (uint32_t)about : most;
+    for (uint32_t turn = 0;; ++turn) {
+        const uint32_t b = b0 + lane < n ? b0 + lane : n - 1;
+        const int32_t from = a.s.cu[b], end = a.s.cu[b + 1], len = a.s.lens[b];
+        const uint64_t has = __ballot(from <= token && token < end);
+        if (has) {
+            const int at = __ffsll((long long)has) - 1;
+            return seq_view(a.s, a.page_log, __builtin_amdgcn_readlane(from, at), __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(len, at));
+        }
+        if (n <= 64 || (turn == 0 && token >= a.s.cu[n]) || turn * 64 >= n + 128) return SeqView{0, 0, 0, false};
+        if (turn == 0) {
+            b0 = 0;
+            for (uint32_t left = n; left > 64;) {
+                const uint32_t step = (left + 63) / 64, k = b0 + lane * step;
+                const uint64_t below = __ballot(lane * step < left && a.s.cu[k < n ? k : n - 1] <= token);
+                const uint32_t at = below ? (63 - (uint32_t)__builtin_clzll(below)) * step : 0;
+                b0 += at;
+                left = left - at < step ? left - at : step;
+            }
+        } else {
+            b0 = (turn - 1) * 64;
+        }
+    }
+}
+
 // A wavefront: one row of the batch and a head.  Lanes hold four dimensions each; the lanes left of 64 take parts in turn.
 __device__ __forceinline__ void join_row(const PrefixArgs& a, uint32_t h, uint32_t row) {
     const uint32_t H = a.cache.kv_heads, d = a.cache.head_dim, lane = threadIdx.x & 63, token = row / a.group;
-    // the first sequence that has the row: 64 of them are looked at at once
-    SeqView v;
-    bool found = false;
-    for (uint32_t b0 = 0; b0 < a.s.seqs && !found; b0 += 64) {
-        const uint32_t b = b0 + lane < a.s.seqs ? b0 + lane : a.s.seqs - 1;
-        const int32_t from = a.s.cu[b], end = a.s.cu[b + 1], len = a.s.lens[b];
-        const uint64_t has = __ballot(from <= (int32_t)token && (int32_t)token < end);
-        if (has) {
-            const int at = __ffsll((long long)has) - 1;
-            v = seq_view(a.s, a.page_log, __builtin_amdgcn_readlane(from, at), __builtin_amdgcn_readlane(end, at), __builtin_amdgcn_readlane(len, at));
-            found = true;
-        }
-    }
-    if (!found) return;  // nobody's
-    const size_t out0 = (size_t)token * a.orow + (size_t)(h * a.group + (row - token * a.group)) * a.ohead;
-    const size_t lse_at = (size_t)token * H * a.group + h * a.group + (row - token * a.group);
-    if (!v.ok) {
-        for (uint32_t i = lane; i < d; i += 64) put_at(a.out, out0 + i, __builtin_nanf(""), a.dtype);
-        if (a.lse && lane == 0) a.lse[lse_at] = __builtin_nanf("");
+    const SeqView v = seq_of(a, (int32_t)token);
+    if (!v.ok) {  // nobody's, or one of a sequence that is skipped
+        if (v.rows == 0) return;
+        const size_t head = h * a.group + (row - token * a.group);
+        for (uint32_t i = lane; i < d; i += 64) put_at(a.out, token * a.orow + head * a.ohead + i, __builtin_nanf(""), a.dtype);
+        if (a.lse && lane == 0) a.lse[(size_t)token * H * a.group + head] = __builtin_nanf("");
         return;
     }
     const uint32_t r = row - (uint32_t)v.row0 * a.group;
@@ -143,11 +163,12 @@ __device__ __forceinline__ void join_row(const PrefixArgs& a, uint32_t h, uint32
     const uint32_t front = pos >= 0 ? a.front_splits : 0;
     const Tiles tiles = a.few ? tiles_of(a, v, 0, v.rows - 1) : tiles_of_rows(a, v, r / a.row_tile * a.row_tile, a.row_tile);
     const uint32_t each = part_of(a, tiles), n = tiles.end - tiles.first, own = pos >= 0 && n ? (n + each - 1) / each : 0, parts = front + own;
-    const size_t first = part_rows(a, h, 0) + row;
-    const uint32_t R = a.s.rows * a.group;  // from a part to the next
+    const size_t R = a.s.rows * a.group, front0 = front_part(a, h, 0) + row, own0 = own_part(a, v, 0, h, 0) + r;
+    const size_t own_less = own0 - front * R * H;
+    const auto at = [&](uint32_t p) { return (p < front ? front0 : own_less) + p * (p < front ? R : R * H); };
     float m = -kInf, l = 0.0f;
     if (lane < parts) {
-        const float2 ml = a.parts_ml[first + (size_t)lane * R];
+        const float2 ml = a.parts_ml[at(lane)];
         m = ml.x;
         l = ml.y;
     }
@@ -161,7 +182,7 @@ __device__ __forceinline__ void join_row(const PrefixArgs& a, uint32_t h, uint32
         for (int u = 0; u < 8; ++u) {
             const uint32_t p = p0 + u * ways + way;
             x[u] = v4f{0, 0, 0, 0};
-            if (way < ways && p < parts) x[u] = ((const v4f*)a.parts)[(first + (size_t)p * R) * quads + c];
+            if (way < ways && p < parts) x[u] = ((const v4f*)a.parts)[at(p) * quads + c];
         }
         if (p0 == 0) {
             const float top = wave_max(m);
@@ -184,15 +205,22 @@ __device__ __forceinline__ void join_row(const PrefixArgs& a, uint32_t h, uint32
         }
     }
     if (way == 0) {
+        const size_t to = row_at(a, v, h, r, a.orow, a.ohead) + 4 * c;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) put_at(a.out, out0 + 4 * c + e, l == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
+        for (int e = 0; e < 4; ++e) put_at(a.out, to + e, l == 0.0f ? 0.0f : sum[e] * inv, a.dtype);
     }
-    if (a.lse && lane == 0) a.lse[lse_at] = lse_of(ref, l);
+    if (a.lse && lane == 0) a.lse[row_at(a, v, h, r, (size_t)H * a.group, 1)] = lse_of(ref, l);
 }
+// Workgroups behind those that join look the sequences over.
 __global__ __launch_bounds__(kBlock) void k_prefix_join(PrefixArgs a) {
-    const uint32_t R = a.s.rows * a.group, step = gridDim.x * (kBlock / 64);
-    for (uint32_t row = uniform(blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)); row < R; row += step) join_row(a, blockIdx.y, row);
+    if (blockIdx.x >= a.joins) {
+        const uint32_t b = (blockIdx.x - a.joins) * kBlock + threadIdx.x;
+        if (blockIdx.y + blockIdx.z == 0 && b < a.s.seqs && !seq_view(a.s, b, a.page_log).ok) report(a.s, ZK_FAULT_LENGTH);
+        return;
+    }
+    const uint32_t row = uniform((blockIdx.z * a.joins + blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6));
+    if (row < a.s.rows * a.group) join_row(a, blockIdx.y, row);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
@@ -217,8 +245,8 @@ int launch(const PrefixArgs& a, uint64_t own, hipStream_t s) {
     }
     if (lds > 60000) ZK_HIP_TRY(hipFuncSetAttribute((const void*)k_prefix<DT, RT, WV>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL((k_prefix<DT, RT, WV>), dim3((unsigned)(a.front_groups + own)), dim3(64 * WV), lds, s, a);
-    const size_t joins = div_up((size_t)a.s.rows * a.group, kBlock / 64);
-    hipLaunchKernelGGL(k_prefix_join, dim3((unsigned)(joins < kMostJoins ? joins : kMostJoins), a.cache.kv_heads), dim3(kBlock), 0, s, a);
+    hipLaunchKernelGGL(k_prefix_join, dim3(a.joins + (unsigned)div_up(a.s.seqs, kBlock), a.cache.kv_heads, (unsigned)div_up(div_up((size_t)a.s.rows * a.group, kBlock / 64), a.joins)),
+                       dim3(kBlock), 0, s, a);
     ZK_HIP_TRY(hipGetLastError());
     return ZK_OK;
 }
@@ -295,6 +323,9 @@ extern "C" int kvcache_attention_prefix(const kvcache_i8* cache, const void* q, 
     const uint64_t own = (uint64_t)seqs->seqs * cache->kv_heads * p.splits * (a.few ? 1 : div_up(most, p.row_tile));
     if (front + own >= (uint64_t)1 << 23) return ZK_E_BADARG;  // a launch holds fewer than 2^32 threads
     a.front_groups = (uint32_t)front;
+    const size_t joins = div_up(rows, kBlock / 64);
+    a.joins = (uint32_t)(joins < kMostJoins ? joins : kMostJoins);
+    a.seqs_per_row = (float)seqs->seqs / (float)seqs->rows;
     if (!ws) return ZK_E_BUFSZ;
     Carver cv(ws, ws_bytes);
     carve(cv, p, rows, cache->kv_heads, cache->head_dim, &a);

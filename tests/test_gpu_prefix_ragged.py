@@ -88,3 +88,52 @@ def test_a_part_of_a_prompt_beside_steps_takes_little():
     need = zk.kvcache_attention_prefix_workspace_bytes(128, sum(new), 2048, heads, H, d, shared * T, 4096)
     assert need < 32 << 20
     check(cache, q, cu, lens, table, shared, 0.125)
+
+
+@pytest.mark.parametrize("seqs", [65, 130, 1000])
+def test_many_sequences(seqs):
+    """Steps of more sequences than are looked at at once: all alike, some without rows, one with most rows, rows behind them that are nobody's."""
+    T, shared, d = 16, 4, 32
+    for new in ([1] * seqs, [(i * 7) % 3 for i in range(seqs)], [0] * (seqs - 2) + [90, 1], [70] + [1] * (seqs - 1)):
+        lens = [T * shared + n + (5 * i) % 40 for i, n in enumerate(new)]
+        cache, q, cu, table, _ = make(zk, new, lens, 2, 1, d, T, F16, seqs)
+        want, wlse = check(cache, q, cu, lens, table, shared, 0.2)
+        front, full, given = share(table, shared)
+        more = torch.cat([q, torch.full((300, 2, d), float("nan"), dtype=F16, device="cuda")])
+        out, lse = torch.full_like(more, 3.0), torch.full((more.shape[0], 2), 3.0, device="cuda")
+        fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+        rc, _, _ = call(cache, more, cu, lens, given, front, 0.2, out=out, lse=lse, fault=fault)
+        assert rc == zk.ZK_OK and fault.item() == 0
+        assert torch.equal(out[:q.shape[0]], want) and torch.equal(lse[:q.shape[0]], wlse)
+        assert out[q.shape[0]:].eq(3).all() and lse[q.shape[0]:].eq(3).all()
+
+
+@pytest.mark.parametrize("at,value", [(70, 10 ** 6), (70, -5), (150, 10 ** 6), (10, -1), (199, 40)])
+def test_many_sequences_of_which_one_is_refused(at, value):
+    """One entry of cu is none: the two sequences that it bounds are skipped, and the fault is told; rows that no skipped one claims are as without."""
+    seqs, T, shared, d = 200, 16, 4, 32
+    new = [1] * seqs
+    lens = [T * shared + 1 + i % 50 for i in range(seqs)]
+    cache, q, cu, table, _ = make(zk, new, lens, 2, 1, d, T, BF16, 3)
+    front, full, given = share(table, shared)
+    rc, want, wlse = call(cache, q, cu, lens, given, front, 0.2)
+    broken = list(cu)
+    broken[at] = value
+    claimed = torch.zeros(seqs, dtype=torch.bool, device="cuda")
+    for b in (at - 1, at):
+        lo, hi = max(broken[b], 0), min(broken[b + 1], seqs)
+        if hi > lo:
+            claimed[lo:hi] = True
+    pages = torch.tensor(front, dtype=torch.int32, device="cuda")
+    fault = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = torch.full_like(q, 3.0), torch.full((seqs, 2), 3.0, device="cuda")
+    rc, _, _ = zk.kvcache_attention_prefix(cache, q, *device(broken, lens, given), pages, 1, max(lens), 0.2, out=out, lse=lse, fault=fault)
+    assert rc == zk.ZK_OK and fault.item() == zk.ZK_FAULT_LENGTH
+    mine = torch.ones(seqs, dtype=torch.bool, device="cuda")
+    mine[at - 1:at + 1] = False     # rows of the sequences that are left
+    sure = mine & ~claimed
+    assert torch.equal(out[sure], want[sure]) and torch.equal(lse[sure], wlse[sure])
+    only = claimed & ~mine
+    assert out[only].isnan().all() and lse[only].isnan().all()
+    both = claimed & mine
+    assert (out[both].isnan() | (out[both] == want[both])).all()
