@@ -12,7 +12,9 @@
 // Measured: 8192 rows of 5120 bf16 through two norms and a gate to codes (378 MB) 88 us, 4.3 TB/s where a copy reaches 5.1, the vector
 // ALU 61% busy (3 us of it for the look at statistics); 777 rows of 4097 floats, which no 16-byte load takes, 15.6 us, 3.3 TB/s; 4096 of 5120 floats, two
 // norms and a gate to codes (357 MB), 79 us, 4.5 TB/s; 1024 of 20000 bf16 in LDS 78 us, 1.8 TB/s; codes of 8192 x 13824 f16 59 us, 5.8 TB/s (part of it
-// stays in the last cache); one row 3.8 us in a graph, latency, where a launch of nothing is 1.7.  A row that is added up again takes some 3 us more.
+// stays in the last cache); one row 3.8 us in a graph, latency, where a launch of nothing is 1.7.
+// A row whose mean is added up again takes 1.7 us more: layer norms of 8192 x 5120 bf16, of which one in 40 is, 46 us (42 if none were looked at), 4096 of
+// 5120 floats that were centred before, of which all are, 53 (35).
 #include "serve_dev.h"
 
 #pragma clang fp contract(off)
@@ -172,10 +174,11 @@ __device__ __forceinline__ double all_add(double x, Scratch& s, int turn, uint32
     return sum;
 }
 
-// As uniform.
-__device__ __forceinline__ double one_for_all(double x) {
+// A lane's value, for all.
+__device__ __forceinline__ double one_for_all(double x, int lane = 0) {
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    return __builtin_bit_cast(double, ((uint64_t)uniform((uint32_t)(b >> 32)) << 32) | uniform((uint32_t)b));
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
 // What a norm takes off and multiplies by.
@@ -184,15 +187,15 @@ struct Stats {
 };
 __device__ __forceinline__ double rstd_of(double variance, float eps) { return 1.0 / sqrt(variance + (double)eps); }
 
-// A sum of squares and what its additions have lost (Knuth's two-sum): together exact to some 2^-90 of it, since nothing cancels.
-struct Squares {
+// A sum and what its additions have lost (Knuth's two-sum): together exact to some 2^-90 of the summands' sizes.
+struct Whole {
     double sum = 0.0, lost = 0.0;
     __device__ __forceinline__ void add(double x) {
         const double s = sum + x, b = s - sum;
         lost += (sum - (s - b)) + (x - b);
         sum = s;
     }
-    __device__ __forceinline__ void add_of(double v, double mean) {  // (v - mean)^2: v - mean is d + less, d^2 is square and its own loss
+    __device__ __forceinline__ void add_square(double v, double mean) {  // (v - mean)^2: v - mean is d + less, d^2 is square and its own loss
         const double d = v - mean, b = d - v, less = (v - (d - b)) - (mean + b), square = d * d;
         add(square);
         lost += __builtin_fma(d, d, -square) + 2.0 * d * less;
@@ -204,7 +207,7 @@ struct Squares {
         lost += also;
     }
 };
-__device__ __forceinline__ double all_add(Squares x, Scratch& s, int turn, uint32_t waves) {
+__device__ __forceinline__ Whole all_add(Whole x, Scratch& s, int turn, uint32_t waves) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     x.add_partner<0x111, 0xf>();
     x.add_partner<0x112, 0xf>();
@@ -217,16 +220,16 @@ __device__ __forceinline__ double all_add(Squares x, Scratch& s, int turn, uint3
         s.lost[turn & 1][wave] = x.lost;
     }
     __syncthreads();
-    Squares all;
-#pragma unroll 1
-    for (uint32_t w = 0; w < waves; ++w) {
-        all.add(s.sums[turn & 1][w]);
-        all.lost += s.lost[turn & 1][w];
-    }
-    return all.sum + all.lost;
+    const bool has = (lane & 15) < waves;  // 16 wavefronts at most, whose sums a row of lanes adds up
+    x = {has ? s.sums[turn & 1][lane & 15] : 0.0, has ? s.lost[turn & 1][lane & 15] : 0.0};
+    x.add_partner<0x111, 0xf>();
+    x.add_partner<0x112, 0xf>();
+    x.add_partner<0x114, 0xf>();
+    x.add_partner<0x118, 0xf>();
+    return {one_for_all(x.sum, 15), one_for_all(x.lost, 15)};
 }
 
-// A sum of floats, which may cancel, in fixed point: a float's 24 bits lie in two digits, which integers add up in any order.
+// A sum of floats that cancels, in fixed point: a float's 24 bits lie in two digits, which integers add up in any order.
 __device__ __forceinline__ void add_digits(Scratch& s, float v) {
     const uint32_t bits = float_bits(v), e = (bits >> 23) & 0xff, at = e ? e - 1 : 0;
     const uint64_t x = (uint64_t)((bits & 0x7fffffu) | (e ? 0x800000u : 0u)) << (at & 31);
@@ -273,41 +276,55 @@ __device__ __forceinline__ double digits_value(Scratch& s) {
 
 // Whether two sums of the same row in other orders might come to statistics that differ in 32 bits.  A summand goes through `each` additions
 // (at most 32) of its thread, 6 of its wavefront and those of the workgroup's, so that a sum is within as many times 2^-53 of its summands' sizes,
-// whose mean is at most |mean| + sqrt(variance) (Cauchy).  Once in some 2^20 rows they might (where a mean is small beside its row, oftener); then
-// the row is added up again, exactly.  What is given is the same in every thread.
-__device__ __forceinline__ bool undecided(int kind, double mean, double variance, double rstd, float eps, uint32_t each, uint32_t waves) {
+// whose mean is at most |mean| + sqrt(variance) (Cauchy).  For one root in some 2^20 they might, and for one mean in some 2^17 of 32 bits, of 16 bits in 40 (in
+// the very middle), oftener where it is small beside its row; then the row is added up again.  What is given is the same in every thread.
+enum { kMeanOpen = 1, kRstdOpen = 2 };
+__device__ __forceinline__ uint32_t undecided(int kind, double mean, double variance, double rstd, float eps, uint32_t each, uint32_t waves) {
     // within 2^-45 of the middle between two floats, or below the normal ones
     const uint64_t bits = __builtin_bit_cast(uint64_t, rstd);
     const uint32_t low = ((uint32_t)bits - (0x10000000u - 256u)) & 0x1fffffffu, high = (uint32_t)(bits >> 32);
-    bool open = low < 512u || high - 1u < 0x38100000u - 1u;
+    uint32_t open = low < 512u || high - 1u < 0x38100000u - 1u ? kRstdOpen : 0;
     if (kind == ZK_NORM_LAYER) {
         const double by = (double)(each + waves + 10) * 0x1.01p-53 * (__builtin_fabs(mean) + __builtin_amdgcn_sqrt(variance));  // the root to some 2^-20
+        if (__ballot((float)(mean - by) < (float)(mean + by))) open |= kMeanOpen;
         // around a mean that is off by as much the squares come to by^2 more
-        open = open || __ballot((float)(mean - by) < (float)(mean + by) || by * by * 0x1p47 > variance + (double)eps);
+        if (__ballot(by * by * 0x1p47 > variance + (double)eps)) open |= kRstdOpen;
     }
     return open;
 }
-// `over` hands each of the thread's elements on, and whether it is one of the row.
+// The statistics st of a row of which some are undecided, mean and variance as they were before.  `over` hands each of the thread's elements on, and
+// whether it is one of the row.  The mean of numbers of 16 bits often lies in the very middle, but nothing is lost when they are added up; where
+// something is, and two numbers of 64 bits leave the mean open too, it cancels and is taken in fixed point.
 template <typename Over>
-__device__ __forceinline__ Stats exact_stats(int kind, double n, float eps, Scratch& s, int& turn, uint32_t waves, Over over) {
-    double mean = 0.0;
+__device__ __forceinline__ void decide(Stats& st, uint32_t open, int kind, double mean, double variance, double n, float eps, Scratch& s, int& turn, uint32_t waves,
+                                       Over over) {
     if (kind == ZK_NORM_LAYER) {
-        const int slot = turn++ & 1;
-        for (uint32_t k = threadIdx.x; k < kDigits * kCopies; k += blockDim.x) s.digits[0][k] = 0;
-        __syncthreads();
-        over([&](float v, bool in) { add_digits(s, in ? v : 0.0f); });
-        __syncthreads();
-        if (threadIdx.x < kDigits)
-            for (uint32_t c = 1; c < kCopies; ++c) s.digits[threadIdx.x][0] += s.digits[threadIdx.x][c];
-        __syncthreads();
-        if (threadIdx.x == 0) s.sums[slot][0] = digits_value(s);
-        __syncthreads();
-        mean = s.sums[slot][0] / n;
+        Whole sum;
+        over([&](float v, bool in) { sum.add(in ? (double)v : 0.0); });
+        const Whole all = all_add(sum, s, turn++, waves);
+        const double by = 0x1p-85 * (__builtin_fabs(mean) + __builtin_amdgcn_sqrt(variance));
+        mean = (all.sum + all.lost) / n;
+        if (__ballot(all.lost != 0.0 && (float)(mean - by) < (float)(mean + by))) {
+            const int slot = turn++ & 1;
+            for (uint32_t k = threadIdx.x; k < kDigits * kCopies; k += blockDim.x) s.digits[0][k] = 0;
+            __syncthreads();
+            over([&](float v, bool in) { add_digits(s, in ? v : 0.0f); });
+            __syncthreads();
+            if (threadIdx.x < kDigits)
+                for (uint32_t c = 1; c < kCopies; ++c) s.digits[threadIdx.x][0] += s.digits[threadIdx.x][c];
+            __syncthreads();
+            if (threadIdx.x == 0) s.sums[slot][0] = digits_value(s);
+            __syncthreads();
+            mean = s.sums[slot][0] / n;
+        }
+        st.mean = (float)mean;
     }
-    Squares squares;
-    over([&](float v, bool in) { squares.add_of(in ? (double)v : mean, mean); });
-    const double variance = all_add(squares, s, turn++, waves) / n;
-    return Stats{(float)mean, (float)rstd_of(variance, eps)};
+    if (open & kRstdOpen) {
+        Whole squares;
+        over([&](float v, bool in) { squares.add_square(in ? (double)v : mean, mean); });
+        const Whole all = all_add(squares, s, turn++, waves);
+        st.rstd = (float)rstd_of((all.sum + all.lost) / n, eps);
+    }
 }
 __device__ __forceinline__ float normed(float v, int kind, const Stats& st) {
     if (kind == ZK_NORM_LAYER) v = v - st.mean;
@@ -338,8 +355,9 @@ __device__ __forceinline__ void normalise(float (&v)[E], int kind, float eps, co
         }
         const double variance = all_add(sum, s, turn++, waves) / n, rstd = one_for_all(rstd_of(variance, eps));
         Stats st = {(float)mean, (float)rstd};
-        if (__builtin_expect(undecided(kind, mean, variance, rstd, eps, E, waves), 0))
-            st = exact_stats(kind, n, eps, s, turn, waves, [&](auto take) {
+        const uint32_t open = undecided(kind, mean, variance, rstd, eps, E, waves);
+        if (__builtin_expect(open, 0))
+            decide(st, open, kind, mean, variance, n, eps, s, turn, waves, [&](auto take) {
 #pragma unroll
                 for (int i = 0; i < E; ++i) take(v[i], at.in(i));
             });
@@ -421,8 +439,8 @@ __device__ __forceinline__ void store_codes(int8_t* codes, size_t row, float* sc
     }
 }
 
-// Eight wavefronts to a SIMD where eight elements do: 777 rows of 4097 floats 16.3 -> 14.6 us, though registers spill (6 to 8 of a thread's
-// where no 16-byte load is taken, 14 of floats in whole runs); five with 16 elements of 16 bits, which would be four with the registers that the
+// Eight wavefronts to a SIMD where eight elements do: 777 rows of 4097 floats 16.3 -> 14.6 us, though registers spill (13 words of a thread's
+// where no 16-byte load is taken, 5 of floats in whole runs, most of them on the way of rows that are undecided); five with 16 elements of 16 bits, which would be four with the registers that the
 // second sums ask for (8192 rows of 5120 bf16 90 us, 114 with four).
 template <int DT, int E, bool WIDE>
 __global__ __launch_bounds__(kMostThreads, E <= 8 ? 8 : DT == ZK_F32 ? 4 : 5) void k_block_norm(NormArgs n) {
@@ -510,12 +528,13 @@ __global__ __launch_bounds__(kMostThreads, 8) void k_block_norm_long(NormArgs n)
             sum = __builtin_fma(d, d, sum);
         }
         const double variance = all_add(sum, s, turn++, waves) / (double)dim, rstd = one_for_all(rstd_of(variance, a.eps));
-        if (__builtin_expect(undecided(kind, mean, variance, rstd, a.eps, 32, waves), 0))
-            return exact_stats(kind, (double)dim, a.eps, s, turn, waves, [&](auto take) {
-                for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) take(line[i], true);
-            });
         st.rstd = (float)rstd;
         st.mean = (float)mean;
+        const uint32_t open = undecided(kind, mean, variance, rstd, a.eps, 32, waves);
+        if (__builtin_expect(open, 0))
+            decide(st, open, kind, mean, variance, (double)dim, a.eps, s, turn, waves, [&](auto take) {
+                for (uint32_t i = threadIdx.x; i < dim; i += kMostThreads) take(line[i], true);
+            });
         return st;
     };
     auto finished = [&](float v, int kind, const Stats& st, const void* gain, const void* bias, uint32_t i) {
