@@ -8,8 +8,8 @@
 //
 // Measured, 8 heads of 128 and 40 of queries, whole calls in a graph: a step of 64 sequences behind 8192 tokens 37 us (11.1 GFLOP, 54 MB: of
 // it 15 are latency, a prefix of one page takes as long, 15 the tiles, 1.2 each, and the rest parts on their way to memory and back); 16 questions
-// of up to 64 tokens behind 32768 377 to 388 us, 820 to 843 TFLOP/s, on one card, 416 on another (vector ALU 56% and matrix cores 41% busy in a run under the
-// profiler, whose kernels took 430 and 17 us); a prompt's next 2048 tokens beside 127 single ones behind 8192 0.87 ms.
+// of up to 64 tokens behind 32768 377 to 388 us, 820 to 843 TFLOP/s, on one card, 416 on another (vector ALU 55% and matrix cores 41% busy in a run under the
+// profiler, whose kernels took 422 and 17 us); a prompt's next 2048 tokens beside 127 single ones behind 8192 0.87 ms.
 // Registers: kernels of two tiles of rows to a sequence spill, 107 of a thread's for heads beyond 192, 16 for those of 65 to 128 with eight
 // wavefronts; no others do.
 #include "attend_dev.h"

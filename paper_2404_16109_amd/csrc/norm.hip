@@ -10,7 +10,7 @@
 // have moved it over the middle between two floats, its row is added up again without any (Ziv's test).
 //
 // Measured: 8192 rows of 5120 bf16 through two norms and a gate to codes (378 MB) 88 us, 4.3 TB/s where a copy reaches 5.1, the vector
-// ALU 61% busy (3 us of it for the look at statistics); 777 rows of 4097 floats, which no 16-byte load takes, 15.6 us, 3.3 TB/s; 4096 of 5120 floats, two
+// ALU 61% busy (3 us of it for the look at statistics); 777 rows of 4097 floats, which no 16-byte load takes, 14.9 us, 3.4 TB/s; 4096 of 5120 floats, two
 // norms and a gate to codes (357 MB), 79 us, 4.5 TB/s; 1024 of 20000 bf16 in LDS 78 us, 1.8 TB/s; codes of 8192 x 13824 f16 59 us, 5.8 TB/s (part of it
 // stays in the last cache); one row 3.8 us in a graph, latency, where a launch of nothing is 1.7.
 // A row whose mean is added up again takes 1.7 us more: layer norms of 8192 x 5120 bf16, of which one in 40 is, 46 us (42 if none were looked at), 4096 of
